@@ -491,6 +491,268 @@ cl_status cl_allocate_ranks(int32_t n, const float* const* sigma, const int32_t*
  */
 cl_status cl_layer_sensitivity(int32_t L, const double* D, int32_t K, double* S);
 
+/*
+ * cl_kv_cache -- keys and values of many sequences in one pool of pages.
+ *  k, v       device [num_pages][kv_heads][page_size][head_dim] of dtype
+ *             (CL_FP16 or CL_BF16), 16-byte aligned: a head's keys of a page
+ *             are one contiguous run, which is what attention streams
+ *  page_size  a power of two, 1..1024;  kv_heads * head_dim, and so the rows,
+ *             are the same for every page.  A pool may pass 2^31 elements.
+ *  head_dim   64, 128 or 256 (CL_EUNSUPPORTED otherwise)
+ */
+typedef struct cl_kv_cache {
+    void* k;
+    void* v;
+    int32_t num_pages;
+    int32_t page_size;
+    int32_t kv_heads;
+    int32_t head_dim;
+    int32_t dtype;
+} cl_kv_cache;
+
+/*
+ * cl_kv_batch -- the sequences of one step: their new tokens and where their
+ * keys stand.  The same descriptor serves cl_kv_append and cl_attention.
+ *  kv_len       device int32 [num_seqs]: keys of the sequence after the step,
+ *               the shared prefix and the new tokens among them
+ *  q_start      device int32 [num_seqs + 1]: sequence b's new tokens are rows
+ *               q_start[b] .. q_start[b+1] - 1 of every token array; or NULL:
+ *               every sequence has q_len of them (tokens = num_seqs * q_len)
+ *  page_table   device int32 [num_seqs][table_width]: the pages of the keys
+ *               behind the prefix, key prefix_len + i in row i % page_size of
+ *               entry i / page_size.  Entries past kv_len are not read.
+ *  prefix_table device int32 [ceil(prefix_len / page_size)]: the pages of the
+ *               first prefix_len keys, the same for every sequence; NULL with
+ *               prefix_len 0
+ *  tokens       rows of the token arrays (>= 1); rows of no sequence are left
+ *               alone
+ *  q_len        the most new tokens of one sequence (>= 1); further ones are
+ *               not attended for
+ *  max_kv_len   an upper bound of kv_len, which sizes the launch
+ * Token i of a sequence with n keys and a new tokens stands at position
+ * n - a + i.  The arrays live in device memory, so a wrong entry cannot fail
+ * the call; the kernels hold every value inside these bounds: a kv_len is cut
+ * to 0..min(max_kv_len, prefix_len + table_width * page_size), a q_start to
+ * 0..tokens, and a page outside 0..num_pages - 1 is not written, and where
+ * attention meets it among a sequence's keys, that sequence's outputs are NaN.
+ */
+typedef struct cl_kv_batch {
+    const int32_t* q_start;
+    const int32_t* kv_len;
+    const int32_t* page_table;
+    const int32_t* prefix_table;
+    int32_t num_seqs;
+    int32_t tokens;
+    int32_t q_len;
+    int32_t table_width;
+    int32_t prefix_len;
+    int32_t max_kv_len;
+} cl_kv_batch;
+
+/*
+ * cl_rope -- rotary positions: pair j of a head's first rot_dim values turns
+ * by the angle position * inv_freq[j], pairs (x_j, x_{j + rot_dim/2}) or,
+ * interleaved, (x_2j, x_{2j+1}); the other values stay.
+ *  inv_freq   device float32 [rot_dim / 2], radians a position (cl_rope_frequencies
+ *             makes the usual ones, long contexts included)
+ *  rot_dim    a multiple of 8, 8..head_dim
+ *  magnitude  factor of the rotated pairs (1, or cl_rope_frequencies')
+ */
+typedef struct cl_rope {
+    const float* inv_freq;
+    int32_t rot_dim;
+    int32_t interleaved;
+    float magnitude;
+} cl_rope;
+
+/* Scaling of rotary frequencies for contexts beyond the trained length. */
+enum { CL_ROPE_PLAIN = 0, CL_ROPE_LINEAR = 1, CL_ROPE_BASE = 2, CL_ROPE_BANDS = 3, CL_ROPE_RAMP = 4 };
+
+/*
+ * cl_rope_frequencies -- inv_freq[j] = base^(-2 j / rot_dim), scaled (host
+ * code, fp64, rounded once to float32):
+ *  CL_ROPE_PLAIN   as it is (factor and the rest unused)
+ *  CL_ROPE_LINEAR  divided by factor (positions interpolated)
+ *  CL_ROPE_BASE    with base factor^(rot_dim / (rot_dim - 2)) times as large,
+ *                  which divides the slowest pair by factor and leaves the
+ *                  fastest
+ *  CL_ROPE_BANDS   by turns t_j = trained_len inv_freq[j] / (2 pi) over the
+ *                  trained length: t_j >= high kept, t_j <= low divided by
+ *                  factor, between them the mean of both weighted by
+ *                  (t_j - low) / (high - low)
+ *  CL_ROPE_RAMP    the same mean, weighted by a ramp that is linear in j
+ *                  between the pairs that make `high` and `low` turns:
+ *                  j(t) = rot_dim ln(trained_len / (2 pi t)) / (2 ln base), its
+ *                  ends rounded outward to whole pairs and held in
+ *                  0..rot_dim - 1; *magnitude = 0.1 ln(factor) + 1
+ *  factor >= 1; 0 < low < high; trained_len >= 1; rot_dim even, 4..1024;
+ *  base > 1.  *magnitude is 1 for the other kinds.
+ * Errors: CL_EINVAL (nothing written).
+ */
+cl_status cl_rope_frequencies(int32_t rot_dim, double base, int32_t kind, double factor, double trained_len,
+                              double low, double high, float* inv_freq, float* magnitude);
+
+/*
+ * cl_kv_append -- the new tokens' keys and values into the cache, keys and
+ * queries rotated on the way (the step between the Q/K/V window and
+ * attention): one launch.  Optional before the rotation: each head of q and
+ * k divided by its root mean square, x / sqrt(mean x^2 + eps) * norm.
+ * Computed in float32 (the angle in fp64), rounded once.
+ *
+ *  rope       NULL: no rotation
+ *  q          device [tokens][q_heads][head_dim] of the cache's dtype, a
+ *             token's heads contiguous, q_stride elements from token to
+ *             token (a view of a fused projection); NULL with q_heads 0
+ *  k, v       device [tokens][kv_heads][head_dim], strides as q's
+ *  q_norm, k_norm  device [head_dim] of the cache's dtype, or NULL
+ *  positions  device int32 [tokens] used for the angles in place of the
+ *             tokens' positions, or NULL
+ *  q_out      device [tokens][q_heads][head_dim], dense (may be q, if q is)
+ * A token at a position below prefix_len (the shared pages are never
+ * written), or below 0, is not stored; its query is rotated all the same.
+ * Errors: CL_EINVAL for bad descriptors, null or misaligned pointers (2
+ * bytes; 8 and strides of 4 take wider accesses), strides shorter than a
+ * token's heads; CL_EUNSUPPORTED for a head_dim that the cache does not take.
+ */
+cl_status cl_kv_append(const cl_kv_cache* cache, const cl_kv_batch* batch, const cl_rope* rope, const void* q,
+                       int64_t q_stride, int32_t q_heads, const void* k, int64_t k_stride, const void* v,
+                       int64_t v_stride, const void* q_norm, const void* k_norm, float eps,
+                       const int32_t* positions, void* q_out, void* stream);
+
+/*
+ * cl_attention -- the new tokens' attention over the cache:
+ *     o = sum_j e^{s_j} v_j / sum_j e^{s_j},   s_j = scale q . k_j,
+ * for every token and head over the keys it sees (query heads
+ * h (q_heads / kv_heads) .. share key head h).  With n keys, a token at
+ * position p sees key j < n, only j <= p if causal, and only j > p - window if
+ * window > 0.  A token that sees no key gets zeros and lse = -inf.  A hidden
+ * key's or value's contents do not matter if it stands at or behind n; those
+ * of the sequence itself must be finite.
+ * One call serves single tokens, drafted tokens and prompts, mixed as they
+ * come; the keys of a shared prefix are read once for all sequences.
+ *
+ *  q          device [tokens][q_heads][head_dim] of the cache's dtype (rotated),
+ *             q_stride elements from token to token, 16-byte aligned rows
+ *             (q_stride a multiple of 8); q_heads a multiple of kv_heads
+ *  out        device [tokens][q_heads][head_dim] of out_dtype, 16-byte aligned
+ *  lse        device float32 [tokens][q_heads], ln sum_j e^{s_j}, or NULL
+ *  ws         device workspace of cl_attention_workspace(...) bytes, 256-byte
+ *             aligned (partial results of keys that were split over workgroups)
+ * Scores, softmax statistics and sums are float32; the probabilities enter the
+ * second product as the cache's dtype.  Results do not depend on the order
+ * in which workgroups run.
+ * Errors: CL_EINVAL, CL_EUNSUPPORTED (head_dim), CL_EWORKSPACE, CL_EHIP.
+ */
+cl_status cl_attention(const cl_kv_cache* cache, const cl_kv_batch* batch, const void* q, int64_t q_stride,
+                       int32_t q_heads, float scale, int32_t causal, int32_t window, void* out, int32_t out_dtype,
+                       float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes for cl_attention: by the descriptors' sizes alone (the device
+ * arrays are not read), 0 for rejected arguments. */
+size_t cl_attention_workspace(const cl_kv_cache* cache, const cl_kv_batch* batch, int32_t q_heads);
+
+/* Scores of a router. */
+enum { CL_SOFTMAX = 1, CL_SIGMOID = 2 };
+
+/*
+ * cl_router -- how tokens choose experts.
+ *  bias        device float32 [num_experts], added to the scores for the
+ *              choice only (a balance bias), or NULL
+ *  num_experts 1..1024;  k  1..64 experts a token
+ *  score       CL_SOFTMAX over all experts, or CL_SIGMOID of each
+ *  groups      experts in `groups` (1..64) runs of equal length, of which the
+ *              top_groups with the highest sum of their group_best (1 or 2)
+ *              best biased scores stay open; 1 and 1 for none
+ *  renormalize divide the chosen weights by their sum
+ *  scale       factor of the weights at the end
+ */
+typedef struct cl_router {
+    const float* bias;
+    int32_t num_experts;
+    int32_t k;
+    int32_t score;
+    int32_t groups;
+    int32_t top_groups;
+    int32_t group_best;
+    int32_t renormalize;
+    float scale;
+} cl_router;
+
+/*
+ * cl_moe_route -- the routing table, weights and per-slot ranks that the MoE
+ * calls take, from the router's logits.  Each token's k experts by descending
+ * score + bias (without a bias by descending logit), ties to the lower id,
+ * their weights the unbiased scores.  A NaN logit is chosen last; by softmax
+ * it makes the token's weights NaN.  A token whose logits are all -inf gets
+ * weights of zero.
+ * Per-slot ranks (Section 4.3.3, Expert Activation for MoE Models): for each
+ * of `tables` linears the level nearest to k w r_e, r_e the expert's static
+ * rank, ties to the lower level: slot_ranks of cl_moe_linear_decode_window.
+ *
+ *  logits       device [T][num_experts] of logits_dtype (CL_FP16, CL_BF16, CL_FP32)
+ *  ids          device int32 [T][k] (output);  weights  device float32 [T][k] (output)
+ *  tables       0..4;  expert_ranks  host array [tables] of device int32
+ *               [num_experts];  slot_ranks  host array [tables] of device
+ *               int32 [T][k] (outputs)
+ *  levels       host int32 [nlevels], 1..16 values >= 0, strictly increasing
+ * T is any number >= 1.  Scores are float32.
+ * Errors: CL_EINVAL for any argument outside the above, and for a k that the
+ * open groups cannot fill.
+ */
+cl_status cl_moe_route(const cl_router* router, const void* logits, int32_t logits_dtype, int32_t T, int32_t* ids,
+                       float* weights, int32_t tables, const int32_t* const* expert_ranks, const int32_t* levels,
+                       int32_t nlevels, int32_t* const* slot_ranks, void* stream);
+
+/* Norms over a row x of d values: x / sqrt(mean x^2 + eps), or the same of
+ * x - mean x. */
+enum { CL_NORM_RMS = 1, CL_NORM_LAYER = 2 };
+
+/*
+ * cl_norm -- the norms around a block and how its output joins the residual.
+ *  weight       device [d]: of the norm before the next block
+ *  bias         device [d] added after it, or NULL
+ *  post_weight  device [d]: of a norm of the block's output, or NULL for none
+ *  gate         device [d], or [T][d] with gate_per_token, or NULL for none
+ *  w_dtype      of these four (CL_FP16, CL_BF16 or CL_FP32)
+ *  kind         CL_NORM_RMS or CL_NORM_LAYER, for both norms
+ *  alpha, beta  factors of the residual and of the block's output
+ */
+typedef struct cl_norm {
+    const void* weight;
+    const void* bias;
+    const void* post_weight;
+    const void* gate;
+    int32_t w_dtype;
+    int32_t kind;
+    int32_t gate_per_token;
+    float eps;
+    float alpha;
+    float beta;
+} cl_norm;
+
+/*
+ * cl_residual_norm -- a block's output into the residual stream, and the next
+ * block's input, in one pass:
+ *     u = y[t], or sum_j slot_weights[t][j] y[t][j] (a MoE token's slots),
+ *     u = N(u) post_weight           (if post_weight),
+ *     h = alpha residual + beta gate u,
+ *     out = N(h) weight + bias.
+ * float32 throughout; h and out are each rounded once (out is formed from the
+ * unrounded h).
+ *
+ *  y            device [T][d], or [T][slots][d] with slots > 0, of y_dtype
+ *  slot_weights device float32 [T][slots]; NULL with slots 0 (slots 0..64)
+ *  residual     device [T][d] of h_dtype, or NULL: none
+ *  h            device [T][d] of h_dtype (may be residual), or NULL: not written
+ *  out          device [T][d] of out_dtype; may not overlap an input
+ * T >= 1; d 1..32768 (CL_EUNSUPPORTED beyond).  Any d and element alignment;
+ * d a multiple of 8 with 16-byte aligned arrays takes wide accesses.
+ * Errors: CL_EINVAL, CL_EUNSUPPORTED, CL_EHIP.
+ */
+cl_status cl_residual_norm(const cl_norm* norm, const void* y, int32_t y_dtype, int32_t slots,
+                           const float* slot_weights, const void* residual, void* h, int32_t h_dtype, void* out,
+                           int32_t out_dtype, int32_t T, int32_t d, void* stream);
+
 /* Message describing the last non-CL_OK status returned on this thread. */
 const char* cl_last_error(void);
 

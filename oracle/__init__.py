@@ -30,6 +30,7 @@ comp    -- compensation factors from the SVD of the residual
 linear  -- the compensated forward (decode and prefill compute the same thing)
 moe     -- expert-gathered compensated forward
 ranks   -- rank allocation from the residual spectra (Section 4.3, Appendix B.1)
+layer   -- between the linears of a layer: attention, rotary positions, routing, norms
 """
 
-from . import quant, comp, linear, moe, ranks  # noqa: F401
+from . import quant, comp, layer, linear, moe, ranks  # noqa: F401

@@ -42,6 +42,37 @@ class LowRankC(ctypes.Structure):
                 ("rank", ctypes.c_int32)]
 
 
+class KvCacheC(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class KvBatchC(ctypes.Structure):
+    _fields_ = [("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("prefix_table", ctypes.c_void_p), ("num_seqs", ctypes.c_int32), ("tokens", ctypes.c_int32),
+                ("q_len", ctypes.c_int32), ("table_width", ctypes.c_int32), ("prefix_len", ctypes.c_int32),
+                ("max_kv_len", ctypes.c_int32)]
+
+
+class RopeC(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("magnitude", ctypes.c_float)]
+
+
+class RouterC(ctypes.Structure):
+    _fields_ = [("bias", ctypes.c_void_p), ("num_experts", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("score", ctypes.c_int32), ("groups", ctypes.c_int32), ("top_groups", ctypes.c_int32),
+                ("group_best", ctypes.c_int32), ("renormalize", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class NormC(ctypes.Structure):
+    _fields_ = [("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("post_weight", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("w_dtype", ctypes.c_int32), ("kind", ctypes.c_int32),
+                ("gate_per_token", ctypes.c_int32), ("eps", ctypes.c_float), ("alpha", ctypes.c_float),
+                ("beta", ctypes.c_float)]
+
+
 _lib = None
 
 _SIGNATURES = {
@@ -105,6 +136,27 @@ _SIGNATURES = {
     "cl_linear_decode_glu": (ctypes.c_int32, [ctypes.POINTER(QWeightC), ctypes.POINTER(LowRankC), ctypes.c_void_p,
                                               ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int32,
                                               ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "cl_rope_frequencies": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_double, ctypes.c_int32, ctypes.c_double,
+                                             ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_void_p,
+                                             ctypes.POINTER(ctypes.c_float)]),
+    "cl_kv_append": (ctypes.c_int32, [ctypes.POINTER(KvCacheC), ctypes.POINTER(KvBatchC), ctypes.POINTER(RopeC),
+                                      ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p,
+                                      ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                      ctypes.c_void_p, ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p,
+                                      ctypes.c_void_p]),
+    "cl_attention_workspace": (ctypes.c_size_t, [ctypes.POINTER(KvCacheC), ctypes.POINTER(KvBatchC),
+                                                 ctypes.c_int32]),
+    "cl_attention": (ctypes.c_int32, [ctypes.POINTER(KvCacheC), ctypes.POINTER(KvBatchC), ctypes.c_void_p,
+                                      ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_int32, ctypes.c_int32,
+                                      ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p,
+                                      ctypes.c_size_t, ctypes.c_void_p]),
+    "cl_moe_route": (ctypes.c_int32, [ctypes.POINTER(RouterC), ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32,
+                                      ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
+                                      ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p]),
+    "cl_residual_norm": (ctypes.c_int32, [ctypes.POINTER(NormC), ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32,
+                                          ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
+                                          ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                          ctypes.c_void_p]),
 }
 
 
@@ -124,14 +176,16 @@ def lib():
             fn = handle[name]
             res, args = _SIGNATURES[name]
             fn.restype = res
-            fn.argtypes = [a if a in (ctypes.c_int32, ctypes.c_size_t) else ctypes.c_void_p for a in args]
+            fn.argtypes = [a if a in _SCALARS else ctypes.c_void_p for a in args]
             _packed[name] = fn
         _lib = handle
     return _lib
 
 
 _PACKED = ("cl_linear_decode", "cl_linear_decode_noalloc", "cl_linear_decode_window", "cl_linear_decode_glu",
-           "cl_linear_prefill", "cl_linear_workspace", "cl_linear_window_workspace", "cl_prefill_workspace")
+           "cl_linear_prefill", "cl_linear_workspace", "cl_linear_window_workspace", "cl_prefill_workspace",
+           "cl_kv_append", "cl_attention", "cl_attention_workspace", "cl_moe_route", "cl_residual_norm")
+_SCALARS = (ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float)
 _packed = {}
 
 
@@ -669,3 +723,292 @@ def build_compensation(W, w, r_max, stream=None):
     _check(lib().cl_build_compensation(_ptr(W), ctypes.byref(q), r_max, _ptr(A), _ptr(B), _ptr(sigma), _ptr(ws),
                                        ws.numel(), _stream(stream)))
     return A, B, sigma
+
+
+# ------------------------------------- between the linears of a decoder layer
+
+_KV = (torch.float16, torch.bfloat16)
+_PACK_CACHE = struct.Struct("PPiiiii").pack
+_PACK_BATCH = struct.Struct("PPPPiiiiii").pack
+_PACK_ROPE = struct.Struct("Piif").pack
+_PACK_ROUTER = struct.Struct("Piiiiiiif").pack
+_PACK_NORM = struct.Struct("PPPPiiifff").pack
+_SCORES = {"softmax": 1, "sigmoid": 2}
+_NORMS = {"rms": 1, "layer": 2}
+ROPE_KINDS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
+
+
+def _opt_ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+class KvCache:
+    """A pool of pages: k and v [num_pages][kv_heads][page_size][head_dim],
+    fp16 or bf16.  Checked once, when it is made."""
+
+    def __init__(self, k, v):
+        chk = _Checked()
+        _dev_tensor(k, "k", _KV, chk=chk)
+        _need(k.dim() == 4, "k must be [num_pages][kv_heads][page_size][head_dim]")
+        _dev_tensor(v, "v", (k.dtype,), k.shape, chk)
+        chk.on_gpu()
+        self.k, self.v = k, v
+        self.num_pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        self.dtype = k.dtype
+        self._bytes = _PACK_CACHE(k.data_ptr(), v.data_ptr(), self.num_pages, self.page_size, self.kv_heads,
+                                  self.head_dim, _DTYPE_CODE[k.dtype])
+
+    @classmethod
+    def empty(cls, num_pages, page_size, kv_heads, head_dim, dtype=torch.float16, device="cuda"):
+        """A new pool; its pages hold nothing until something is appended."""
+        shape = (num_pages, kv_heads, page_size, head_dim)
+        return cls(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device))
+
+    def packed(self):
+        """The bytes of a cl_kv_cache."""
+        return self._bytes
+
+
+class KvBatch:
+    """The sequences of a step (cl_kv_batch): kv_len int32 [num_seqs],
+    page_table int32 [num_seqs][table_width], the step's ``tokens``, and
+    q_start int32 [num_seqs + 1] or None for q_len tokens each.  Checked once,
+    when it is made; the arrays' values may change between steps as long as
+    they keep to q_len and max_kv_len (by default what the tables can hold)."""
+
+    def __init__(self, kv_len, page_table, tokens, q_len=1, q_start=None, max_kv_len=None, prefix_table=None,
+                 prefix_len=0):
+        chk = _Checked()
+        _dev_tensor(kv_len, "kv_len", _I32, chk=chk)
+        _need(kv_len.dim() == 1, "kv_len must be [num_seqs]")
+        _dev_tensor(page_table, "page_table", _I32, chk=chk)
+        _need(page_table.dim() == 2 and page_table.shape[0] == kv_len.shape[0],
+              "page_table must be [num_seqs][table_width]")
+        if q_start is not None:
+            _dev_tensor(q_start, "q_start", _I32, (kv_len.shape[0] + 1,), chk)
+        else:
+            _need(kv_len.shape[0] * q_len == tokens, "without q_start, tokens must be num_seqs * q_len")
+        if prefix_table is not None:
+            _dev_tensor(prefix_table, "prefix_table", _I32, chk=chk)
+            _need(prefix_table.dim() == 1, "prefix_table must be [pages]")
+        _need((prefix_table is None) == (prefix_len == 0), "prefix_table and prefix_len go together")
+        chk.on_gpu()
+        self.kv_len, self.page_table, self.q_start, self.prefix_table = kv_len, page_table, q_start, prefix_table
+        self.tokens, self.q_len, self.prefix_len = int(tokens), int(q_len), int(prefix_len)
+        self.max_kv_len = (1 << 31) - 1 if max_kv_len is None else int(max_kv_len)
+        self._bytes = _PACK_BATCH(0 if q_start is None else q_start.data_ptr(), kv_len.data_ptr(),
+                                  page_table.data_ptr(), 0 if prefix_table is None else prefix_table.data_ptr(),
+                                  kv_len.shape[0], self.tokens, self.q_len, page_table.shape[1], self.prefix_len,
+                                  self.max_kv_len)
+
+    def packed(self):
+        """The bytes of a cl_kv_batch."""
+        return self._bytes
+
+
+def _check_prefix(cache, batch):
+    if batch.prefix_len:
+        _need(batch.prefix_table.shape[0] * cache.page_size >= batch.prefix_len, "prefix_table is too short for "
+              "prefix_len")
+
+
+def rope_frequencies(rot_dim, base=10000.0, kind="plain", factor=1.0, trained_len=1.0, low=1.0, high=4.0):
+    """``cl_rope_frequencies`` (host code): (inv_freq float32 CPU tensor
+    [rot_dim / 2], magnitude)."""
+    _need(kind in ROPE_KINDS, "kind must be one of %s" % ", ".join(ROPE_KINDS))
+    out = torch.empty(max(int(rot_dim), 0) // 2, dtype=torch.float32)
+    mag = ctypes.c_float()
+    _check(lib().cl_rope_frequencies(int(rot_dim), float(base), ROPE_KINDS[kind], float(factor), float(trained_len),
+                                     float(low), float(high), _ptr(out), ctypes.byref(mag)))
+    return out, mag.value
+
+
+class Rope:
+    """Rotary positions (cl_rope): inv_freq float32 [rot_dim / 2] on the GPU,
+    pairs in halves or interleaved.  Checked once, when it is made."""
+
+    def __init__(self, inv_freq, interleaved=False, magnitude=1.0):
+        _dev_tensor(inv_freq, "inv_freq", (torch.float32,))
+        _need(inv_freq.dim() == 1, "inv_freq must be [rot_dim / 2]")
+        self.inv_freq, self.interleaved, self.magnitude = inv_freq, bool(interleaved), float(magnitude)
+        self.rot_dim = 2 * inv_freq.shape[0]
+        self._bytes = _PACK_ROPE(inv_freq.data_ptr(), self.rot_dim, int(self.interleaved), self.magnitude)
+
+    def packed(self):
+        """The bytes of a cl_rope."""
+        return self._bytes
+
+
+def _token_rows(t, name, dtype, tokens, heads, dim):
+    """[tokens][heads][dim] with a token's heads contiguous; the token stride."""
+    if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.dim() == 3 and t.is_cuda):
+        _need(isinstance(t, torch.Tensor), "%s must be a torch.Tensor" % name)
+        _need(t.dtype == dtype, "%s must have dtype %s (got %s)" % (name, dtype, t.dtype))
+        _need(t.dim() == 3, "%s must be [tokens][heads][head_dim]" % name)
+        _need(t.is_cuda, "%s must be on the GPU (got %s)" % (name, t.device))
+    n, h, d = t.shape
+    _need(n == tokens and d == dim and (heads is None or h == heads), "%s must have shape %s (got %s)"
+          % (name, (tokens, heads or "heads", dim), (n, h, d)))
+    a, b, c = t.stride()
+    _need((c == 1 or d == 1) and (b == d or h == 1) and (a >= h * d or n == 1),
+          "a token's heads of %s must be contiguous" % name)
+    return a if n > 1 else h * d
+
+
+def kv_append(cache, batch, k, v, q=None, rope=None, q_norm=None, k_norm=None, eps=1e-6, positions=None, q_out=None,
+              stream=None):
+    """``cl_kv_append``: k, v [tokens][kv_heads][head_dim] into the cache, q
+    [tokens][q_heads][head_dim] rotated into q_out (returned; None without q).
+    A token's heads are contiguous, tokens at any stride."""
+    dt, D, n = cache.dtype, cache.head_dim, batch.tokens
+    ks = _token_rows(k, "k", dt, n, cache.kv_heads, D)
+    vs = _token_rows(v, "v", dt, n, cache.kv_heads, D)
+    qs = heads = 0
+    if q is not None:
+        qs = _token_rows(q, "q", dt, n, None, D)
+        heads = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty((n, heads, D), dtype=dt, device=q.device)
+        else:
+            _dev_tensor(q_out, "q_out", (dt,), q.shape)
+    if q_norm is not None:
+        _dev_tensor(q_norm, "q_norm", (dt,), (D,))
+    if k_norm is not None:
+        _dev_tensor(k_norm, "k_norm", (dt,), (D,))
+    if positions is not None:
+        _dev_tensor(positions, "positions", _I32, (n,))
+    _check(_call("cl_kv_append")(cache._bytes, batch._bytes, None if rope is None else rope._bytes, _opt_ptr(q), qs,
+                                 heads, k.data_ptr(), ks, v.data_ptr(), vs, _opt_ptr(q_norm), _opt_ptr(k_norm), eps,
+                                 _opt_ptr(positions), _opt_ptr(q_out) if q is not None else None,
+                                 _raw_stream(stream)))
+    return q_out if q is not None else None
+
+
+def attention_workspace(cache, batch, q_heads):
+    return _call("cl_attention_workspace")(cache._bytes, batch._bytes, q_heads)
+
+
+def attention(cache, batch, q, scale=None, causal=True, window=0, out=None, out_dtype=None, lse=None, ws=None,
+              stream=None):
+    """``cl_attention``: q [tokens][q_heads][head_dim] of the cache's dtype ->
+    out of out_dtype (default: q's).  scale: head_dim ** -0.5 by default;
+    ``lse``: None, or a float32 [tokens][q_heads] tensor to be filled."""
+    D, n = cache.head_dim, batch.tokens
+    _check_prefix(cache, batch)
+    qs = _token_rows(q, "q", cache.dtype, n, None, D)
+    heads = q.shape[1]
+    if out is None:
+        out = torch.empty((n, heads, D), dtype=out_dtype or q.dtype, device=q.device)
+    else:
+        _dev_tensor(out, "out", _OUT, q.shape)
+    if lse is not None:
+        _dev_tensor(lse, "lse", (torch.float32,), (n, heads))
+    if ws is None:
+        need = _call("cl_attention_workspace")(cache._bytes, batch._bytes, heads)
+        ws = workspace(need, q.device) if need else None
+    else:
+        _dev_tensor(ws, "ws", (torch.uint8,))
+    _check(_call("cl_attention")(cache._bytes, batch._bytes, q.data_ptr(), qs, heads,
+                                 D ** -0.5 if scale is None else scale, int(causal), window, out.data_ptr(),
+                                 _DTYPE_CODE[out.dtype], _opt_ptr(lse), _opt_ptr(ws),
+                                 0 if ws is None else ws.numel(), _raw_stream(stream)))
+    return out
+
+
+class Router:
+    """How tokens choose experts (cl_router); bias float32 [num_experts] on
+    the GPU or None.  Checked once, when it is made."""
+
+    def __init__(self, num_experts, k, score="softmax", bias=None, groups=1, top_groups=1, group_best=1,
+                 renormalize=True, scale=1.0):
+        _need(score in _SCORES, "score must be one of %s" % ", ".join(_SCORES))
+        if bias is not None:
+            _dev_tensor(bias, "bias", (torch.float32,), (num_experts,))
+        self.num_experts, self.k, self.score, self.bias = int(num_experts), int(k), score, bias
+        self._bytes = _PACK_ROUTER(0 if bias is None else bias.data_ptr(), self.num_experts, self.k, _SCORES[score],
+                                   int(groups), int(top_groups), int(group_best), int(bool(renormalize)),
+                                   float(scale))
+
+    def packed(self):
+        """The bytes of a cl_router."""
+        return self._bytes
+
+
+def moe_route(router, logits, expert_ranks=(), levels=(), ids=None, weights=None, slot_ranks=None, stream=None):
+    """``cl_moe_route``: logits [T][num_experts] -> (ids int32 [T][k], weights
+    float32 [T][k]), and with ``expert_ranks`` (int32 [num_experts] tensors)
+    and ``levels`` a third item, the list of slot_ranks int32 [T][k]."""
+    _dev_tensor(logits, "logits", _OUT)
+    _need(logits.dim() == 2 and logits.shape[1] == router.num_experts, "logits must be [T][num_experts]")
+    T, k = logits.shape[0], router.k
+    if ids is None:
+        ids = torch.empty((T, k), dtype=torch.int32, device=logits.device)
+    else:
+        _dev_tensor(ids, "ids", _I32, (T, k))
+    if weights is None:
+        weights = torch.empty((T, k), dtype=torch.float32, device=logits.device)
+    else:
+        _dev_tensor(weights, "weights", (torch.float32,), (T, k))
+    n = len(expert_ranks)
+    er = lv = sr = None
+    if n:
+        if slot_ranks is None:
+            slot_ranks = [torch.empty((T, k), dtype=torch.int32, device=logits.device) for _ in range(n)]
+        _need(len(slot_ranks) == n, "one slot-rank table per expert-rank table")
+        for i in range(n):
+            _dev_tensor(expert_ranks[i], "expert_ranks[%d]" % i, _I32, (router.num_experts,))
+            _dev_tensor(slot_ranks[i], "slot_ranks[%d]" % i, _I32, (T, k))
+        er = struct.pack("%dP" % n, *[t.data_ptr() for t in expert_ranks])
+        sr = struct.pack("%dP" % n, *[t.data_ptr() for t in slot_ranks])
+        lv = struct.pack("%di" % len(levels), *levels)
+    _check(_call("cl_moe_route")(router._bytes, logits.data_ptr(), _DTYPE_CODE[logits.dtype], T, ids.data_ptr(),
+                                 weights.data_ptr(), n, er, lv, len(levels), sr, _raw_stream(stream)))
+    return (ids, weights, slot_ranks) if n else (ids, weights)
+
+
+def residual_norm(y, weight, residual=None, slot_weights=None, post_weight=None, gate=None, bias=None, kind="rms",
+                  eps=1e-6, alpha=1.0, beta=1.0, h=None, out=None, out_dtype=None, stream=None):
+    """``cl_residual_norm``: y [T][d] (or [T][slots][d] with slot_weights
+    float32 [T][slots]) and residual [T][d] -> (h [T][d] of the residual's
+    dtype, out [T][d] of out_dtype).  weight, bias, post_weight [d] and gate [d]
+    or [T][d] share a dtype; without a residual h has y's dtype.  h may be the
+    residual itself; h=False computes out alone."""
+    _dev_tensor(y, "y", _OUT)
+    _need(kind in _NORMS, "kind must be one of %s" % ", ".join(_NORMS))
+    slots = 0
+    if slot_weights is not None:
+        _need(y.dim() == 3, "y must be [T][slots][d] with slot_weights")
+        slots = y.shape[1]
+        _dev_tensor(slot_weights, "slot_weights", (torch.float32,), y.shape[:2])
+    else:
+        _need(y.dim() == 2, "y must be [T][d]")
+    T, d = y.shape[0], y.shape[-1]
+    _dev_tensor(weight, "weight", _OUT, (d,))
+    wt = (weight.dtype,)
+    if bias is not None:
+        _dev_tensor(bias, "bias", wt, (d,))
+    if post_weight is not None:
+        _dev_tensor(post_weight, "post_weight", wt, (d,))
+    per_token = 0
+    if gate is not None:
+        per_token = int(gate.dim() == 2)
+        _dev_tensor(gate, "gate", wt, (T, d) if per_token else (d,))
+    ht = y.dtype
+    if residual is not None:
+        _dev_tensor(residual, "residual", _OUT, (T, d))
+        ht = residual.dtype
+    if h is None:
+        h = torch.empty((T, d), dtype=ht, device=y.device)
+    elif h is not False:
+        _dev_tensor(h, "h", (ht,), (T, d))
+    if out is None:
+        out = torch.empty((T, d), dtype=out_dtype or ht, device=y.device)
+    else:
+        _dev_tensor(out, "out", _OUT, (T, d))
+    nb = _PACK_NORM(weight.data_ptr(), 0 if bias is None else bias.data_ptr(),
+                    0 if post_weight is None else post_weight.data_ptr(), 0 if gate is None else gate.data_ptr(),
+                    _DTYPE_CODE[weight.dtype], _NORMS[kind], per_token, eps, alpha, beta)
+    _check(_call("cl_residual_norm")(nb, y.data_ptr(), _DTYPE_CODE[y.dtype], slots, _opt_ptr(slot_weights),
+                                     _opt_ptr(residual), None if h is False else h.data_ptr(), _DTYPE_CODE[ht],
+                                     out.data_ptr(), _DTYPE_CODE[out.dtype], T, d, _raw_stream(stream)))
+    return (out if h is False else (h, out))

@@ -499,3 +499,265 @@ cl_status cl_linear_decode_glu(const cl_qweight* w, const cl_lowrank* c, const v
 }
 
 }  // extern "C"
+
+// ------------------------------------- between the linears of a decoder layer
+
+namespace {
+
+bool act_type(int dt) { return dt == CL_FP16 || dt == CL_BF16; }
+bool out_type(int dt) { return act_type(dt) || dt == CL_FP32; }
+size_t type_size(int dt) { return dt == CL_FP32 ? 4 : 2; }
+
+cl_status check_kv(const cl_kv_cache* c, const cl_kv_batch* b, cl::KvCache* oc, cl::KvBatch* ob, const char* who) {
+    if (!c || !b) return fail(CL_EINVAL, "%s: null cache or batch descriptor", who);
+    if (!c->k || !c->v || !aligned(c->k, 16) || !aligned(c->v, 16))
+        return fail(CL_EINVAL, "%s: cache k and v must be non-null and 16-byte aligned", who);
+    if (!act_type(c->dtype)) return fail(CL_EINVAL, "%s: the cache's dtype must be CL_FP16 or CL_BF16", who);
+    if (c->num_pages < 1 || c->kv_heads < 1) return fail(CL_EINVAL, "%s: num_pages and kv_heads must be positive", who);
+    if (c->page_size < 1 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)))
+        return fail(CL_EINVAL, "%s: page_size must be a power of two in 1..1024 (got %d)", who, c->page_size);
+    if (!cl::attention_dim_ok(c->head_dim))
+        return fail(CL_EUNSUPPORTED, "%s: head_dim must be 64, 128 or 256 (got %d)", who, c->head_dim);
+    if (b->num_seqs < 1 || b->tokens < 1 || b->q_len < 1)
+        return fail(CL_EINVAL, "%s: num_seqs, tokens and q_len must be positive", who);
+    if (!b->kv_len || !aligned(b->kv_len, 4)) return fail(CL_EINVAL, "%s: null or misaligned kv_len", who);
+    if (b->table_width < 0 || b->max_kv_len < 0 || b->prefix_len < 0)
+        return fail(CL_EINVAL, "%s: table_width, prefix_len and max_kv_len must not be negative", who);
+    if (b->table_width > 0 && (!b->page_table || !aligned(b->page_table, 4)))
+        return fail(CL_EINVAL, "%s: null or misaligned page_table", who);
+    if (b->prefix_len > 0 && (!b->prefix_table || !aligned(b->prefix_table, 4)))
+        return fail(CL_EINVAL, "%s: null or misaligned prefix_table", who);
+    if (b->q_start) {
+        if (!aligned(b->q_start, 4)) return fail(CL_EINVAL, "%s: misaligned q_start", who);
+    } else if (static_cast<long long>(b->num_seqs) * b->q_len != b->tokens) {
+        return fail(CL_EINVAL, "%s: without q_start, tokens must be num_seqs * q_len (%d, %d, %d)", who, b->tokens,
+                    b->num_seqs, b->q_len);
+    }
+    int shift = 0;
+    while ((1 << shift) < c->page_size) ++shift;
+    long long limit = b->prefix_len + (static_cast<long long>(b->table_width) << shift);
+    if (limit > b->max_kv_len) limit = b->max_kv_len;
+    *oc = {static_cast<uint16_t*>(c->k), static_cast<uint16_t*>(c->v), c->num_pages, shift, c->kv_heads, c->head_dim,
+           c->dtype};
+    *ob = {b->q_start, b->kv_len, b->page_table, b->prefix_table, b->num_seqs, b->tokens, b->q_len, b->table_width,
+           b->prefix_len, static_cast<int>(limit)};
+    return CL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+cl_status cl_rope_frequencies(int32_t rot_dim, double base, int32_t kind, double factor, double trained_len,
+                              double low, double high, float* inv_freq, float* magnitude) {
+    const char* who = "cl_rope_frequencies";
+    if (rot_dim < 4 || rot_dim > 1024 || rot_dim % 2)
+        return fail(CL_EINVAL, "%s: rot_dim must be even and in 4..1024 (got %d)", who, rot_dim);
+    if (!(base > 1.0) || !isfinite(base)) return fail(CL_EINVAL, "%s: base must be finite and above 1", who);
+    if (kind < CL_ROPE_PLAIN || kind > CL_ROPE_RAMP) return fail(CL_EINVAL, "%s: unknown kind %d", who, kind);
+    if (!inv_freq || !magnitude) return fail(CL_EINVAL, "%s: null output", who);
+    if (kind != CL_ROPE_PLAIN && (!(factor >= 1.0) || !isfinite(factor)))
+        return fail(CL_EINVAL, "%s: factor must be finite and at least 1", who);
+    if (kind >= CL_ROPE_BANDS && (!(trained_len >= 1.0) || !isfinite(trained_len) || !(low > 0.0) || !(high > low) || !isfinite(high)))
+        return fail(CL_EINVAL, "%s: need trained_len >= 1 and 0 < low < high", who);
+    cl::rope_frequencies(rot_dim, base, kind, factor, trained_len, low, high, inv_freq, magnitude);
+    return CL_OK;
+}
+
+cl_status cl_kv_append(const cl_kv_cache* cache, const cl_kv_batch* batch, const cl_rope* rope, const void* q,
+                       int64_t q_stride, int32_t q_heads, const void* k, int64_t k_stride, const void* v,
+                       int64_t v_stride, const void* q_norm, const void* k_norm, float eps,
+                       const int32_t* positions, void* q_out, void* stream) {
+    const char* who = "cl_kv_append";
+    cl::AppendArgs a{};
+    cl_status st = check_kv(cache, batch, &a.cache, &a.batch, who);
+    if (st) return st;
+    if (rope) {
+        if (!rope->inv_freq || !aligned(rope->inv_freq, 4)) return fail(CL_EINVAL, "%s: null or misaligned inv_freq", who);
+        if (rope->rot_dim < 8 || rope->rot_dim > cache->head_dim || rope->rot_dim % 8)
+            return fail(CL_EINVAL, "%s: rot_dim must be a multiple of 8 in 8..head_dim (got %d)", who, rope->rot_dim);
+        if (!isfinite(rope->magnitude)) return fail(CL_EINVAL, "%s: magnitude must be finite", who);
+        a.rope = {rope->inv_freq, rope->rot_dim, rope->interleaved ? 1 : 0, rope->magnitude};
+    }
+    if (q_heads < 0 || (q_heads > 0) != (q != nullptr)) return fail(CL_EINVAL, "%s: q and q_heads go together", who);
+    if (!k || !v) return fail(CL_EINVAL, "%s: null k or v", who);
+    if (q && !q_out) return fail(CL_EINVAL, "%s: null q_out", who);
+    if (!aligned(q, 2) || !aligned(k, 2) || !aligned(v, 2) || !aligned(q_out, 2) || !aligned(q_norm, 2) || !aligned(k_norm, 2))
+        return fail(CL_EINVAL, "%s: misaligned q, k, v, q_out or norm", who);
+    if (positions && !aligned(positions, 4)) return fail(CL_EINVAL, "%s: misaligned positions", who);
+    const int64_t D = cache->head_dim;
+    if ((q && q_stride < q_heads * D) || k_stride < cache->kv_heads * D || v_stride < cache->kv_heads * D)
+        return fail(CL_EINVAL, "%s: a token stride is shorter than the token's heads", who);
+    if ((q_norm || k_norm) && !(eps >= 0.f && isfinite(eps))) return fail(CL_EINVAL, "%s: eps must be finite and >= 0", who);
+    a.q = static_cast<const uint16_t*>(q);
+    a.k = static_cast<const uint16_t*>(k);
+    a.v = static_cast<const uint16_t*>(v);
+    a.q_norm = static_cast<const uint16_t*>(q_norm);
+    a.k_norm = static_cast<const uint16_t*>(k_norm);
+    a.positions = positions;
+    a.q_out = static_cast<uint16_t*>(q_out);
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.q_heads = q_heads;
+    a.eps = eps;
+    return hip_status(cl::launch_kv_append(a, static_cast<hipStream_t>(stream)), who);
+}
+
+size_t cl_attention_workspace(const cl_kv_cache* cache, const cl_kv_batch* batch, int32_t q_heads) {
+    char saved[sizeof(g_err)];
+    memcpy(saved, g_err, sizeof(g_err));
+    cl::KvCache c;
+    cl::KvBatch b;
+    size_t bytes = 0;
+    if (check_kv(cache, batch, &c, &b, "") == CL_OK && q_heads >= c.heads && q_heads % c.heads == 0)
+        bytes = cl::attention_workspace_bytes(c, b, q_heads);
+    memcpy(g_err, saved, sizeof(g_err));
+    return bytes;
+}
+
+cl_status cl_attention(const cl_kv_cache* cache, const cl_kv_batch* batch, const void* q, int64_t q_stride,
+                       int32_t q_heads, float scale, int32_t causal, int32_t window, void* out, int32_t out_dtype,
+                       float* lse, void* ws, size_t ws_bytes, void* stream) {
+    const char* who = "cl_attention";
+    cl::AttnArgs a{};
+    cl_status st = check_kv(cache, batch, &a.cache, &a.batch, who);
+    if (st) return st;
+    if (q_heads < 1 || q_heads % cache->kv_heads)
+        return fail(CL_EINVAL, "%s: q_heads (%d) must be a positive multiple of kv_heads (%d)", who, q_heads, cache->kv_heads);
+    if (!q || !out) return fail(CL_EINVAL, "%s: null q or out", who);
+    if (!aligned(q, 16) || q_stride % 8 || !aligned(out, 16))
+        return fail(CL_EINVAL, "%s: q rows and out must be 16-byte aligned", who);
+    if (q_stride < static_cast<int64_t>(q_heads) * cache->head_dim)
+        return fail(CL_EINVAL, "%s: q_stride is shorter than a token's heads", who);
+    if (!isfinite(scale)) return fail(CL_EINVAL, "%s: scale must be finite", who);
+    if (window < 0) return fail(CL_EINVAL, "%s: window must not be negative", who);
+    if (!out_type(out_dtype)) return fail(CL_EINVAL, "%s: out_dtype must be CL_FP16, CL_BF16 or CL_FP32", who);
+    if (lse && !aligned(lse, 4)) return fail(CL_EINVAL, "%s: misaligned lse", who);
+    const size_t need = cl::attention_workspace_bytes(a.cache, a.batch, q_heads);
+    if (need > 0) {
+        if (!ws || ws_bytes < need)
+            return fail(CL_EWORKSPACE, "%s: workspace of %zu bytes needed (got %zu)", who, need, ws ? ws_bytes : 0);
+        if (!aligned(ws, 256)) return fail(CL_EINVAL, "%s: workspace must be 256-byte aligned", who);
+    }
+    a.q = static_cast<const uint16_t*>(q);
+    a.q_stride = q_stride;
+    a.q_heads = q_heads;
+    a.causal = causal ? 1 : 0;
+    a.window = window;
+    a.out_dtype = out_dtype;
+    a.scale = scale;
+    a.out = out;
+    a.lse = lse;
+    return hip_status(cl::launch_attention(a, ws, static_cast<hipStream_t>(stream)), who);
+}
+
+cl_status cl_moe_route(const cl_router* router, const void* logits, int32_t logits_dtype, int32_t T, int32_t* ids,
+                       float* weights, int32_t tables, const int32_t* const* expert_ranks, const int32_t* levels,
+                       int32_t nlevels, int32_t* const* slot_ranks, void* stream) {
+    const char* who = "cl_moe_route";
+    if (!router) return fail(CL_EINVAL, "%s: null router", who);
+    const cl_router& r = *router;
+    if (r.num_experts < 1 || r.num_experts > 1024)
+        return fail(CL_EINVAL, "%s: num_experts must be in 1..1024 (got %d)", who, r.num_experts);
+    if (r.k < 1 || r.k > 64) return fail(CL_EINVAL, "%s: k must be in 1..64 (got %d)", who, r.k);
+    if (r.score != CL_SOFTMAX && r.score != CL_SIGMOID)
+        return fail(CL_EINVAL, "%s: score must be CL_SOFTMAX or CL_SIGMOID", who);
+    if (r.groups < 1 || r.groups > 64 || r.num_experts % r.groups)
+        return fail(CL_EINVAL, "%s: groups must be in 1..64 and divide num_experts (got %d)", who, r.groups);
+    if (r.top_groups < 1 || r.top_groups > r.groups)
+        return fail(CL_EINVAL, "%s: top_groups must be in 1..groups (got %d)", who, r.top_groups);
+    if (r.group_best != 1 && r.group_best != 2) return fail(CL_EINVAL, "%s: group_best must be 1 or 2", who);
+    if (r.k > r.num_experts / r.groups * r.top_groups)
+        return fail(CL_EINVAL, "%s: %d open experts are fewer than k = %d", who, r.num_experts / r.groups * r.top_groups, r.k);
+    if (!isfinite(r.scale)) return fail(CL_EINVAL, "%s: scale must be finite", who);
+    if (!out_type(logits_dtype)) return fail(CL_EINVAL, "%s: logits_dtype must be CL_FP16, CL_BF16 or CL_FP32", who);
+    if (T < 1) return fail(CL_EINVAL, "%s: T must be >= 1 (got %d)", who, T);
+    if (!logits || !ids || !weights) return fail(CL_EINVAL, "%s: null logits, ids or weights", who);
+    if (!aligned(logits, type_size(logits_dtype)) || !aligned(ids, 4) || !aligned(weights, 4) || !aligned(r.bias, 4))
+        return fail(CL_EINVAL, "%s: misaligned logits, ids, weights or bias", who);
+    if (tables < 0 || tables > cl::kMaxRouteTables)
+        return fail(CL_EINVAL, "%s: tables must be in 0..%d (got %d)", who, cl::kMaxRouteTables, tables);
+    cl::RouteArgs a{};
+    if (tables > 0) {
+        if (!expert_ranks || !slot_ranks || !levels) return fail(CL_EINVAL, "%s: null rank array", who);
+        if (nlevels < 1 || nlevels > cl::kMaxRankLevels)
+            return fail(CL_EINVAL, "%s: nlevels must be in 1..%d (got %d)", who, cl::kMaxRankLevels, nlevels);
+        for (int l = 0; l < nlevels; ++l) {
+            if (levels[l] < 0 || (l > 0 && levels[l] <= levels[l - 1]))
+                return fail(CL_EINVAL, "%s: levels must be >= 0 and strictly increasing", who);
+            a.levels[l] = levels[l];
+        }
+        for (int n = 0; n < tables; ++n) {
+            if (!expert_ranks[n] || !slot_ranks[n] || !aligned(expert_ranks[n], 4) || !aligned(slot_ranks[n], 4))
+                return fail(CL_EINVAL, "%s: null or misaligned rank table %d", who, n);
+            a.expert_ranks[n] = expert_ranks[n];
+            a.slot_ranks[n] = slot_ranks[n];
+        }
+    }
+    a.logits = logits;
+    a.bias = r.bias;
+    a.ids = ids;
+    a.weights = weights;
+    a.tables = tables;
+    a.nlevels = nlevels;
+    a.T = T;
+    a.E = r.num_experts;
+    a.k = r.k;
+    a.dtype = logits_dtype;
+    a.sigmoid = r.score == CL_SIGMOID;
+    a.groups = r.groups;
+    a.top_groups = r.top_groups;
+    a.group_best = r.group_best;
+    a.renormalize = r.renormalize ? 1 : 0;
+    a.scale = r.scale;
+    return hip_status(cl::launch_moe_route(a, static_cast<hipStream_t>(stream)), who);
+}
+
+cl_status cl_residual_norm(const cl_norm* norm, const void* y, int32_t y_dtype, int32_t slots,
+                           const float* slot_weights, const void* residual, void* h, int32_t h_dtype, void* out,
+                           int32_t out_dtype, int32_t T, int32_t d, void* stream) {
+    const char* who = "cl_residual_norm";
+    if (!norm) return fail(CL_EINVAL, "%s: null norm descriptor", who);
+    if (norm->kind != CL_NORM_RMS && norm->kind != CL_NORM_LAYER)
+        return fail(CL_EINVAL, "%s: kind must be CL_NORM_RMS or CL_NORM_LAYER", who);
+    if (!out_type(norm->w_dtype) || !out_type(y_dtype) || !out_type(h_dtype) || !out_type(out_dtype))
+        return fail(CL_EINVAL, "%s: dtypes must be CL_FP16, CL_BF16 or CL_FP32", who);
+    if (!(norm->eps >= 0.f) || !isfinite(norm->eps) || !isfinite(norm->alpha) || !isfinite(norm->beta))
+        return fail(CL_EINVAL, "%s: eps must be finite and >= 0, alpha and beta finite", who);
+    if (T < 1 || d < 1) return fail(CL_EINVAL, "%s: T and d must be positive (got %d, %d)", who, T, d);
+    if (d > 32768) return fail(CL_EUNSUPPORTED, "%s: d must be at most 32768 (got %d)", who, d);
+    if (slots < 0 || slots > 64) return fail(CL_EINVAL, "%s: slots must be in 0..64 (got %d)", who, slots);
+    if ((slots > 0) != (slot_weights != nullptr)) return fail(CL_EINVAL, "%s: slots and slot_weights go together", who);
+    if (!norm->weight || !y || !out) return fail(CL_EINVAL, "%s: null weight, y or out", who);
+    const size_t ws = type_size(norm->w_dtype), hs = type_size(h_dtype);
+    if (!aligned(norm->weight, ws) || !aligned(norm->bias, ws) || !aligned(norm->post_weight, ws) ||
+        !aligned(norm->gate, ws) || !aligned(y, type_size(y_dtype)) || !aligned(residual, hs) || !aligned(h, hs) ||
+        !aligned(out, type_size(out_dtype)) || !aligned(slot_weights, 4))
+        return fail(CL_EINVAL, "%s: an array is not aligned to its elements", who);
+    cl::NormArgs a{};
+    a.y = y;
+    a.residual = residual;
+    a.weight = norm->weight;
+    a.bias = norm->bias;
+    a.post_weight = norm->post_weight;
+    a.gate = norm->gate;
+    a.slot_weights = slot_weights;
+    a.h = h;
+    a.out = out;
+    a.T = T;
+    a.d = d;
+    a.slots = slots;
+    a.layer = norm->kind == CL_NORM_LAYER;
+    a.gate_per_token = norm->gate_per_token ? 1 : 0;
+    a.y_dtype = y_dtype;
+    a.h_dtype = h_dtype;
+    a.out_dtype = out_dtype;
+    a.w_dtype = norm->w_dtype;
+    a.eps = norm->eps;
+    a.alpha = norm->alpha;
+    a.beta = norm->beta;
+    return hip_status(cl::launch_residual_norm(a, static_cast<hipStream_t>(stream)), who);
+}
+
+}  // extern "C"

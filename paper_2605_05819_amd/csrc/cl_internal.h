@@ -64,6 +64,90 @@ hipError_t launch_moe_decode(int n, const QW* w, const uint16_t* const* A, const
 // stream, returns the record in *word (0: none) and clears it.
 hipError_t moe_take_routing_error(hipStream_t st, unsigned long long* word);
 
+// Paged keys and values, validated: [num_pages][heads][page_size][dim] each,
+// page_size = 1 << page_shift.
+struct KvCache {
+    uint16_t* k;
+    uint16_t* v;
+    int num_pages, page_shift, heads, dim, dtype;
+};
+
+// Sequences of a call, validated.  key_limit is the most keys a sequence may
+// have: min(max_kv_len, prefix_len + table_width * page_size).
+struct KvBatch {
+    const int32_t* q_start;        // [num_seqs + 1], or null: q_len tokens each
+    const int32_t* kv_len;         // [num_seqs]
+    const int32_t* page_table;     // [num_seqs][table_width]
+    const int32_t* prefix_table;
+    int num_seqs, tokens, q_len, table_width, prefix_len, key_limit;
+};
+
+struct Rope {                  // inv_freq null: no rotation
+    const float* inv_freq;
+    int rot_dim, interleaved;
+    float magnitude;
+};
+
+// Rotation of q into q_out and of k into the cache beside v (append.hip).
+// Strides are in elements between tokens; q may be null.
+struct AppendArgs {
+    KvCache cache;
+    KvBatch batch;
+    Rope rope;
+    const uint16_t *q, *k, *v, *q_norm, *k_norm;
+    const int32_t* positions;
+    uint16_t* q_out;
+    long long q_stride, k_stride, v_stride;
+    int q_heads;
+    float eps;
+};
+hipError_t launch_kv_append(const AppendArgs& a, hipStream_t st);
+void rope_frequencies(int rot_dim, double base, int kind, double factor, double trained_len, double low, double high,
+                      float* inv_freq, float* magnitude);      // host code
+
+// Attention over the paged cache (attention.hip).
+struct AttnArgs {
+    KvCache cache;
+    KvBatch batch;
+    const uint16_t* q;
+    long long q_stride;
+    int q_heads, causal, window, out_dtype;
+    float scale;
+    void* out;
+    float* lse;                    // may be null
+};
+bool attention_dim_ok(int dim);
+size_t attention_workspace_bytes(const KvCache& c, const KvBatch& b, int q_heads);
+hipError_t launch_attention(const AttnArgs& a, void* ws, hipStream_t st);
+
+// Residual add, gate, combination of slots and norms of one row (norm.hip).
+struct NormArgs {
+    const void *y, *residual, *weight, *bias, *post_weight, *gate;
+    const float* slot_weights;     // [T][slots], or null: y is [T][d]
+    void *h, *out;                 // h may be null
+    int T, d, slots, layer, gate_per_token;
+    int y_dtype, h_dtype, out_dtype, w_dtype;
+    float eps, alpha, beta;
+};
+hipError_t launch_residual_norm(const NormArgs& a, hipStream_t st);
+
+// Routing of tokens to experts (route.hip).
+constexpr int kMaxRouteTables = 4;
+constexpr int kMaxRankLevels = 16;
+struct RouteArgs {
+    const void* logits;
+    const float* bias;
+    int32_t* ids;
+    float* weights;
+    const int32_t* expert_ranks[kMaxRouteTables];
+    int32_t* slot_ranks[kMaxRouteTables];
+    int levels[kMaxRankLevels];
+    int tables, nlevels;
+    int T, E, k, dtype, sigmoid, groups, top_groups, group_best, renormalize;
+    float scale;
+};
+hipError_t launch_moe_route(const RouteArgs& a, hipStream_t st);
+
 // Rank allocation (host code, ranks.hip): salient-set size and salience
 // ratio of one descending spectrum; ranks of one compensation window (cont,
 // if not null, receives the continuous ranks before alignment); layer scores

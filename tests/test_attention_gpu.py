@@ -1,0 +1,260 @@
+"""cl_attention against the fp64 oracle, through the paged cache.
+
+Every cache row that belongs to no key of the batch holds NaN in k and v, so a
+kernel that reads past a length, into another page or past a table shows it.
+
+Tolerances, from the arithmetic: products of 16-bit values are exact in fp32 and
+summed there, so a score is off by at most D 2^-24 scale sum|q k|, which moves a
+probability by that much relative to itself; probabilities are rounded once to
+the cache's type (u_p; fp16 ones below 2^-14 to multiples of 2^-24 instead), and
+sums of n terms in fp32 lose at most n 2^-24.  With A = sum p |v| / sum p an
+element is off by at most A times these, plus the output's own rounding."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer
+from paper_2605_05819_amd import cl
+from tests.helpers import UNIT_ROUNDOFF, out_to_numpy
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+
+
+class Case:
+    """A batch with its own pages in a pool of NaN, and the oracle's view of it."""
+
+    def __init__(self, q_lens, kv_lens, Hq, Hkv, D, page, dtype, prefix=0, seed=0, uniform=False, spare=3, kstd=1.0):
+        g = np.random.default_rng(seed)
+        rnd = lambda *s: torch.from_numpy(g.standard_normal(s).astype(np.float32)).to(dtype)  # noqa: E731
+        self.q_lens, self.kv_lens, self.Hq, self.Hkv, self.D, self.dtype = q_lens, kv_lens, Hq, Hkv, D, dtype
+        B, self.prefix = len(q_lens), prefix
+        self.N = sum(q_lens)
+        own = [max(0, n - prefix) for n in kv_lens]
+        need = [-(-n // page) for n in own]
+        shared = -(-prefix // page)
+        total = sum(need) + shared + spare
+        pool = g.permutation(total).astype(np.int32)
+        width = max(need + [1]) + 1
+        table = np.full((B, width), -1, np.int32)        # entries past the keys are not read
+        k = torch.full((total, Hkv, page, D), float("nan"), dtype=dtype)
+        v = torch.full((total, Hkv, page, D), float("nan"), dtype=dtype)
+        kp, vp = rnd(Hkv, prefix, D) * kstd, rnd(Hkv, prefix, D)
+        for j in range(prefix):
+            k[pool[j // page], :, j % page], v[pool[j // page], :, j % page] = kp[:, j], vp[:, j]
+        at, self.ks, self.vs = shared, [], []
+        for b in range(B):
+            table[b, :need[b]] = pool[at:at + need[b]]
+            kb, vb = rnd(Hkv, own[b], D) * kstd, rnd(Hkv, own[b], D)
+            for j in range(own[b]):
+                k[pool[at + j // page], :, j % page], v[pool[at + j // page], :, j % page] = kb[:, j], vb[:, j]
+            at += need[b]
+            n = min(kv_lens[b], prefix)
+            self.ks.append(torch.cat([kp[:, :n], kb], 1).double().numpy())
+            self.vs.append(torch.cat([vp[:, :n], vb], 1).double().numpy())
+        self.q = rnd(max(self.N, 1), Hq, D)
+        i32 = lambda a: torch.tensor(np.asarray(a, np.int32)).cuda()  # noqa: E731
+        self.cache = cl.KvCache(k.cuda(), v.cuda())
+        start = np.concatenate([[0], np.cumsum(q_lens)])
+        self.table = i32(table)
+        self.batch = cl.KvBatch(i32(kv_lens), self.table, max(self.N, 1), q_len=max(q_lens + [1]),
+                                q_start=None if uniform else i32(start), max_kv_len=max(kv_lens + [1]),
+                                prefix_table=i32(pool[:shared]) if prefix else None, prefix_len=prefix)
+
+    def oracle(self, scale, causal, window):
+        parts, at = [], 0
+        for b, a in enumerate(self.q_lens):
+            parts.append(layer.attend(self.q[at:at + a].double().numpy(), self.ks[b], self.vs[b], scale, causal, window))
+            at += a
+        return [np.concatenate([p[i] for p in parts]) for i in range(4)]
+
+
+def check(c, causal=True, window=0, out_dtype=None, scale=None, q=None):
+    out_dtype = out_dtype or c.dtype
+    s = c.D ** -0.5 if scale is None else scale
+    lse = torch.full((max(c.N, 1), c.Hq), 7.0, device="cuda")
+    out = torch.full((max(c.N, 1), c.Hq, c.D), 7.0, dtype=out_dtype, device="cuda")
+    r = cl.attention(c.cache, c.batch, c.q.cuda() if q is None else q, scale=scale, causal=causal, window=window,
+                     out=out, lse=lse)
+    torch.cuda.synchronize()
+    assert r is out
+    if c.N == 0:
+        return
+    ref, rlse, A, most = c.oracle(s, causal, window)
+    n = max(c.kv_lens)
+    rel = 2.0 ** -24 * (2 * c.D * most + 2 * n + 16) + 2.0 ** -21
+    up = UNIT_ROUNDOFF[c.dtype]
+    allow = UNIT_ROUNDOFF[out_dtype] * np.abs(ref) * 1.01 + A * (up + rel[..., None]) * 1.01
+    if c.dtype == F16:
+        # n probabilities off by 2^-25 at most, over a sum of at least 1
+        allow = allow + 2.0 ** -25 * n * max([np.abs(v).max(initial=0) for v in c.vs])
+    got = out_to_numpy(out)
+    bad = np.abs(got - ref) > allow
+    assert np.isfinite(got).all() and not bad.any(), (np.abs(got - ref) / np.maximum(allow, 1e-30)).max()
+    gl = lse.double().cpu().numpy()
+    empty = np.isneginf(rlse)
+    assert np.array_equal(np.isneginf(gl), empty) and (got[empty] == 0).all()
+    err = np.abs(gl[~empty] - rlse[~empty])
+    assert (err <= (2 * rel + 2.0 ** -22 * np.abs(rlse))[~empty]).all(), err.max()
+
+
+SHAPES = [
+    # q_lens, kv_lens, Hq, Hkv, D, page, prefix
+    ([1], [1], 4, 4, 64, 16, 0),
+    ([1], [257], 8, 2, 128, 16, 0),
+    ([1, 1, 1], [1, 33, 700], 32, 8, 128, 64, 0),
+    ([1, 1], [64, 65], 7, 1, 128, 8, 0),
+    ([1, 1, 1, 1], [0, 5, 31, 32], 16, 1, 64, 1, 0),          # a sequence without keys, pages of one key
+    ([1] * 5, [130, 1, 90, 511, 512], 6, 2, 256, 32, 0),
+    ([4, 4], [300, 77], 8, 2, 128, 16, 0),                     # drafted tokens
+    ([8, 8], [1000, 9], 32, 2, 64, 64, 0),                     # 128 rows a key head
+    ([5], [3], 4, 2, 128, 16, 0),                              # more new tokens than keys: the first see none
+    ([65], [65], 4, 1, 128, 16, 0),                            # prompts
+    ([200, 0, 17, 1], [200, 40, 100, 333], 8, 2, 128, 16, 0),
+    ([129, 64], [300, 64], 3, 3, 64, 64, 0),
+    ([77, 130], [80, 200], 4, 4, 256, 128, 0),
+    ([0, 0], [5, 0], 4, 4, 64, 16, 0),
+    ([300], [1024], 14, 2, 64, 1024, 0),
+    ([1] * 6, [100, 101, 133, 300, 164, 100], 8, 2, 128, 16, 100),     # a shared prefix, odd and even pages
+    ([1] * 20, [256 + 3 * i for i in range(20)], 32, 8, 128, 64, 256),
+    ([3, 2, 1], [520, 515, 514], 16, 2, 64, 32, 513),
+    ([40, 7], [400, 300], 4, 1, 256, 64, 290),
+    ([1] * 3, [20, 700, 0], 8, 8, 128, 16, 600),               # shorter than the prefix, and empty
+]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["fp16", "bf16"])
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_against_oracle(shape, dtype):
+    q, kv, Hq, Hkv, D, page, prefix = SHAPES[shape]
+    c = Case(q, kv, Hq, Hkv, D, page, dtype, prefix, seed=shape)
+    check(c)
+    check(c, causal=False, out_dtype=F32)
+
+
+@pytest.mark.parametrize("window", [1, 2, 33, 100, 5000])
+@pytest.mark.parametrize("shape", [2, 6, 10, 12, 17])
+def test_window(shape, window):
+    q, kv, Hq, Hkv, D, page, prefix = SHAPES[shape]
+    c = Case(q, kv, Hq, Hkv, D, page, BF16 if shape % 2 else F16, prefix, seed=shape)
+    check(c, window=window)
+    check(c, window=window, causal=False)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_long_keys_are_split_and_joined(D):
+    c = Case([1, 2], [9001, 4097], 8, 2, D, 64, F16, seed=D)
+    check(c)
+    c = Case([1] * 4, [6000, 6100, 5555, 7000], 8, 2, D, 32, BF16, prefix=5555, seed=D)
+    check(c, out_dtype=F32)
+
+
+@pytest.mark.parametrize("n", [1, 15, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 255, 257])
+def test_lengths_around_tiles(n):
+    check(Case([1], [n], 4, 2, 128, 16, F16, seed=n))
+    check(Case([n], [n], 2, 1, 128, 16, BF16, seed=n))
+    check(Case([n], [n + 40], 1, 1, 64, 32, F16, seed=n))
+
+
+def test_uniform_batches_need_no_starts():
+    check(Case([3] * 4, [10, 500, 3, 129], 8, 2, 128, 16, F16, uniform=True))
+    check(Case([1] * 4, [10, 500, 3, 129], 8, 2, 128, 16, BF16, uniform=True))
+
+
+def test_sharp_scores_and_other_scales():
+    """Scores in the hundreds: the largest dominates and nothing overflows."""
+    c = Case([1, 30], [700, 300], 8, 2, 128, 16, F16, kstd=8.0)
+    check(c, scale=1.0)
+    check(c, scale=-0.5)
+    check(c, scale=0.0)
+
+
+def test_fused_projection_views():
+    """q as a view of a wider row: its tokens at a stride of their own."""
+    c = Case([2, 40], [100, 60], 8, 2, 128, 16, F16)
+    wide = torch.full((c.N, 8 * 128 + 2 * 2 * 128), float("nan"), dtype=F16, device="cuda")
+    wide[:, :8 * 128] = c.q.cuda().reshape(c.N, -1)
+    check(c, q=wide[:, :8 * 128].view(c.N, 8, 128))
+
+
+def test_rows_of_no_sequence_are_left_alone():
+    c = Case([2, 3], [40, 50], 4, 2, 64, 16, F16)
+    start = torch.tensor([1, 3, 6], dtype=torch.int32, device="cuda")
+    b = cl.KvBatch(c.batch.kv_len, c.table, 8, q_len=3, q_start=start, max_kv_len=50)
+    q = torch.zeros((8, 4, 64), dtype=F16, device="cuda")
+    q[1:6] = c.q.cuda()
+    out = torch.full((8, 4, 64), 7.0, dtype=F32, device="cuda")
+    cl.attention(c.cache, b, q, out=out)
+    want = cl.attention(c.cache, c.batch, c.q.cuda(), out_dtype=F32)
+    torch.cuda.synchronize()
+    assert torch.equal(out[1:6], want) and (out[0] == 7).all() and (out[6:] == 7).all()
+
+
+def test_pages_outside_the_pool_give_nan_and_touch_nothing_else():
+    c = Case([1, 1, 20], [100, 100, 100], 4, 2, 64, 16, F16)
+    good = cl.attention(c.cache, c.batch, c.q.cuda())
+    for bad in (-1, c.cache.num_pages, 1 << 30):
+        c.table[1, 3] = bad
+        out = cl.attention(c.cache, c.batch, c.q.cuda())
+        torch.cuda.synchronize()
+        assert out[1].isnan().all() and torch.equal(out[0], good[0]) and torch.equal(out[2:], good[2:])
+
+
+def test_lengths_beyond_the_bounds_are_cut():
+    """A kv_len past max_kv_len or the table, and starts past the tokens, stay inside what the host gave."""
+    c = Case([1, 1], [64, 64], 4, 2, 64, 16, F16, spare=0)
+    want = cl.attention(c.cache, c.batch, c.q.cuda())
+    wide = cl.KvBatch(torch.tensor([1 << 30, 64], dtype=torch.int32, device="cuda"), c.table[:, :4].contiguous(), 2,
+                      q_start=torch.tensor([0, 1, 999], dtype=torch.int32, device="cuda"))
+    got = cl.attention(c.cache, wide, c.q.cuda())
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_results_repeat_bit_for_bit_and_on_other_streams():
+    c = Case([1, 3, 50], [5000, 3000, 400], 8, 2, 128, 16, BF16, prefix=300)
+    q = c.q.cuda()
+    want = cl.attention(c.cache, c.batch, q, out_dtype=F32)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        assert torch.equal(cl.attention(c.cache, c.batch, q, out_dtype=F32), want)
+        with torch.cuda.stream(side):
+            x = q + 0
+            got = cl.attention(c.cache, c.batch, x, out_dtype=F32)
+        explicit = cl.attention(c.cache, c.batch, q, out_dtype=F32, stream=torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(explicit, want)
+
+
+def test_a_pool_beyond_2_31_elements():
+    """The last pages of a pool of 2^31 + elements: offsets pass 32 bits."""
+    Hkv, page, D = 8, 64, 128
+    pages = (1 << 31) // (Hkv * page * D) + 3
+    k = torch.empty((pages, Hkv, page, D), dtype=F16, device="cuda")
+    v = torch.empty_like(k)
+    c = Case([1, 9], [150, 100], 16, Hkv, D, page, F16, spare=0)
+    own = torch.arange(c.cache.num_pages, dtype=torch.int32, device="cuda")
+    at = pages - c.cache.num_pages
+    k[at:], v[at:] = c.cache.k[own.long()], c.cache.v[own.long()]
+    table = torch.where(c.table >= 0, c.table + at, c.table)
+    b = cl.KvBatch(c.batch.kv_len, table, c.N, q_len=9, q_start=c.batch.q_start, max_kv_len=150)
+    got = cl.attention(cl.KvCache(k, v), b, c.q.cuda())
+    want = cl.attention(c.cache, c.batch, c.q.cuda())
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_workspace_is_checked_and_sized_by_the_descriptors():
+    c = Case([1], [9000], 8, 2, 128, 16, F16)
+    need = cl.attention_workspace(c.cache, c.batch, 8)
+    if need:
+        with pytest.raises(cl.ClError) as e:
+            cl.attention(c.cache, c.batch, c.q.cuda(), ws=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
+        assert e.value.status == cl.CL_EWORKSPACE
+    ws = torch.full((need + 256,), 255, dtype=torch.uint8, device="cuda")     # NaN: nothing in it has to be set
+    out = cl.attention(c.cache, c.batch, c.q.cuda(), ws=ws)
+    torch.cuda.synchronize()
+    assert out.isfinite().all() and (ws[need:] == 255).all()
