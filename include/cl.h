@@ -496,8 +496,9 @@ cl_status cl_layer_sensitivity(int32_t L, const double* D, int32_t K, double* S)
  *  k, v       device [num_pages][kv_heads][page_size][head_dim] of dtype
  *             (CL_FP16 or CL_BF16), 16-byte aligned: a head's keys of a page
  *             are one contiguous run, which is what attention streams
- *  page_size  a power of two, 1..1024;  kv_heads * head_dim, and so the rows,
- *             are the same for every page.  A pool may pass 2^31 elements.
+ *  page_size  a power of two, 1..1024.  A pool may pass 2^31 elements;
+ *             num_pages * kv_heads * page_size stays below 2^31
+ *             (CL_EUNSUPPORTED beyond)
  *  head_dim   64, 128 or 256 (CL_EUNSUPPORTED otherwise)
  */
 typedef struct cl_kv_cache {
@@ -528,7 +529,8 @@ typedef struct cl_kv_cache {
  *               alone
  *  q_len        the most new tokens of one sequence (>= 1); further ones are
  *               not attended for
- *  max_kv_len   an upper bound of kv_len, which sizes the launch
+ *  max_kv_len   an upper bound of kv_len, which sizes the launch (a sequence
+ *               holds 2^30 keys at most)
  * Token i of a sequence with n keys and a new tokens stands at position
  * n - a + i.  The arrays live in device memory, so a wrong entry cannot fail
  * the call; the kernels hold every value inside these bounds: a kv_len is cut

@@ -508,6 +508,8 @@ bool act_type(int dt) { return dt == CL_FP16 || dt == CL_BF16; }
 bool out_type(int dt) { return act_type(dt) || dt == CL_FP32; }
 size_t type_size(int dt) { return dt == CL_FP32 ? 4 : 2; }
 
+constexpr long long kMaxKeys = 1ll << 30;    // of one sequence
+
 cl_status check_kv(const cl_kv_cache* c, const cl_kv_batch* b, cl::KvCache* oc, cl::KvBatch* ob, const char* who) {
     if (!c || !b) return fail(CL_EINVAL, "%s: null cache or batch descriptor", who);
     if (!c->k || !c->v || !aligned(c->k, 16) || !aligned(c->v, 16))
@@ -537,9 +539,13 @@ cl_status check_kv(const cl_kv_cache* c, const cl_kv_batch* b, cl::KvCache* oc, 
     while ((1 << shift) < c->page_size) ++shift;
     long long limit = b->prefix_len + (static_cast<long long>(b->table_width) << shift);
     if (limit > b->max_kv_len) limit = b->max_kv_len;
+    if (limit > kMaxKeys) limit = kMaxKeys;
+    if ((static_cast<long long>(c->num_pages) * c->kv_heads << shift) > 0x7fffffffll)
+        return fail(CL_EUNSUPPORTED, "%s: num_pages * kv_heads * page_size must be below 2^31", who);
     *oc = {static_cast<uint16_t*>(c->k), static_cast<uint16_t*>(c->v), c->num_pages, shift, c->kv_heads, c->head_dim,
            c->dtype};
-    *ob = {b->q_start, b->kv_len, b->page_table, b->prefix_table, b->num_seqs, b->tokens, b->q_len, b->table_width,
+    const int q_len = b->q_len < b->tokens ? b->q_len : b->tokens;
+    *ob = {b->q_start, b->kv_len, b->page_table, b->prefix_table, b->num_seqs, b->tokens, q_len, b->table_width,
            b->prefix_len, static_cast<int>(limit)};
     return CL_OK;
 }
@@ -630,6 +636,8 @@ cl_status cl_attention(const cl_kv_cache* cache, const cl_kv_batch* batch, const
         return fail(CL_EINVAL, "%s: q rows and out must be 16-byte aligned", who);
     if (q_stride < static_cast<int64_t>(q_heads) * cache->head_dim)
         return fail(CL_EINVAL, "%s: q_stride is shorter than a token's heads", who);
+    if (static_cast<long long>(batch->tokens) * q_heads > 0x7fffffffll)
+        return fail(CL_EUNSUPPORTED, "%s: tokens * q_heads must be below 2^31", who);
     if (!isfinite(scale)) return fail(CL_EINVAL, "%s: scale must be finite", who);
     if (window < 0) return fail(CL_EINVAL, "%s: window must not be negative", who);
     if (!out_type(out_dtype)) return fail(CL_EINVAL, "%s: out_dtype must be CL_FP16, CL_BF16 or CL_FP32", who);
@@ -644,7 +652,7 @@ cl_status cl_attention(const cl_kv_cache* cache, const cl_kv_batch* batch, const
     a.q_stride = q_stride;
     a.q_heads = q_heads;
     a.causal = causal ? 1 : 0;
-    a.window = window;
+    a.window = window < kMaxKeys ? window : 0;         // a window of the longest sequence hides nothing
     a.out_dtype = out_dtype;
     a.scale = scale;
     a.out = out;

@@ -5,8 +5,34 @@
 //
 //     o = sum_j e^{s_j - m} v_j / sum_j e^{s_j - m},  s_j = scale q . k_j,  m = max_j s_j
 //
-// A workgroup takes one token and head; its four waves take every fourth key
-// with a running maximum and sum of their own and meet in LDS at the end.
+// One pass over the keys with a running maximum and sum.  The rows of a unit
+// are the queries that share a key head: token i and head h of the group are
+// row i g + h (g = q_heads / kv_heads), 16 rows to an MFMA block.  Both products
+// are taken transposed on v_mfma_f32_16x16x32:
+//
+//     S^T = K Q^T    a lane holds 4 keys of one row (column) per block
+//     O^T = V^T P^T  the same lane's probabilities are its operand as they are
+//
+// Between them no value changes lanes: 16x16x32 sums over 8 keys of each lane
+// group g, and which keys these are is free as long as both operands agree, so
+// group g takes keys 4g..4g+3 of two neighbouring 16-key blocks, what S^T left
+// there.  V^T comes from row-major V in LDS by the transposing read (16 lanes
+// turn 4 keys x 16 dims).  Row sums stay per lane until the end; only the
+// maximum crosses lanes (two swaps a block).
+//
+// The keys are two segments, the shared prefix and a sequence's own pages.
+// Where there are fewer units than the chip has room for, or a prefix, a
+// segment is cut into splits that write partial results (unnormalised O, m, l)
+// to the workspace, and attn_join_kernel adds them in split order.
+//
+//  * attn_stream_kernel: units of up to 32 rows (decode).  Bound by the read
+//    of K and V: each wave streams keys of its own, 32 at a time, K straight
+//    into operand registers, V through its own slice of LDS; nothing in the
+//    loop waits for another wave.
+//  * attn_tile_kernel: more rows (prompts, a shared prefix under many
+//    sequences).  Bound by MFMA and the softmax: four waves of 16 NQ rows
+//    share tiles of 64 keys in LDS, double-buffered, the next tile's loads in
+//    flight during the current one's products.
 
 #include "cl_device.h"
 #include "cl_internal.h"
@@ -15,80 +41,751 @@
 namespace cl {
 namespace {
 
-__global__ __launch_bounds__(256) void attention_kernel(AttnArgs a) {
-    __shared__ float part[4][2 + 256];
-    const int t = blockIdx.x, head = blockIdx.y;
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+template <bool BF>
+__device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
+    if constexpr (BF)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, a), __builtin_bit_cast(b16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// Two floats to two 16-bit values, round to nearest even (one instruction).
+template <bool BF>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    if constexpr (BF) return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), b16x2));
+    else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
+}
+
+// The two values of a lane pair (l, l ^ 32), then of the rows of 16 lanes.
+// (Elements are copied out before they are reinterpreted: a bit cast of a
+// vector's element takes element 0.)
+__device__ __forceinline__ f32x2 swap32(float v) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t x = r[0], y = r[1];
+    return f32x2{__builtin_bit_cast(float, x), __builtin_bit_cast(float, y)};
+}
+
+__device__ __forceinline__ f32x2 swap16(float v) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const uint32_t x = r[0], y = r[1];
+    return f32x2{__builtin_bit_cast(float, x), __builtin_bit_cast(float, y)};
+}
+
+// Over the four lanes that share a row (l, l ^ 16, l ^ 32, l ^ 48).
+__device__ __forceinline__ float row_max(float v) {
+    const f32x2 a = swap32(v);
+    const f32x2 b = swap16(fmaxf(a[0], a[1]));
+    return fmaxf(b[0], b[1]);
+}
+
+__device__ __forceinline__ float row_sum(float v) {
+    const f32x2 a = swap32(v);
+    const f32x2 b = swap16(a[0] + a[1]);
+    return b[0] + b[1];
+}
+
+// How a call is cut; every field follows from the host's sizes alone.
+struct Plan {
+    int rows;              // most rows of a unit
+    int blocks;            // row blocks of a unit
+    int splits, len;       // of a sequence's own keys: splits of `len` keys
+    int pblocks, psplits, plen;      // of the shared prefix, whose unit has every token's rows
+    int direct;            // one split and no prefix: results go straight to out
+    float* part;           // [psplits + splits][tokens * q_heads][dim], unnormalised
+    float2* stat;          // [psplits + splits][tokens * q_heads]: m (in bits), l
+};
+
+// A row's place: its token (-1: none) and the keys it sees, [lo, hi) of the segment.
+struct Row {
+    int token, lo, hi;
+};
+
+// One unit's segment of keys.
+struct Segment {
+    const int32_t* table;
+    int keys;              // keys of the segment
+    int base;              // position of its first key
+    Seq seq;               // of the sequence (own keys only)
+};
+
+__device__ __forceinline__ Row clip(const AttnArgs& a, int token, int pos, int keys, int base, int seg_keys) {
+    Row r;
+    r.token = token;
+    const int hi = a.causal ? min(pos + 1, keys) : keys;
+    const int lo = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
+    r.hi = min(max(hi - base, 0), seg_keys);
+    r.lo = min(max(lo - base, 0), seg_keys);
+    return r;
+}
+
+__device__ __forceinline__ Row row_place(const AttnArgs& a, const Segment& g, int row, int group, bool prefix) {
+    const int i = row / group;
+    if (!prefix) {
+        if (i >= g.seq.count) return Row{-1, 0, 0};
+        return clip(a, g.seq.start + i, g.seq.keys - g.seq.count + i, g.seq.keys, g.base, g.keys);
+    }
+    // the rows of every token: the last sequence that starts at or before it
+    if (i >= a.batch.tokens) return Row{-1, 0, 0};
+    int s = i / a.batch.q_len;
+    if (a.batch.q_start) {
+        s = -1;
+        for (int j = 0; j < a.batch.num_seqs; ++j) s += a.batch.q_start[j] <= i;
+        if (s < 0) return Row{-1, 0, 0};
+    }
+    const Seq q = load_seq(a.batch, s);
+    if (i >= q.start + q.count) return Row{-1, 0, 0};
+    return clip(a, i, q.keys - q.count + (i - q.start), q.keys, 0, g.keys);
+}
+
+// Row number in the pool of key `key` of the segment (a head's row of dim
+// values), or -1 if its page is outside the pool.
+__device__ __forceinline__ int pool_row(const AttnArgs& a, const Segment& g, int head, int key) {
+    const int page = g.table[key >> a.cache.page_shift];
+    const int in = key & ((1 << a.cache.page_shift) - 1);
+    if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.cache.num_pages)) return -1;
+    return ((page * a.cache.heads + head) << a.cache.page_shift) + in;
+}
+
+constexpr u32x4 kNaNs = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};   // NaN in fp16 and bf16
+constexpr u32x4 kZeros = {0u, 0u, 0u, 0u};
+
+// A block's queries as the second operand, with scale's sign: dims 32 i + 8 g ..
+template <int D, bool BF>
+__device__ __forceinline__ void load_q(const AttnArgs& a, const Row& r, int head, u32x4 (&q)[D / 32]) {
+    const int g = (threadIdx.x & 63) >> 4;
+    const uint16_t* p = a.q + static_cast<long long>(r.token) * a.q_stride + static_cast<long long>(head) * D + 8 * g;
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+        q[i] = kZeros;
+        if (r.token >= 0 && a.scale != 0.f) q[i] = *reinterpret_cast<const u32x4*>(p + 32 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[i][j] ^= flip;
+    }
+}
+
+// Running softmax of one row block over KB 16-key blocks of scores: s becomes
+// probabilities (packed into p), m and l move on, o and l are rescaled if the
+// maximum rose.  sc > 0 is |scale| log2 e; m is in the scores' own units.
+template <int KB, int ND, bool BF>
+__device__ __forceinline__ void softmax_step(f32x4 (&s)[KB], uint32_t (&p)[KB][2], float sc, float& m, float& l,
+                                             f32x4 (&o)[ND]) {
+    float mx = s[0][0];
+#pragma unroll
+    for (int k = 0; k < KB; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[k][i]);
+    mx = fmaxf(m, row_max(mx));
+    const float mc = mx == -INFINITY ? 0.f : mx * sc;
+    if (__ballot(mx > m)) {
+        const float old = m == -INFINITY ? mc : m * sc;
+        const float c = __builtin_amdgcn_exp2f(old - mc);
+        l *= c;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] *= c;
+    }
+    m = mx;
+#pragma unroll
+    for (int k = 0; k < KB; ++k) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s[k][i] = __builtin_amdgcn_exp2f(fmaf(s[k][i], sc, -mc));
+            l += s[k][i];
+        }
+        p[k][0] = pack2<BF>(s[k][0], s[k][1]);
+        p[k][1] = pack2<BF>(s[k][2], s[k][3]);
+    }
+}
+
+// Results of a row block: o[d] holds dims 16 d + 4 g + 0..3 of the lane's row.
+template <int ND>
+__device__ __forceinline__ void finish(const AttnArgs& a, const Plan& pl, int slot, const Row& r, int head, float sc,
+                                       float m, float l, const f32x4 (&o)[ND]) {
+    if (r.token < 0) return;
+    const int g = (threadIdx.x & 63) >> 4;
+    constexpr int D = 16 * ND;
+    const size_t row = static_cast<size_t>(r.token) * a.q_heads + head;
+    if (!pl.direct) {
+        const size_t at = static_cast<size_t>(slot) * a.batch.tokens * a.q_heads + row;
+        float* to = pl.part + at * D + 4 * g;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4*>(to + 16 * d) = o[d];
+        if (g == 0) pl.stat[at] = float2{m * sc, l};
+        return;
+    }
+    const float inv = l != 0.f ? 1.0f / l : 0.f;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+        const size_t at = row * D + 16 * d + 4 * g;
+        f32x4 v = o[d] * inv;
+        if (l == 0.f) v = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (a.out_dtype == DT_FP32) {
+            *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = v;
+        } else {
+            const u32x2 u = a.out_dtype == DT_BF16 ? u32x2{pack2<true>(v[0], v[1]), pack2<true>(v[2], v[3])}
+                                                   : u32x2{pack2<false>(v[0], v[1]), pack2<false>(v[2], v[3])};
+            *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at) = u;
+        }
+    }
+    if (a.lse && g == 0) a.lse[row] = l != 0.f ? (m * sc + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+}
+
+// V in LDS, row-major with D values a row, 16-byte chunk c of row r at place
+// c ^ (r & kMask): rows of 128 bytes and more start on the same banks, the
+// exclusive or spreads a column of rows over them.
+template <int D>
+__device__ __forceinline__ int swz(int row, int chunk) {
+    constexpr int kMask = D / 8 < 16 ? D / 8 - 1 : 15;
+    return row * (D / 8) + (chunk ^ (row & kMask));
+}
+
+// Operand of V^T: 16 dims (block d) x 32 keys (rows 32 kk ..) of a tile in LDS.
+template <int D>
+__device__ __forceinline__ u32x4 load_vt(const uint16_t* v, int kk, int d) {
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const int lane = threadIdx.x & 63, g = lane >> 4, i = lane & 15;
+    u32x4 r;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const int row = 32 * kk + 16 * half + 4 * g + (i >> 2);
+        const int col = 16 * d + 4 * (i & 3);
+        const uint16_t* p = v + 8 * swz<D>(row, col >> 3) + (col & 7);
+        const s16x4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+        const u32x2 u = __builtin_bit_cast(u32x2, t);
+        r[2 * half] = u[0];
+        r[2 * half + 1] = u[1];
+    }
+    return r;
+}
+
+__device__ __forceinline__ Segment own_segment(const AttnArgs& a, int s) {
+    Segment g;
+    g.seq = load_seq(a.batch, s);
+    g.table = a.batch.page_table + static_cast<size_t>(s) * a.batch.table_width;
+    g.base = a.batch.prefix_len;
+    g.keys = max(g.seq.keys - g.base, 0);
+    return g;
+}
+
+__device__ __forceinline__ Segment prefix_segment(const AttnArgs& a) {
+    return Segment{a.batch.prefix_table, min(a.batch.prefix_len, a.batch.key_limit), 0, Seq{0, 0, 0}};
+}
+
+// ------------------------------------------------------------- few rows
+
+template <int D, bool BF, int NQ>
+__global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnArgs a, Plan pl, int prefix) {
+    constexpr int NS = D / 32, ND = D / 16, CH = D / 8;
+    __shared__ __attribute__((aligned(16))) uint16_t vbuf[4][32 * D];
+    __shared__ float2 stat[4][16 * NQ];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g4 = lane >> 4, col = lane & 15;
+    const int Hk = a.cache.heads, group = a.q_heads / Hk;
+    const int head = blockIdx.x % Hk;
+    int rest = blockIdx.x / Hk;
+    const int splits = prefix ? pl.psplits : pl.splits, len = prefix ? pl.plen : pl.len;
+    const int split = rest % splits;
+    rest /= splits;
+    const Segment seg = prefix ? prefix_segment(a) : own_segment(a, rest);
+    const int begin = split * len, end = min(begin + len, seg.keys);
+    if (begin >= end && !pl.direct) return;
+
+    Row row[NQ];
+    u32x4 q[NQ][NS];
+    int hidx[NQ];
+    int lo = 0x7fffffff, hi = 0;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const int r = 16 * n + col;
+        row[n] = r < (prefix ? a.batch.tokens * group : pl.rows) ? row_place(a, seg, r, group, prefix) : Row{-1, 0, 0};
+        hidx[n] = head * group + r % group;
+        load_q<D, BF>(a, row[n], hidx[n], q[n]);
+        if (row[n].hi > row[n].lo) lo = min(lo, row[n].lo), hi = max(hi, row[n].hi);
+    }
+    // the wave's steps cover the keys that any of its rows sees
+#pragma unroll
+    for (int off = 1; off < 16; off <<= 1) {
+        lo = min(lo, __shfl_xor(lo, off, 64));
+        hi = max(hi, __shfl_xor(hi, off, 64));
+    }
+    lo = max(lo, begin) & ~31;
+    hi = min(hi, end);
+    if (hi <= lo) lo = hi = 0;                        // nothing to see here
+    const float sc = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f;
+
+    float m[NQ], l[NQ];
+    f32x4 o[NQ][ND];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        m[n] = -INFINITY;
+        l[n] = 0.f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    uint16_t* vl = vbuf[wave];
+    u32x4 kr[2][NS], vr[CH / 2];
+    constexpr int VR = CH / 2;                // 32 rows x CH chunks over 64 lanes
+    // lane l looks up key l of a step; the lanes that load a row ask for it
+    const auto look = [&](int at) { return at + (lane & 31) < seg.keys ? pool_row(a, seg, head, at + (lane & 31)) : -2; };
+    const auto fetch = [&](int where) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int r = __shfl(where, 16 * b + col, 64);
+            const uint16_t* p = a.cache.k + static_cast<size_t>(r < 0 ? 0 : r) * D + 8 * g4;
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                kr[b][i] = r == -1 ? kNaNs : kZeros;
+                if (r >= 0) kr[b][i] = *reinterpret_cast<const u32x4*>(p + 32 * i);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < VR; ++i) {
+            const int c = lane + 64 * i;
+            const int r = __shfl(where, c / CH, 64);
+            vr[i] = kZeros;
+            if (r >= 0) vr[i] = *reinterpret_cast<const u32x4*>(a.cache.v + static_cast<size_t>(r) * D + 8 * (c % CH));
+        }
+    };
+
+    int at = lo + 32 * wave;
+    if (at < hi) {
+        fetch(look(at));
+        int next = look(at + 128);
+        for (; at < hi; at += 128) {
+            f32x4 s[NQ][2];
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    s[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) s[n][b] = mma<BF>(kr[b][i], q[n][i], s[n][b]);
+                }
+#pragma unroll
+            for (int i = 0; i < VR; ++i) {
+                const int c = lane + 64 * i;
+                *reinterpret_cast<u32x4*>(vl + 8 * swz<D>(c / CH, c % CH)) = vr[i];
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const int cur = at;
+            if (at + 128 < hi) {
+                fetch(next);
+                next = look(at + 256);
+            }
+            uint32_t p[NQ][2][2];
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = cur + 16 * b + 4 * g4 + i;
+                        if (key < row[n].lo || key >= min(row[n].hi, end)) s[n][b][i] = -INFINITY;
+                    }
+                softmax_step<2, ND, BF>(s[n], p[n], sc, m[n], l[n], o[n]);
+            }
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                const u32x4 vt = load_vt<D>(vl, 0, d);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+                    o[n][d] = mma<BF>(vt, u32x4{p[n][0][0], p[n][0][1], p[n][1][0], p[n][1][1]}, o[n][d]);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+    }
+
+    // the four waves' results meet: maxima first, then the rescaled sums, in
+    // wave order, through the V buffers (16 NQ rows x D floats)
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        l[n] = row_sum(l[n]);
+        if (g4 == 0) stat[wave][16 * n + col] = float2{m[n], l[n]};
+    }
+    __syncthreads();
+    float* sum = reinterpret_cast<float*>(&vbuf[0][0]);
+    static_assert(sizeof(vbuf) >= 4 * 16 * D * sizeof(float), "one row block of every wave");
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        float mm = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) mm = fmaxf(mm, stat[w][16 * n + col].x);
+        const float mc = mm == -INFINITY ? 0.f : mm * sc;
+        float ll = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float2 t = stat[w][16 * n + col];
+            if (t.x != -INFINITY || t.y != 0.f) ll += t.y * __builtin_amdgcn_exp2f((t.x == -INFINITY ? mc : t.x * sc) - mc);
+        }
+        const float c = __builtin_amdgcn_exp2f((m[n] == -INFINITY ? mc : m[n] * sc) - mc);
+        if (n) __syncthreads();
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+            *reinterpret_cast<f32x4*>(sum + (wave * 16 + col) * D + 4 * ((4 * d + g4) ^ col)) = o[n][d] * c;
+        __syncthreads();
+        // wave w adds the quarter of the dims it stores
+        constexpr int PER = ND / 4;
+        f32x4 r[ND];
+#pragma unroll
+        for (int d = 0; d < ND; ++d) r[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+                r[j] += *reinterpret_cast<const f32x4*>(sum + (w * 16 + col) * D + 4 * ((4 * (wave * PER + j) + g4) ^ col));
+        }
+        if (row[n].token < 0) continue;
+        const size_t rw = static_cast<size_t>(row[n].token) * a.q_heads + hidx[n];
+        const int slot = prefix ? split : pl.psplits + split;
+        if (!pl.direct) {
+            const size_t at2 = static_cast<size_t>(slot) * a.batch.tokens * a.q_heads + rw;
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+                *reinterpret_cast<f32x4*>(pl.part + at2 * D + 16 * (wave * PER + j) + 4 * g4) = r[j];
+            if (g4 == 0 && wave == 0) pl.stat[at2] = float2{mm * sc, ll};
+        } else {
+            const float inv = ll != 0.f ? 1.0f / ll : 0.f;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                const size_t to = rw * D + 16 * (wave * PER + j) + 4 * g4;
+                f32x4 v = r[j] * inv;
+                if (ll == 0.f) v = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (a.out_dtype == DT_FP32) {
+                    *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to) = v;
+                } else {
+                    const u32x2 u = a.out_dtype == DT_BF16 ? u32x2{pack2<true>(v[0], v[1]), pack2<true>(v[2], v[3])}
+                                                           : u32x2{pack2<false>(v[0], v[1]), pack2<false>(v[2], v[3])};
+                    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + to) = u;
+                }
+            }
+            if (a.lse && g4 == 0 && wave == 0)
+                a.lse[rw] = ll != 0.f ? (mm * sc + __builtin_amdgcn_logf(ll)) * kLn2 : -INFINITY;
+        }
+    }
+}
+
+// ------------------------------------------------------------- many rows
+
+template <int D, bool BF, int NQ>
+__global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_tile_kernel(AttnArgs a, Plan pl, int prefix) {
+    constexpr int NS = D / 32, ND = D / 16, CH = D / 8, KT = 64;
+    constexpr int RW = 64 * NQ;                       // rows of a workgroup
+    constexpr int CP = KT * CH / 256;                 // 16-byte chunks of K (and of V) a thread moves
+    extern __shared__ __attribute__((aligned(16))) uint16_t tiles[];          // [2][K, V][KT * D]
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g4 = lane >> 4, col = lane & 15;
+    const int Hk = a.cache.heads, group = a.q_heads / Hk;
+    const int head = blockIdx.x % Hk;
+    int rest = blockIdx.x / Hk;
+    const int splits = prefix ? pl.psplits : pl.splits, len = prefix ? pl.plen : pl.len;
+    const int split = rest % splits;
+    rest /= splits;
+    const int blocks = prefix ? pl.pblocks : pl.blocks;
+    const int block = blocks - 1 - rest % blocks;     // causal rows see more keys the later they stand: longest first
+    rest /= blocks;
+    const Segment seg = prefix ? prefix_segment(a) : own_segment(a, rest);
+    const int nrows = (prefix ? a.batch.tokens : min(seg.seq.count, a.batch.q_len)) * group;
+    if (block * RW >= nrows) return;
+    const int begin = split * len, end = min(begin + len, seg.keys);
+    if (begin >= end && !pl.direct) return;
+
+    Row row[NQ];
+    u32x4 q[NQ][NS];
+    int hidx[NQ];
+    int lo = 0x7fffffff, hi = 0, full_lo = 0, full_hi = 0x7fffffff;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const int r = block * RW + wave * 16 * NQ + 16 * n + col;
+        row[n] = r < nrows ? row_place(a, seg, r, group, prefix) : Row{-1, 0, 0};
+        hidx[n] = head * group + r % group;
+        load_q<D, BF>(a, row[n], hidx[n], q[n]);
+        if (row[n].hi > row[n].lo) lo = min(lo, row[n].lo), hi = max(hi, row[n].hi);
+        if (row[n].token >= 0) full_lo = max(full_lo, row[n].lo), full_hi = min(full_hi, row[n].hi);
+    }
+    // the wave's bounds, then the workgroup's
+#pragma unroll
+    for (int off = 1; off < 16; off <<= 1) {
+        lo = min(lo, __shfl_xor(lo, off, 64));
+        hi = max(hi, __shfl_xor(hi, off, 64));
+        full_lo = max(full_lo, __shfl_xor(full_lo, off, 64));
+        full_hi = min(full_hi, __shfl_xor(full_hi, off, 64));
+    }
+    __shared__ int bounds[2][4];
+    if (lane == 0) bounds[0][wave] = lo, bounds[1][wave] = hi;
+    __syncthreads();
+    int wlo = lo, whi = hi;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) lo = min(lo, bounds[0][w]), hi = max(hi, bounds[1][w]);
+    lo = max(lo, begin) & ~(KT - 1);
+    hi = min(hi, end);
+    wlo = __builtin_amdgcn_readfirstlane(wlo);
+    whi = __builtin_amdgcn_readfirstlane(whi);
+    full_lo = __builtin_amdgcn_readfirstlane(full_lo);
+    full_hi = __builtin_amdgcn_readfirstlane(min(full_hi, end));
+    const float sc = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f;
+
+    float m[NQ], l[NQ];
+    f32x4 o[NQ][ND];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        m[n] = -INFINITY;
+        l[n] = 0.f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    u32x4 kr[CP], vr[CP];
+    int where[CP];
+    const auto look = [&](int at) {
+#pragma unroll
+        for (int i = 0; i < CP; ++i) {
+            const int key = at + (tid + 256 * i) / CH;
+            where[i] = key < seg.keys ? pool_row(a, seg, head, key) : -2;
+        }
+    };
+    const auto fetch = [&]() {
+#pragma unroll
+        for (int i = 0; i < CP; ++i) {
+            const int r = where[i];
+            const size_t at = static_cast<size_t>(r < 0 ? 0 : r) * D + 8 * ((tid + 256 * i) % CH);
+            kr[i] = r == -1 ? kNaNs : kZeros;
+            vr[i] = kZeros;
+            if (r >= 0) {
+                kr[i] = *reinterpret_cast<const u32x4*>(a.cache.k + at);
+                vr[i] = *reinterpret_cast<const u32x4*>(a.cache.v + at);
+            }
+        }
+    };
+    const auto stash = [&](int buf) {
+        uint16_t* kt = tiles + buf * 2 * KT * D;
+#pragma unroll
+        for (int i = 0; i < CP; ++i) {
+            const int c = tid + 256 * i;
+            const int to = 8 * swz<D>(c / CH, c % CH);
+            *reinterpret_cast<u32x4*>(kt + to) = kr[i];
+            *reinterpret_cast<u32x4*>(kt + KT * D + to) = vr[i];
+        }
+    };
+
+    if (lo < hi) {
+        look(lo);
+        fetch();
+        look(lo + KT);
+        stash(0);
+        int buf = 0;
+        for (int at = lo; at < hi; at += KT, buf ^= 1) {
+            __syncthreads();
+            const bool more = at + KT < hi;
+            if (more) {
+                fetch();
+                look(at + 2 * KT);
+            }
+            const uint16_t* kt = tiles + buf * 2 * KT * D;
+            const uint16_t* vt = kt + KT * D;
+            if (at < whi && at + KT > wlo) {
+                f32x4 s[NQ][4];
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) s[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) {
+                        const u32x4 kf = *reinterpret_cast<const u32x4*>(kt + 8 * swz<D>(16 * b + col, 4 * i + g4));
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n) s[n][b] = mma<BF>(kf, q[n][i], s[n][b]);
+                    }
+                const bool masked = at < full_lo || at + KT > full_hi;
+                uint32_t p[NQ][4][2];
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) {
+                    if (masked) {
+                        const int from = row[n].lo, to = min(row[n].hi, end);
+#pragma unroll
+                        for (int b = 0; b < 4; ++b)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int key = at + 16 * b + 4 * g4 + i;
+                                if (key < from || key >= to) s[n][b][i] = -INFINITY;
+                            }
+                    }
+                    softmax_step<4, ND, BF>(s[n], p[n], sc, m[n], l[n], o[n]);
+                }
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        const u32x4 vf = load_vt<D>(vt, kk, d);
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n)
+                            o[n][d] = mma<BF>(vf, u32x4{p[n][2 * kk][0], p[n][2 * kk][1], p[n][2 * kk + 1][0], p[n][2 * kk + 1][1]},
+                                              o[n][d]);
+                    }
+            }
+            if (more) stash(buf ^ 1);
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+        finish<ND>(a, pl, prefix ? split : pl.psplits + split, row[n], hidx[n], sc, m[n], row_sum(l[n]), o[n]);
+}
+
+// ------------------------------------------------------------- joining splits
+
+// One wave a row: sum_i w_i O_i / sum_i w_i l_i, w_i = 2^{m_i - max m}, over
+// the row's live splits in order.  Splits that hold no key of the row's
+// sequence were never written and are not read.
+template <int D>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, Plan pl) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int D = a.cache.dim, dt = a.cache.dtype;
+    const size_t rows = static_cast<size_t>(a.batch.tokens) * a.q_heads;
+    const size_t row = static_cast<size_t>(blockIdx.x) * 4 + wave;
+    if (row >= rows) return;
+    const int t = static_cast<int>(row / a.q_heads);
     const int s = seq_of(a.batch, t);
     if (s < 0) return;
     const Seq q = load_seq(a.batch, s);
-    if (t >= q.start + q.count) return;
-    const int p = q.keys - q.count + (t - q.start);
-    const int hi = a.causal ? min(p + 1, q.keys) : q.keys;
-    const int lo = a.window > 0 ? max(0, p - a.window + 1) : 0;
-    const int kvh = head / (a.q_heads / a.cache.heads);
-    float qv[4], o[4] = {0.f, 0.f, 0.f, 0.f};
+    if (t >= q.start + q.count || t - q.start >= a.batch.q_len) return;
+    const int own = max(q.keys - a.batch.prefix_len, 0);
+    const int live = pl.psplits + (own + pl.len - 1) / pl.len;
+    float m = -INFINITY;
+    for (int i = lane; i < live; i += 64) m = fmaxf(m, pl.stat[i * rows + row].x);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int d = 64 * i + lane;
-        qv[i] = d < D ? act_to_f32(a.q[t * a.q_stride + static_cast<long long>(head) * D + d], dt) * a.scale : 0.f;
+    for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    const float base = m == -INFINITY ? 0.f : m;
+    constexpr int PER = D / 64;
+    float acc[PER], l = 0.f;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) acc[j] = 0.f;
+    for (int i = 0; i < live; ++i) {
+        const float2 st = pl.stat[i * rows + row];
+        if (st.y == 0.f) continue;                 // no key seen there
+        const float w = __builtin_amdgcn_exp2f((st.x == -INFINITY ? base : st.x) - base);
+        l += w * st.y;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) acc[j] += w * pl.part[(i * rows + row) * D + PER * lane + j];
     }
-    float m = -INFINITY, l = 0.f;
-    for (int j = lo + wave; j < hi; j += 4) {
-        const int mine = j - a.batch.prefix_len;
-        const int at = mine < 0 ? j : mine;
-        int page = mine < 0 ? a.batch.prefix_table[at >> a.cache.page_shift]
-                            : a.batch.page_table[static_cast<size_t>(s) * a.batch.table_width + (at >> a.cache.page_shift)];
-        const bool bad = static_cast<unsigned>(page) >= static_cast<unsigned>(a.cache.num_pages);
-        if (bad) page = 0;
-        const size_t slot = ((static_cast<size_t>(page) * a.cache.heads + kvh) << a.cache.page_shift) +
-                            (at & ((1 << a.cache.page_shift) - 1));
-        const uint16_t* k = a.cache.k + slot * D;
-        const uint16_t* v = a.cache.v + slot * D;
-        float x = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (64 * i + lane < D) x += qv[i] * act_to_f32(k[64 * i + lane], dt);
-        x = wave_sum(x);
-        if (bad) x = NAN;
-        const float mn = x > m ? x : m;
-        const float c = expf(m - (mn == -INFINITY ? 0.f : mn));
-        const float e = x == -INFINITY ? 0.f : expf(x - mn);
-        m = mn;
-        l = l * c + e;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (64 * i + lane < D) o[i] = o[i] * c + e * act_to_f32(v[64 * i + lane], dt);
+    for (int j = 0; j < PER; ++j)
+        store_out(a.out, row * D + PER * lane + j, l != 0.f ? acc[j] / l : 0.f, a.out_dtype);
+    if (a.lse && lane == 0) a.lse[row] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+}
+
+int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b); }
+
+// Rows up to which a unit streams, and rows of a tile workgroup.
+constexpr int kStreamRows = 32;
+int tile_rows(int rows) { return rows <= 64 ? 64 : 128; }
+
+// Splits of `keys` keys for `units` workgroups without splitting: enough to
+// give the chip `want` workgroups, none under `least` keys.
+void cut(long long units, int keys, int want, int least, int* splits, int* len) {
+    int n = ceil_div(want, units);
+    const int most = keys > least ? ceil_div(keys, least) : 1;
+    if (n > most) n = most;
+    if (n < 1) n = 1;
+    *len = keys > 0 ? ceil_div(ceil_div(keys, n), least) * least : least;
+    *splits = keys > 0 ? ceil_div(keys, *len) : 1;
+}
+
+Plan make_plan(const KvCache& c, const KvBatch& b, int q_heads) {
+    Plan p{};
+    const int group = q_heads / c.heads;
+    const long long rows = static_cast<long long>(b.q_len) * group;
+    p.rows = static_cast<int>(rows);
+    const int own = b.key_limit > b.prefix_len ? b.key_limit - b.prefix_len : 0;
+    const bool stream = rows <= kStreamRows;
+    p.blocks = stream ? 1 : ceil_div(rows, tile_rows(p.rows));
+    cut(static_cast<long long>(b.num_seqs) * c.heads * p.blocks, own, stream ? 1024 : 512, stream ? 128 : 512, &p.splits, &p.len);
+    if (b.prefix_len > 0) {
+        const long long prows = static_cast<long long>(b.tokens) * group;
+        const bool ps = prows <= kStreamRows;
+        p.pblocks = ps ? 1 : ceil_div(prows, tile_rows(static_cast<int>(prows < 1000 ? prows : 1000)));
+        const int keys = b.prefix_len < b.key_limit ? b.prefix_len : b.key_limit;
+        if (keys > 0) cut(static_cast<long long>(c.heads) * p.pblocks, keys, ps ? 1024 : 512, ps ? 128 : 256, &p.psplits, &p.plen);
     }
-    if (lane == 0) part[wave][0] = m, part[wave][1] = l;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) part[wave][2 + 64 * i + lane] = o[i];
-    __syncthreads();
-    if (wave) return;
-    float mm = -INFINITY;
-    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, part[w][0]);
-    float ll = 0.f, r[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int w = 0; w < 4; ++w) {
-        const float c = part[w][0] == -INFINITY && part[w][1] == 0.f ? 0.f : expf(part[w][0] - mm);
-        ll += c * part[w][1];
-        for (int i = 0; i < 4; ++i) r[i] += c * part[w][2 + 64 * i + lane];
+    p.direct = p.splits == 1 && p.psplits == 0;
+    return p;
+}
+
+size_t up256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
+
+template <int D, bool BF, int NQ>
+hipError_t tile(const AttnArgs& a, const Plan& p, int prefix, long long grid, hipStream_t st) {
+    constexpr int bytes = 2 * 2 * 64 * D * 2;
+    if (bytes > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_tile_kernel<D, BF, NQ>),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
     }
-    const size_t row = static_cast<size_t>(t) * a.q_heads + head;
-    for (int i = 0; i < 4; ++i)
-        if (64 * i + lane < D) store_out(a.out, row * D + 64 * i + lane, ll != 0.f ? r[i] / ll : 0.f, a.out_dtype);
-    if (a.lse && lane == 0) a.lse[row] = ll != 0.f ? mm + logf(ll) : -INFINITY;
+    hipLaunchKernelGGL((attn_tile_kernel<D, BF, NQ>), dim3(static_cast<unsigned>(grid)), dim3(256), bytes, st, a, p, prefix);
+    return hipGetLastError();
+}
+
+template <int D, bool BF>
+hipError_t part(const AttnArgs& a, const Plan& p, int prefix, hipStream_t st) {
+    const long long rows = prefix ? static_cast<long long>(a.batch.tokens) * (a.q_heads / a.cache.heads) : p.rows;
+    const long long grid = static_cast<long long>(a.cache.heads) *
+                           (prefix ? static_cast<long long>(p.psplits) * p.pblocks
+                                   : static_cast<long long>(p.splits) * p.blocks * a.batch.num_seqs);
+    if (grid > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (rows <= 16) {
+        hipLaunchKernelGGL((attn_stream_kernel<D, BF, 1>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, a, p, prefix);
+        return hipGetLastError();
+    }
+    if (rows <= kStreamRows) {
+        hipLaunchKernelGGL((attn_stream_kernel<D, BF, 2>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, a, p, prefix);
+        return hipGetLastError();
+    }
+    if (rows <= 64) return tile<D, BF, 1>(a, p, prefix, grid, st);
+    return tile<D, BF, 2>(a, p, prefix, grid, st);
+}
+
+template <int D, bool BF>
+hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t st) {
+    if (p.psplits) {
+        const hipError_t e = part<D, BF>(a, p, 1, st);
+        if (e != hipSuccess) return e;
+    }
+    const hipError_t e = part<D, BF>(a, p, 0, st);
+    if (e != hipSuccess || p.direct) return e;
+    const size_t rows = static_cast<size_t>(a.batch.tokens) * a.q_heads;
+    hipLaunchKernelGGL((attn_join_kernel<D>), dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, st, a, p);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 bool attention_dim_ok(int dim) { return dim == 64 || dim == 128 || dim == 256; }
 
-size_t attention_workspace_bytes(const KvCache&, const KvBatch&, int) { return 0; }
+size_t attention_workspace_bytes(const KvCache& c, const KvBatch& b, int q_heads) {
+    const Plan p = make_plan(c, b, q_heads);
+    if (p.direct) return 0;
+    const size_t n = static_cast<size_t>(p.psplits + p.splits) * b.tokens * q_heads;
+    return up256(n * c.dim * sizeof(float)) + up256(n * sizeof(float2));
+}
 
-hipError_t launch_attention(const AttnArgs& a, void*, hipStream_t st) {
-    hipLaunchKernelGGL(attention_kernel, dim3(a.batch.tokens, a.q_heads), dim3(256), 0, st, a);
-    return hipGetLastError();
+hipError_t launch_attention(const AttnArgs& a, void* ws, hipStream_t st) {
+    Plan p = make_plan(a.cache, a.batch, a.q_heads);
+    if (!p.direct) {
+        const size_t n = static_cast<size_t>(p.psplits + p.splits) * a.batch.tokens * a.q_heads;
+        p.part = static_cast<float*>(ws);
+        p.stat = reinterpret_cast<float2*>(static_cast<char*>(ws) + up256(n * a.cache.dim * sizeof(float)));
+    }
+    const bool bf = a.cache.dtype == DT_BF16;
+    if (a.cache.dim == 64) return bf ? run<64, true>(a, p, st) : run<64, false>(a, p, st);
+    if (a.cache.dim == 128) return bf ? run<128, true>(a, p, st) : run<128, false>(a, p, st);
+    return bf ? run<256, true>(a, p, st) : run<256, false>(a, p, st);
 }
 
 }  // namespace cl
