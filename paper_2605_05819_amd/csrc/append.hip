@@ -22,53 +22,78 @@
 namespace cl {
 namespace {
 
+struct Raw {                   // four 16-bit values as they stand
+    uint32_t a, b;
+};
+
 struct Quad {
     float v[4];
 };
 
 template <bool VEC>
-__device__ __forceinline__ Quad load4(const uint16_t* p, int at, int dt) {
-    Quad q;
+__device__ __forceinline__ Raw load4(const uint16_t* p, int at) {
     if constexpr (VEC) {
         const u32x2 u = *reinterpret_cast<const u32x2*>(p + at);
-        const uint32_t a = u[0], b = u[1];
-        q.v[0] = act_to_f32(static_cast<uint16_t>(a & 0xffff), dt);
-        q.v[1] = act_to_f32(static_cast<uint16_t>(a >> 16), dt);
-        q.v[2] = act_to_f32(static_cast<uint16_t>(b & 0xffff), dt);
-        q.v[3] = act_to_f32(static_cast<uint16_t>(b >> 16), dt);
+        return Raw{u[0], u[1]};
     } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) q.v[i] = act_to_f32(p[at + i], dt);
+        return Raw{p[at] | static_cast<uint32_t>(p[at + 1]) << 16, p[at + 2] | static_cast<uint32_t>(p[at + 3]) << 16};
     }
-    return q;
-}
-
-__device__ __forceinline__ uint32_t round_bits(float v, int dt) {
-    return dt == DT_FP16 ? f32_to_f16_bits(v) : f32_to_bf16_bits(v);
 }
 
 template <bool VEC>
-__device__ __forceinline__ void store4(uint16_t* p, int at, int dt, const Quad& q) {
-    uint32_t b[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) b[i] = round_bits(q.v[i], dt);
+__device__ __forceinline__ void store4(uint16_t* p, int at, Raw r) {
     if constexpr (VEC) {
-        *reinterpret_cast<u32x2*>(p + at) = u32x2{b[0] | b[1] << 16, b[2] | b[3] << 16};
+        *reinterpret_cast<u32x2*>(p + at) = u32x2{r.a, r.b};
     } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[at + i] = static_cast<uint16_t>(b[i]);
+        p[at] = static_cast<uint16_t>(r.a);
+        p[at + 1] = static_cast<uint16_t>(r.a >> 16);
+        p[at + 2] = static_cast<uint16_t>(r.b);
+        p[at + 3] = static_cast<uint16_t>(r.b >> 16);
     }
 }
 
-// Heads of a token in the order q, k, v; group `first` of `step` groups takes
-// every step-th head.  head_dim is a multiple of 8 and rot_dim of 8 (LG lanes
-// of 8 values cover a head).
-template <int LG, bool VEC>
-__global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a, int groups_per_token) {
+__device__ __forceinline__ Quad widen(Raw r, int dt) {
+    return Quad{{act_to_f32(static_cast<uint16_t>(r.a & 0xffff), dt), act_to_f32(static_cast<uint16_t>(r.a >> 16), dt),
+                 act_to_f32(static_cast<uint16_t>(r.b & 0xffff), dt), act_to_f32(static_cast<uint16_t>(r.b >> 16), dt)}};
+}
+
+__device__ __forceinline__ Raw narrow(const Quad& q, int dt) {
+    uint32_t b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = dt == DT_FP16 ? f32_to_f16_bits(q.v[i]) : f32_to_bf16_bits(q.v[i]);
+    return Raw{b[0] | b[1] << 16, b[2] | b[3] << 16};
+}
+
+// Heads of a token in the order q, k, v; group `first` takes every
+// step-th head, HP of them at most: their loads are issued together, ahead of
+// the chain that finds the token's page.  head_dim and rot_dim are multiples
+// of 8 (LG lanes of 8 values cover a head).
+template <int LG, bool VEC, int HP>
+__global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a, int step) {
     const int t = blockIdx.x;
     const int lane = threadIdx.x % LG;
     const int first = blockIdx.y * (blockDim.x / LG) + threadIdx.x / LG;
     const int D = a.cache.dim, dt = a.cache.dtype;
+    const int Hq = a.q ? a.q_heads : 0, Hk = a.cache.heads;
+
+    const int at = 8 * lane;                          // first of the lane's 8 values in memory order
+    const bool live = at < D;
+    const bool turned = a.rope.inv_freq && at < a.rope.rot_dim;
+    const bool half = turned && !a.rope.interleaved;
+    const int lo = half ? 4 * lane : at, hi = half ? a.rope.rot_dim / 2 + 4 * lane : at + 4;
+
+    Raw x[HP], y[HP];
+#pragma unroll
+    for (int i = 0; i < HP; ++i) {
+        const int h = first + i * step;
+        if (!live || h >= Hq + 2 * Hk) continue;
+        const bool is_v = h >= Hq + Hk;
+        const uint16_t* src = h < Hq ? a.q + static_cast<long long>(t) * a.q_stride + static_cast<size_t>(h) * D
+                              : is_v ? a.v + static_cast<long long>(t) * a.v_stride + static_cast<size_t>(h - Hq - Hk) * D
+                                     : a.k + static_cast<long long>(t) * a.k_stride + static_cast<size_t>(h - Hq) * D;
+        x[i] = load4<VEC>(src, is_v ? at : lo);
+        y[i] = load4<VEC>(src, is_v ? at + 4 : hi);
+    }
 
     // the token's place: the same for the whole workgroup
     const int s = seq_of(a.batch, t);
@@ -86,12 +111,6 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a, int groups
     }
     const bool stored = page >= 0 && page < a.cache.num_pages;
     const int angle_pos = a.positions ? a.positions[t] : pos;
-
-    const int at = 8 * lane;                          // first of the lane's 8 values in memory order
-    const bool live = at < D;
-    const bool turned = a.rope.inv_freq && at < a.rope.rot_dim;
-    const bool half = turned && !a.rope.interleaved;
-    const int lo = half ? 4 * lane : at, hi = half ? a.rope.rot_dim / 2 + 4 * lane : at + 4;
     float cs[4], sn[4];
     if (turned) {
 #pragma unroll
@@ -104,14 +123,12 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a, int groups
         }
     }
 
-    const int Hq = a.q ? a.q_heads : 0, Hk = a.cache.heads;
-    for (int h = first; h < Hq + 2 * Hk; h += groups_per_token) {
+#pragma unroll
+    for (int n = 0; n < HP; ++n) {
+        const int h = first + n * step;
+        if (h >= Hq + 2 * Hk) continue;
         const bool is_q = h < Hq, is_v = h >= Hq + Hk;
         const int head = is_q ? h : is_v ? h - Hq - Hk : h - Hq;
-        const uint16_t* src = is_q   ? a.q + static_cast<long long>(t) * a.q_stride
-                              : is_v ? a.v + static_cast<long long>(t) * a.v_stride
-                                     : a.k + static_cast<long long>(t) * a.k_stride;
-        src += static_cast<size_t>(head) * D;
         uint16_t* dst;
         if (is_q) {
             dst = a.q_out + (static_cast<size_t>(t) * Hq + head) * D;
@@ -121,71 +138,71 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a, int groups
         }
         if (is_v) {
             if (live && stored) {
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    if constexpr (VEC)
-                        *reinterpret_cast<u32x2*>(dst + at + 4 * c) = *reinterpret_cast<const u32x2*>(src + at + 4 * c);
-                    else
-                        for (int i = 0; i < 4; ++i) dst[at + 4 * c + i] = src[at + 4 * c + i];
-                }
+                store4<VEC>(dst, at, x[n]);
+                store4<VEC>(dst, at + 4, y[n]);
             }
             continue;
         }
-        Quad x{}, y{};
-        if (live) {
-            x = load4<VEC>(src, lo, dt);
-            y = load4<VEC>(src, hi, dt);
-        }
+        Quad u = live ? widen(x[n], dt) : Quad{}, v = live ? widen(y[n], dt) : Quad{};
         const uint16_t* w = is_q ? a.q_norm : a.k_norm;
         if (w) {
             float s2 = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s2 += x.v[i] * x.v[i] + y.v[i] * y.v[i];
+            for (int i = 0; i < 4; ++i) s2 += u.v[i] * u.v[i] + v.v[i] * v.v[i];
 #pragma unroll
             for (int off = LG / 2; off > 0; off >>= 1) s2 += __shfl_xor(s2, off, 64);
             const float r = 1.0f / sqrtf(s2 / static_cast<float>(D) + a.eps);
             if (live) {
-                const Quad wx = load4<VEC>(w, lo, dt), wy = load4<VEC>(w, hi, dt);
+                const Quad wx = widen(load4<VEC>(w, lo), dt), wy = widen(load4<VEC>(w, hi), dt);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x.v[i] *= r * wx.v[i], y.v[i] *= r * wy.v[i];
+                for (int i = 0; i < 4; ++i) u.v[i] *= r * wx.v[i], v.v[i] *= r * wy.v[i];
             }
         }
         if (half) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float u = x.v[i], v = y.v[i];
-                x.v[i] = u * cs[i] - v * sn[i];
-                y.v[i] = u * sn[i] + v * cs[i];
+                const float p = u.v[i], q = v.v[i];
+                u.v[i] = p * cs[i] - q * sn[i];
+                v.v[i] = p * sn[i] + q * cs[i];
             }
         } else if (turned) {
 #pragma unroll
             for (int i = 0; i < 4; i += 2) {
-                float u = x.v[i], v = x.v[i + 1];
-                x.v[i] = u * cs[i / 2] - v * sn[i / 2];
-                x.v[i + 1] = u * sn[i / 2] + v * cs[i / 2];
-                u = y.v[i], v = y.v[i + 1];
-                y.v[i] = u * cs[2 + i / 2] - v * sn[2 + i / 2];
-                y.v[i + 1] = u * sn[2 + i / 2] + v * cs[2 + i / 2];
+                float p = u.v[i], q = u.v[i + 1];
+                u.v[i] = p * cs[i / 2] - q * sn[i / 2];
+                u.v[i + 1] = p * sn[i / 2] + q * cs[i / 2];
+                p = v.v[i], q = v.v[i + 1];
+                v.v[i] = p * cs[2 + i / 2] - q * sn[2 + i / 2];
+                v.v[i + 1] = p * sn[2 + i / 2] + q * cs[2 + i / 2];
             }
         }
         if (live && (is_q || stored)) {
-            store4<VEC>(dst, lo, dt, x);
-            store4<VEC>(dst, hi, dt, y);
+            store4<VEC>(dst, lo, narrow(u, dt));
+            store4<VEC>(dst, hi, narrow(v, dt));
         }
     }
 }
 
-template <int LG>
-hipError_t launch(const AppendArgs& a, bool vec, hipStream_t st) {
-    const int heads = (a.q ? a.q_heads : 0) + 2 * a.cache.heads;
-    constexpr int per = 256 / LG;
-    const int blocks = (heads + per - 1) / per;
+template <int LG, int HP>
+hipError_t launch(const AppendArgs& a, bool vec, int blocks, hipStream_t st) {
     const dim3 grid(a.batch.tokens, blocks);
+    const int step = blocks * (256 / LG);
     if (vec)
-        hipLaunchKernelGGL((kv_append_kernel<LG, true>), grid, dim3(256), 0, st, a, blocks * per);
+        hipLaunchKernelGGL((kv_append_kernel<LG, true, HP>), grid, dim3(256), 0, st, a, step);
     else
-        hipLaunchKernelGGL((kv_append_kernel<LG, false>), grid, dim3(256), 0, st, a, blocks * per);
+        hipLaunchKernelGGL((kv_append_kernel<LG, false, HP>), grid, dim3(256), 0, st, a, step);
     return hipGetLastError();
+}
+
+// A lane group takes one head where workgroups are few (latency) and up to
+// four of a token's where they are many, which share its sines and its page.
+template <int LG>
+hipError_t choose(const AppendArgs& a, bool vec, hipStream_t st) {
+    constexpr int per = 256 / LG;
+    const int heads = (a.q ? a.q_heads : 0) + 2 * a.cache.heads;
+    const int blocks = (heads + per - 1) / per;
+    if (static_cast<long long>(a.batch.tokens) * blocks < 2048) return launch<LG, 1>(a, vec, blocks, st);
+    return launch<LG, 4>(a, vec, (heads + 4 * per - 1) / (4 * per), st);
 }
 
 bool even8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7) == 0; }
@@ -220,9 +237,9 @@ void rope_frequencies(int rot_dim, double base, int kind, double factor, double 
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t st) {
     const bool vec = even8(a.q) && even8(a.k) && even8(a.v) && even8(a.q_out) && even8(a.q_norm) && even8(a.k_norm) &&
                      a.q_stride % 4 == 0 && a.k_stride % 4 == 0 && a.v_stride % 4 == 0;
-    if (a.cache.dim <= 64) return launch<8>(a, vec, st);
-    if (a.cache.dim <= 128) return launch<16>(a, vec, st);
-    return launch<32>(a, vec, st);
+    if (a.cache.dim <= 64) return choose<8>(a, vec, st);
+    if (a.cache.dim <= 128) return choose<16>(a, vec, st);
+    return choose<32>(a, vec, st);
 }
 
 }  // namespace cl

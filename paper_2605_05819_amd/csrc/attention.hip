@@ -46,6 +46,9 @@ typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
+// Most splits of a call (the prefix's and a sequence's own together).
+constexpr int kMaxSplits = 128;
+
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -207,6 +210,17 @@ __device__ __forceinline__ void softmax_step(f32x4 (&s)[KB], uint32_t (&p)[KB][2
     }
 }
 
+// Four neighbouring results to out.
+__device__ __forceinline__ void store4(const AttnArgs& a, size_t at, f32x4 v) {
+    if (a.out_dtype == DT_FP32) {
+        *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = v;
+    } else {
+        const u32x2 u = a.out_dtype == DT_BF16 ? u32x2{pack2<true>(v[0], v[1]), pack2<true>(v[2], v[3])}
+                                               : u32x2{pack2<false>(v[0], v[1]), pack2<false>(v[2], v[3])};
+        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at) = u;
+    }
+}
+
 // Results of a row block: o[d] holds dims 16 d + 4 g + 0..3 of the lane's row.
 template <int ND>
 __device__ __forceinline__ void finish(const AttnArgs& a, const Plan& pl, int slot, const Row& r, int head, float sc,
@@ -226,16 +240,7 @@ __device__ __forceinline__ void finish(const AttnArgs& a, const Plan& pl, int sl
     const float inv = l != 0.f ? 1.0f / l : 0.f;
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
-        const size_t at = row * D + 16 * d + 4 * g;
-        f32x4 v = o[d] * inv;
-        if (l == 0.f) v = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (a.out_dtype == DT_FP32) {
-            *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = v;
-        } else {
-            const u32x2 u = a.out_dtype == DT_BF16 ? u32x2{pack2<true>(v[0], v[1]), pack2<true>(v[2], v[3])}
-                                                   : u32x2{pack2<false>(v[0], v[1]), pack2<false>(v[2], v[3])};
-            *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at) = u;
-        }
+        store4(a, row * D + 16 * d + 4 * g, l != 0.f ? o[d] * inv : f32x4{0.f, 0.f, 0.f, 0.f});
     }
     if (a.lse && g == 0) a.lse[row] = l != 0.f ? (m * sc + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
@@ -457,16 +462,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnA
             const float inv = ll != 0.f ? 1.0f / ll : 0.f;
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
-                const size_t to = rw * D + 16 * (wave * PER + j) + 4 * g4;
-                f32x4 v = r[j] * inv;
-                if (ll == 0.f) v = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (a.out_dtype == DT_FP32) {
-                    *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to) = v;
-                } else {
-                    const u32x2 u = a.out_dtype == DT_BF16 ? u32x2{pack2<true>(v[0], v[1]), pack2<true>(v[2], v[3])}
-                                                           : u32x2{pack2<false>(v[0], v[1]), pack2<false>(v[2], v[3])};
-                    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + to) = u;
-                }
+                store4(a, rw * D + 16 * (wave * PER + j) + 4 * g4, ll != 0.f ? r[j] * inv : f32x4{0.f, 0.f, 0.f, 0.f});
             }
             if (a.lse && g4 == 0 && wave == 0)
                 a.lse[rw] = ll != 0.f ? (mm * sc + __builtin_amdgcn_logf(ll)) * kLn2 : -INFINITY;
@@ -642,16 +638,28 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_tile_kernel(AttnArg
 
 // ------------------------------------------------------------- joining splits
 
-// One wave a row: sum_i w_i O_i / sum_i w_i l_i, w_i = 2^{m_i - max m}, over
-// the row's live splits in order.  Splits that hold no key of the row's
-// sequence were never written and are not read.
+// One workgroup a row: sum_i w_i O_i / sum_i w_i l_i, w_i = 2^{m_i - max m},
+// over the row's live splits.  Splits that hold no key of the row's sequence
+// were never written and are not used.  256 / (D / 4) splits are read at a
+// time, 16 bytes a lane; partial sums over a lane's splits meet in LDS, so the
+// order of the additions depends on the number of splits alone.
 template <int D>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, Plan pl) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int LANES = D / 4, AT = 256 / LANES;
+    __shared__ float weight[kMaxSplits];
+    __shared__ f32x4 sums[AT][LANES];
+    const int tid = threadIdx.x, lane = tid & 63;
     const size_t rows = static_cast<size_t>(a.batch.tokens) * a.q_heads;
-    const size_t row = static_cast<size_t>(blockIdx.x) * 4 + wave;
-    if (row >= rows) return;
+    const size_t row = blockIdx.x;
     const int t = static_cast<int>(row / a.q_heads);
+    const int total = pl.psplits + pl.splits;
+    // the statistics of every split, read ahead of the length that says which count
+    float2 st[kMaxSplits / 64];
+#pragma unroll
+    for (int j = 0; j < kMaxSplits / 64; ++j) {
+        st[j] = float2{-INFINITY, 0.f};
+        if (64 * j < total && 64 * j + lane < total) st[j] = pl.stat[(64 * j + lane) * rows + row];
+    }
     const int s = seq_of(a.batch, t);
     if (s < 0) return;
     const Seq q = load_seq(a.batch, s);
@@ -659,26 +667,43 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, Plan pl) {
     const int own = max(q.keys - a.batch.prefix_len, 0);
     const int live = pl.psplits + (own + pl.len - 1) / pl.len;
     float m = -INFINITY;
-    for (int i = lane; i < live; i += 64) m = fmaxf(m, pl.stat[i * rows + row].x);
+#pragma unroll
+    for (int j = 0; j < kMaxSplits / 64; ++j)
+        if (64 * j + lane < live) m = fmaxf(m, st[j].x);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
     const float base = m == -INFINITY ? 0.f : m;
-    constexpr int PER = D / 64;
-    float acc[PER], l = 0.f;
+    float l = 0.f;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) acc[j] = 0.f;
-    for (int i = 0; i < live; ++i) {
-        const float2 st = pl.stat[i * rows + row];
-        if (st.y == 0.f) continue;                 // no key seen there
-        const float w = __builtin_amdgcn_exp2f((st.x == -INFINITY ? base : st.x) - base);
-        l += w * st.y;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) acc[j] += w * pl.part[(i * rows + row) * D + PER * lane + j];
+    for (int j = 0; j < kMaxSplits / 64; ++j)
+        if (64 * j < live) {
+            // l = 0: no key seen there, whatever its sums hold
+            const bool used = 64 * j + lane < live && st[j].y != 0.f;
+            const float w = used ? __builtin_amdgcn_exp2f((st[j].x == -INFINITY ? base : st[j].x) - base) : 0.f;
+            if (tid < 64) weight[64 * j + lane] = w;
+            l += used ? w * st[j].y : 0.f;
+        }
+    l = wave_sum(l);
+    __syncthreads();
+    const int part = tid / LANES, at = tid % LANES;
+    const f32x4* from = reinterpret_cast<const f32x4*>(pl.part + row * D) + at;
+    const size_t step = rows * (D / 4);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = part; i < live; i += AT) {
+        const float w = weight[i];
+        const f32x4 v = from[i * step];
+        if (w != 0.f) acc += v * w;
     }
+    sums[part][at] = acc;
+    __syncthreads();
+    if (tid >= LANES) return;
+    acc = sums[0][at];
 #pragma unroll
-    for (int j = 0; j < PER; ++j)
-        store_out(a.out, row * D + PER * lane + j, l != 0.f ? acc[j] / l : 0.f, a.out_dtype);
-    if (a.lse && lane == 0) a.lse[row] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    for (int j = 1; j < AT; ++j) acc += sums[j][at];
+    const float inv = l != 0.f ? 1.0f / l : 0.f;
+    store4(a, row * D + 4 * at, l != 0.f ? acc * inv : f32x4{0.f, 0.f, 0.f, 0.f});
+    if (a.lse && tid == 0) a.lse[row] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b); }
@@ -693,6 +718,7 @@ void cut(long long units, int keys, int want, int least, int* splits, int* len) 
     int n = ceil_div(want, units);
     const int most = keys > least ? ceil_div(keys, least) : 1;
     if (n > most) n = most;
+    if (n > kMaxSplits / 2) n = kMaxSplits / 2;
     if (n < 1) n = 1;
     *len = keys > 0 ? ceil_div(ceil_div(keys, n), least) * least : least;
     *splits = keys > 0 ? ceil_div(keys, *len) : 1;
@@ -706,7 +732,7 @@ Plan make_plan(const KvCache& c, const KvBatch& b, int q_heads) {
     const int own = b.key_limit > b.prefix_len ? b.key_limit - b.prefix_len : 0;
     const bool stream = rows <= kStreamRows;
     p.blocks = stream ? 1 : ceil_div(rows, tile_rows(p.rows));
-    cut(static_cast<long long>(b.num_seqs) * c.heads * p.blocks, own, stream ? 1024 : 512, stream ? 128 : 512, &p.splits, &p.len);
+    cut(static_cast<long long>(b.num_seqs) * c.heads * p.blocks, own, stream ? 4096 : 512, stream ? 128 : 512, &p.splits, &p.len);
     if (b.prefix_len > 0) {
         const long long prows = static_cast<long long>(b.tokens) * group;
         const bool ps = prows <= kStreamRows;
@@ -760,7 +786,7 @@ hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t st) {
     const hipError_t e = part<D, BF>(a, p, 0, st);
     if (e != hipSuccess || p.direct) return e;
     const size_t rows = static_cast<size_t>(a.batch.tokens) * a.q_heads;
-    hipLaunchKernelGGL((attn_join_kernel<D>), dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, st, a, p);
+    hipLaunchKernelGGL((attn_join_kernel<D>), dim3(static_cast<unsigned>(rows)), dim3(256), 0, st, a, p);
     return hipGetLastError();
 }
 

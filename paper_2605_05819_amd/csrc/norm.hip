@@ -120,6 +120,7 @@ __global__ void residual_norm_kernel(NormArgs a) {
         for (int j = 0; j < VEC; ++j) x[i][j] = 0.f;
     }
     if (a.slots) {
+#pragma unroll 4
         for (int s = 0; s < a.slots; ++s) {
             const float w = a.slot_weights[static_cast<size_t>(t) * a.slots + s];
             const size_t base = (static_cast<size_t>(t) * a.slots + s) * a.d;

@@ -95,8 +95,8 @@ __global__ __launch_bounds__(256) void moe_route_kernel(RouteArgs a) {
 
     if (a.groups > 1) {
         // c of every expert to the wave's own LDS row (the key back as a float;
-        // a sum of two without a bias takes the scores), then lane g takes
-        // group g's best one or two
+        // a sum of two without a bias takes the scores), then the groups'
+        // best one or two are found
         const bool scores = a.group_best == 2 && !a.bias;
         float* c = group_choice[wave];
 #pragma unroll
@@ -109,17 +109,30 @@ __global__ __launch_bounds__(256) void moe_route_kernel(RouteArgs a) {
         }
         __builtin_amdgcn_wave_barrier();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        // `per` neighbouring lanes share a group and each scans every per-th of
+        // its values; the pairs of best ones meet by shuffles
         const int size = a.E / a.groups;
-        uint32_t gk = kTaken;
-        if (lane < a.groups) {
-            float b1 = -INFINITY, b2 = -INFINITY;
-            for (int j = 0; j < size; ++j) {
-                const float v = c[lane * size + j];
+        int per = 64;
+        while (per * a.groups > 64) per >>= 1;
+        const int mine = lane / per;
+        float b1 = -INFINITY, b2 = -INFINITY;
+        if (mine < a.groups) {
+#pragma unroll 4
+            for (int j = lane % per; j < size; j += per) {
+                const float v = c[mine * size + j];
                 b2 = fmaxf(b2, fminf(b1, v));
                 b1 = fmaxf(b1, v);
             }
-            gk = order_key(a.group_best == 2 ? b1 + b2 : b1);
         }
+        for (int off = 1; off < per; off <<= 1) {
+            const float o1 = __shfl_xor(b1, off, 64), o2 = __shfl_xor(b2, off, 64);
+            b2 = fmaxf(fminf(b1, o1), fmaxf(b2, o2));
+            b1 = fmaxf(b1, o1);
+        }
+        // lane g carries on for group g
+        b1 = __shfl(b1, min(lane * per, 63), 64);
+        b2 = __shfl(b2, min(lane * per, 63), 64);
+        uint32_t gk = lane < a.groups ? order_key(a.group_best == 2 ? b1 + b2 : b1) : kTaken;
         uint64_t open = 0;
         for (int j = 0; j < a.top_groups; ++j) {
             const uint32_t best = wave_max_u32(gk);
