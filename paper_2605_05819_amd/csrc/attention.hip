@@ -221,10 +221,10 @@ __device__ __forceinline__ void store4(const AttnArgs& a, size_t at, f32x4 v) {
     }
 }
 
-// Results of a row block: o[d] holds dims 16 d + 4 g + 0..3 of the lane's row.
+// Results of a row block (m in bits): o[d] holds dims 16 d + 4 g + 0..3 of the lane's row.
 template <int ND>
-__device__ __forceinline__ void finish(const AttnArgs& a, const Plan& pl, int slot, const Row& r, int head, float sc,
-                                       float m, float l, const f32x4 (&o)[ND]) {
+__device__ __forceinline__ void finish(const AttnArgs& a, const Plan& pl, int slot, const Row& r, int head, float m,
+                                       float l, const f32x4 (&o)[ND]) {
     if (r.token < 0) return;
     const int g = (threadIdx.x & 63) >> 4;
     constexpr int D = 16 * ND;
@@ -234,7 +234,7 @@ __device__ __forceinline__ void finish(const AttnArgs& a, const Plan& pl, int sl
         float* to = pl.part + at * D + 4 * g;
 #pragma unroll
         for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4*>(to + 16 * d) = o[d];
-        if (g == 0) pl.stat[at] = float2{m * sc, l};
+        if (g == 0) pl.stat[at] = float2{m, l};
         return;
     }
     const float inv = l != 0.f ? 1.0f / l : 0.f;
@@ -242,7 +242,7 @@ __device__ __forceinline__ void finish(const AttnArgs& a, const Plan& pl, int sl
     for (int d = 0; d < ND; ++d) {
         store4(a, row * D + 16 * d + 4 * g, l != 0.f ? o[d] * inv : f32x4{0.f, 0.f, 0.f, 0.f});
     }
-    if (a.lse && g == 0) a.lse[row] = l != 0.f ? (m * sc + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    if (a.lse && g == 0) a.lse[row] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // V in LDS, row-major with D values a row, 16-byte chunk c of row r at place
@@ -472,13 +472,56 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnA
 
 // ------------------------------------------------------------- many rows
 
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// What a lane copies for a key that is not there: zeros for one past the
+// segment, NaN for one whose page is outside the pool.
+__device__ const u32x4 absent[2] = {{0u, 0u, 0u, 0u}, {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu}};
+
+// 64 x 16 bytes from global memory straight to LDS at `to` (the same for the
+// whole wave), in lane order.  Written as assembly, which returns no register:
+// the compiler, which cannot tell the two halves of a double buffer apart,
+// would wait for these copies before every later LDS read.  copies_done()
+// waits for them.
+__device__ __forceinline__ void copy_to_lds(uint32_t to, const void* base, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base)
+                 : "memory", "m0");
+}
+__device__ __forceinline__ void copy_to_lds(uint32_t to, const void* from) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// A value that is the same for the whole wave, by a scalar load (read-only
+// memory during the kernel), which does not queue behind the copies.
+__device__ __forceinline__ int load_scalar(const int32_t* p) {
+    return *(const __attribute__((address_space(4))) int32_t*)p;
+}
+
+// Keys of a tile: 64, or 32 for 256-wide heads (two workgroups' tiles fit a CU).
+constexpr int tile_keys(int D) { return D > 128 ? 32 : 64; }
+
+// A step of the loop needs V of tile i and K of tile i + 1: the scores of the
+// next tile are multiplied while this one's become probabilities, so the
+// matrix and vector units of a SIMD both have work of one wave.  K and V have
+// two buffers each, filled by direct copies to LDS that are issued a step
+// ahead.  A maximum within 2^kSlack of the one in use leaves it in use
+// (probabilities up to 2^kSlack; every result divides by their sum), which
+// saves nearly all rescaling.
+constexpr float kSlack = 6.f;
+
 template <int D, bool BF, int NQ>
-__global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_tile_kernel(AttnArgs a, Plan pl, int prefix) {
-    constexpr int NS = D / 32, ND = D / 16, CH = D / 8, KT = 64;
+__global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnArgs a, Plan pl, int prefix) {
+    constexpr int NS = D / 32, ND = D / 16, CH = D / 8, KT = tile_keys(D), KB = KT / 16;
     constexpr int RW = 64 * NQ;                       // rows of a workgroup
-    constexpr int CP = KT * CH / 256;                 // 16-byte chunks of K (and of V) a thread moves
-    extern __shared__ __attribute__((aligned(16))) uint16_t tiles[];          // [2][K, V][KT * D]
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g4 = lane >> 4, col = lane & 15;
+    constexpr int WR = KT / 4;                        // keys of a tile that a wave copies
+    constexpr int CP = WR * CH / 64;                  // copies of 64 x 16 bytes a wave makes
+    constexpr int TILE = KT * D * 2;                  // bytes
+    extern __shared__ __attribute__((aligned(16))) unsigned char tiles[];     // K0, V0, K1, V1
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int g4 = lane >> 4, col = lane & 15;
     const int Hk = a.cache.heads, group = a.q_heads / Hk;
     const int head = blockIdx.x % Hk;
     int rest = blockIdx.x / Hk;
@@ -502,12 +545,13 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_tile_kernel(AttnArg
     for (int n = 0; n < NQ; ++n) {
         const int r = block * RW + wave * 16 * NQ + 16 * n + col;
         row[n] = r < nrows ? row_place(a, seg, r, group, prefix) : Row{-1, 0, 0};
+        row[n].hi = max(min(row[n].hi, end), row[n].lo);
         hidx[n] = head * group + r % group;
         load_q<D, BF>(a, row[n], hidx[n], q[n]);
         if (row[n].hi > row[n].lo) lo = min(lo, row[n].lo), hi = max(hi, row[n].hi);
         if (row[n].token >= 0) full_lo = max(full_lo, row[n].lo), full_hi = min(full_hi, row[n].hi);
     }
-    // the wave's bounds, then the workgroup's
+    // the wave's bounds (tiles it works on, tiles without a mask), then the workgroup's
 #pragma unroll
     for (int off = 1; off < 16; off <<= 1) {
         lo = min(lo, __shfl_xor(lo, off, 64));
@@ -518,122 +562,200 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_tile_kernel(AttnArg
     __shared__ int bounds[2][4];
     if (lane == 0) bounds[0][wave] = lo, bounds[1][wave] = hi;
     __syncthreads();
-    int wlo = lo, whi = hi;
+    const int wlo = __builtin_amdgcn_readfirstlane(lo), whi = __builtin_amdgcn_readfirstlane(hi);
 #pragma unroll
     for (int w = 0; w < 4; ++w) lo = min(lo, bounds[0][w]), hi = max(hi, bounds[1][w]);
-    lo = max(lo, begin) & ~(KT - 1);
-    hi = min(hi, end);
-    wlo = __builtin_amdgcn_readfirstlane(wlo);
-    whi = __builtin_amdgcn_readfirstlane(whi);
+    lo = __builtin_amdgcn_readfirstlane(max(lo, begin) & ~(KT - 1));
+    hi = __builtin_amdgcn_readfirstlane(hi);
     full_lo = __builtin_amdgcn_readfirstlane(full_lo);
-    full_hi = __builtin_amdgcn_readfirstlane(min(full_hi, end));
+    full_hi = __builtin_amdgcn_readfirstlane(full_hi);
     const float sc = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f;
 
-    float m[NQ], l[NQ];
-    f32x4 o[NQ][ND];
+    float m[NQ], mc[NQ], l[NQ];                       // mc = m sc, 0 before any key
+    f32x4 o[NQ][ND], s[NQ][KB];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         m[n] = -INFINITY;
-        l[n] = 0.f;
+        mc[n] = l[n] = 0.f;
 #pragma unroll
         for (int d = 0; d < ND; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    u32x4 kr[CP], vr[CP];
-    int where[CP];
-    const auto look = [&](int at) {
+    // Copies: the wave's keys WR wave .. of a tile; LDS place c ^ row & mask
+    // holds chunk c, so the lanes of a copy (places in order) ask for the
+    // chunks that belong there.
+    uint32_t from[CP];
 #pragma unroll
-        for (int i = 0; i < CP; ++i) {
-            const int key = at + (tid + 256 * i) / CH;
-            where[i] = key < seg.keys ? pool_row(a, seg, head, key) : -2;
-        }
+    for (int i = 0; i < CP; ++i) {
+        const int c = 64 * i + lane, r = c / CH;
+        from[i] = (r * D + 8 * (swz<D>(WR * wave + r, c % CH) % CH)) * 2;
+    }
+    const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte*)tiles));
+    const bool paged = (1 << a.cache.page_shift) >= WR;         // a wave's keys of a tile lie in one page
+    const auto page_of = [&](int at) {
+        const int key = at + WR * wave;
+        return paged && key < seg.keys ? load_scalar(seg.table + (key >> a.cache.page_shift)) : -1;
     };
-    const auto fetch = [&]() {
+    const auto copy = [&](const uint16_t* pool, uint32_t to, int at, int page) {
+        to += WR * wave * D * 2;
+        if (static_cast<unsigned>(page) < static_cast<unsigned>(a.cache.num_pages) && at + KT <= seg.keys) {
+            const int in = (at + WR * wave) & ((1 << a.cache.page_shift) - 1);
+            const uint16_t* src = pool + static_cast<size_t>(((page * Hk + head) << a.cache.page_shift) + in) * D;
 #pragma unroll
-        for (int i = 0; i < CP; ++i) {
-            const int r = where[i];
-            const size_t at = static_cast<size_t>(r < 0 ? 0 : r) * D + 8 * ((tid + 256 * i) % CH);
-            kr[i] = r == -1 ? kNaNs : kZeros;
-            vr[i] = kZeros;
-            if (r >= 0) {
-                kr[i] = *reinterpret_cast<const u32x4*>(a.cache.k + at);
-                vr[i] = *reinterpret_cast<const u32x4*>(a.cache.v + at);
+            for (int i = 0; i < CP; ++i) copy_to_lds(to + 1024 * i, src, from[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < CP; ++i) {
+                const int key = at + WR * wave + (64 * i + lane) / CH;
+                const int r = key < seg.keys ? pool_row(a, seg, head, key) : -2;
+                const char* src = r >= 0 ? reinterpret_cast<const char*>(pool + static_cast<size_t>(r) * D) +
+                                               from[i] % (2 * D)
+                                         : reinterpret_cast<const char*>(&absent[r + 2]);
+                copy_to_lds(to + 1024 * i, src);
             }
-        }
-    };
-    const auto stash = [&](int buf) {
-        uint16_t* kt = tiles + buf * 2 * KT * D;
-#pragma unroll
-        for (int i = 0; i < CP; ++i) {
-            const int c = tid + 256 * i;
-            const int to = 8 * swz<D>(c / CH, c % CH);
-            *reinterpret_cast<u32x4*>(kt + to) = kr[i];
-            *reinterpret_cast<u32x4*>(kt + KT * D + to) = vr[i];
         }
     };
 
-    if (lo < hi) {
-        look(lo);
-        fetch();
-        look(lo + KT);
-        stash(0);
-        int buf = 0;
-        for (int at = lo; at < hi; at += KT, buf ^= 1) {
-            __syncthreads();
-            const bool more = at + KT < hi;
-            if (more) {
-                fetch();
-                look(at + 2 * KT);
+    // LDS addresses of the wave's reads: of K, row 16 b + col, chunk 4 i + g4; of
+    // V^T, rows 32 kk + 16 half + 4 g4 + (col >> 2), columns 16 d + 4 (col & 3)
+    uint32_t kat[NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) kat[i] = 16 * swz<D>(col, 4 * i + g4);
+    const int vrow = 4 * g4 + (col >> 2);
+    const uint32_t vat = 16 * swz<D>(vrow, (col & 3) >> 1) + 8 * (col & 1);
+
+    const auto scores = [&](uint32_t kt) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) s[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                const u32x4 kf = *(const lds_u32x4*)((const lds_byte*)(uintptr_t)(kt + kat[i]) + 32 * D * b);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) s[n][b] = mma<BF>(kf, q[n][i], s[n][b]);
             }
-            const uint16_t* kt = tiles + buf * 2 * KT * D;
-            const uint16_t* vt = kt + KT * D;
-            if (at < whi && at + KT > wlo) {
-                f32x4 s[NQ][4];
+        }
+    };
+    // maxima, masks and, where one rose past the slack, the new reference
+    const auto settle = [&](int at) {
+        if (at < full_lo || at + KT > full_hi) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int b = 0; b < KB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        // lo <= key < hi
+                        const unsigned past = at + 16 * b + 4 * g4 + i - row[n].lo;
+                        if (past >= static_cast<unsigned>(row[n].hi - row[n].lo)) s[n][b][i] = -INFINITY;
+                    }
+        }
+        float mx[NQ];
+        bool rose = false;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            mx[n] = s[n][0][0];
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mx[n] = fmaxf(mx[n], s[n][b][i]);
+            mx[n] = row_max(mx[n]);
+            rose |= m[n] == -INFINITY ? mx[n] != -INFINITY : mx[n] * sc > mc[n] + kSlack;
+        }
+        if (__ballot(rose)) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                mx[n] = fmaxf(mx[n], m[n]);
+                const float now = mx[n] == -INFINITY ? 0.f : mx[n] * sc;
+                const float c = m[n] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mc[n] - now);
+                m[n] = mx[n];
+                mc[n] = now;
+                l[n] *= c;
+#pragma unroll
+                for (int d = 0; d < ND; ++d) o[n][d] *= c;
+            }
+        }
+    };
+    // this tile's scores to probabilities, block by block, each block's place
+    // taken by the next tile's scores as it becomes free (behind the last tile
+    // they are of whatever the buffer holds, and nothing uses them)
+    const auto turn = [&](uint32_t (&p)[NQ][KB][2], uint32_t kt) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+            f32x4 to[NQ];
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) to[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                const u32x4 kf = *(const lds_u32x4*)((const lds_byte*)(uintptr_t)(kt + kat[i]) + 32 * D * b);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) to[n] = mma<BF>(kf, q[n][i], to[n]);
+            }
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[n][b][i] = __builtin_amdgcn_exp2f(fmaf(s[n][b][i], sc, -mc[n]));
+                    l[n] += s[n][b][i];
+                }
+                p[n][b][0] = pack2<BF>(s[n][b][0], s[n][b][1]);
+                p[n][b][1] = pack2<BF>(s[n][b][2], s[n][b][3]);
+                s[n][b] = to[n];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    const auto values = [&](const uint32_t (&p)[NQ][KB][2], uint32_t vt) {
+#pragma unroll
+        for (int kk = 0; kk < KB / 2; ++kk)
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                lds_byte* at = (lds_byte*)(uintptr_t)(vt + (vat ^ (32 * d))) + 64 * D * kk;
+                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+                const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 32 * D));
+                const u32x2 ux = __builtin_bit_cast(u32x2, x), uy = __builtin_bit_cast(u32x2, y);
+                const u32x4 vf = {ux[0], ux[1], uy[0], uy[1]};
 #pragma unroll
                 for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) s[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int b = 0; b < 4; ++b)
-#pragma unroll
-                    for (int i = 0; i < NS; ++i) {
-                        const u32x4 kf = *reinterpret_cast<const u32x4*>(kt + 8 * swz<D>(16 * b + col, 4 * i + g4));
-#pragma unroll
-                        for (int n = 0; n < NQ; ++n) s[n][b] = mma<BF>(kf, q[n][i], s[n][b]);
-                    }
-                const bool masked = at < full_lo || at + KT > full_hi;
-                uint32_t p[NQ][4][2];
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) {
-                    if (masked) {
-                        const int from = row[n].lo, to = min(row[n].hi, end);
-#pragma unroll
-                        for (int b = 0; b < 4; ++b)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const int key = at + 16 * b + 4 * g4 + i;
-                                if (key < from || key >= to) s[n][b][i] = -INFINITY;
-                            }
-                    }
-                    softmax_step<4, ND, BF>(s[n], p[n], sc, m[n], l[n], o[n]);
-                }
-#pragma unroll
-                for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-                    for (int d = 0; d < ND; ++d) {
-                        const u32x4 vf = load_vt<D>(vt, kk, d);
-#pragma unroll
-                        for (int n = 0; n < NQ; ++n)
-                            o[n][d] = mma<BF>(vf, u32x4{p[n][2 * kk][0], p[n][2 * kk][1], p[n][2 * kk + 1][0], p[n][2 * kk + 1][1]},
-                                              o[n][d]);
-                    }
+                    o[n][d] = mma<BF>(vf, u32x4{p[n][2 * kk][0], p[n][2 * kk][1], p[n][2 * kk + 1][0], p[n][2 * kk + 1][1]},
+                                      o[n][d]);
             }
-            if (more) stash(buf ^ 1);
+    };
+
+    if (lo < hi) {
+        const auto mine = [&](int at) { return at < whi && at + KT > wlo; };
+        int page_v = page_of(lo), page_k = page_of(lo + KT);
+        copy(a.cache.k, base, lo, page_v);
+        copies_done();
+        __syncthreads();
+        copy(a.cache.v, base + TILE, lo, page_v);
+        if (lo + KT < hi) copy(a.cache.k, base + 2 * TILE, lo + KT, page_k);
+        page_v = page_k;
+        page_k = page_of(lo + 2 * KT);
+        if (mine(lo)) scores(base);
+        int buf = 0;
+        for (int at = lo; at < hi; at += KT, buf ^= 1) {
+            copies_done();
+            __syncthreads();              // V of this tile and K of the next are there, their other buffers free
+            if (at + KT < hi) copy(a.cache.v, base + (2 * (buf ^ 1) + 1) * TILE, at + KT, page_v);
+            if (at + 2 * KT < hi) copy(a.cache.k, base + 2 * buf * TILE, at + 2 * KT, page_k);
+            page_v = page_k;
+            page_k = page_of(at + 3 * KT);
+            const uint32_t kt = base + 2 * (buf ^ 1) * TILE, vt = base + (2 * buf + 1) * TILE;
+            if (mine(at)) {
+                settle(at);
+                uint32_t p[NQ][KB][2];
+                turn(p, kt);
+                values(p, vt);
+            } else if (mine(at + KT)) {
+                scores(kt);
+            }
         }
     }
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
-        finish<ND>(a, pl, prefix ? split : pl.psplits + split, row[n], hidx[n], sc, m[n], row_sum(l[n]), o[n]);
+        finish<ND>(a, pl, prefix ? split : pl.psplits + split, row[n], hidx[n], m[n] == -INFINITY ? -INFINITY : mc[n], row_sum(l[n]), o[n]);
 }
 
 // ------------------------------------------------------------- joining splits
@@ -748,7 +870,7 @@ size_t up256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 
 template <int D, bool BF, int NQ>
 hipError_t tile(const AttnArgs& a, const Plan& p, int prefix, long long grid, hipStream_t st) {
-    constexpr int bytes = 2 * 2 * 64 * D * 2;
+    constexpr int bytes = 4 * tile_keys(D) * D * 2;
     if (bytes > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_tile_kernel<D, BF, NQ>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
