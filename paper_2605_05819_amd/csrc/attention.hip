@@ -103,6 +103,8 @@ struct Plan {
     int blocks;            // row blocks of a unit
     int splits, len;       // of a sequence's own keys: splits of `len` keys
     int pblocks, psplits, plen;      // of the shared prefix, whose unit has every token's rows
+    int pgrid;             // workgroups of the prefix, ahead of the others
+    int paired;            // order of the row blocks (see attn_tile)
     int direct;            // one split and no prefix: results go straight to out
     float* part;           // [psplits + splits][tokens * q_heads][dim], unnormalised
     float2* stat;          // [psplits + splits][tokens * q_heads]: m (in bits), l
@@ -131,9 +133,10 @@ __device__ __forceinline__ Row clip(const AttnArgs& a, int token, int pos, int k
     return r;
 }
 
-__device__ __forceinline__ Row row_place(const AttnArgs& a, const Segment& g, int row, int group, bool prefix) {
+template <bool PREFIX>
+__device__ __forceinline__ Row row_place(const AttnArgs& a, const Segment& g, int row, int group) {
     const int i = row / group;
-    if (!prefix) {
+    if constexpr (!PREFIX) {
         if (i >= g.seq.count) return Row{-1, 0, 0};
         return clip(a, g.seq.start + i, g.seq.keys - g.seq.count + i, g.seq.keys, g.base, g.keys);
     }
@@ -288,20 +291,34 @@ __device__ __forceinline__ Segment prefix_segment(const AttnArgs& a) {
 
 // ------------------------------------------------------------- few rows
 
-template <int D, bool BF, int NQ>
-__global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnArgs a, Plan pl, int prefix) {
+// Bytes of LDS: every wave's V, then the statistics.
+constexpr int stream_lds(int D, int NQ) { return 256 * D + 512 * NQ; }
+
+template <int D, bool BF, int NQ, bool PREFIX>
+__device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, int id, unsigned char* lds) {
     constexpr int NS = D / 32, ND = D / 16, CH = D / 8;
-    __shared__ __attribute__((aligned(16))) uint16_t vbuf[4][32 * D];
-    __shared__ float2 stat[4][16 * NQ];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g4 = lane >> 4, col = lane & 15;
+    uint16_t* const vl = reinterpret_cast<uint16_t*>(lds) + wave * 32 * D;
+    float2(*stat)[16 * NQ] = reinterpret_cast<float2(*)[16 * NQ]>(lds + 256 * D);
     const int Hk = a.cache.heads, group = a.q_heads / Hk;
-    const int head = blockIdx.x % Hk;
-    int rest = blockIdx.x / Hk;
-    const int splits = prefix ? pl.psplits : pl.splits, len = prefix ? pl.plen : pl.len;
+    const int head = id % Hk;
+    int rest = id / Hk;
+    const int splits = PREFIX ? pl.psplits : pl.splits, len = PREFIX ? pl.plen : pl.len;
     const int split = rest % splits;
     rest /= splits;
-    const Segment seg = prefix ? prefix_segment(a) : own_segment(a, rest);
-    const int begin = split * len, end = min(begin + len, seg.keys);
+    const int begin = split * len;
+    // the first step's pages, looked up beside the lengths (entries are in
+    // bounds up to the host's limit; what stands behind a length is not used)
+    int first = -2;
+    if (a.window == 0) {
+        const Segment any = PREFIX ? prefix_segment(a)
+                                   : Segment{a.batch.page_table + static_cast<size_t>(rest) * a.batch.table_width,
+                                             a.batch.key_limit - a.batch.prefix_len, 0, Seq{0, 0, 0}};
+        const int key = begin + 32 * wave + (lane & 31);
+        if (key < any.keys) first = pool_row(a, any, head, key);
+    }
+    const Segment seg = PREFIX ? prefix_segment(a) : own_segment(a, rest);
+    const int end = min(begin + len, seg.keys);
     if (begin >= end && !pl.direct) return;
 
     Row row[NQ];
@@ -311,7 +328,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnA
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         const int r = 16 * n + col;
-        row[n] = r < (prefix ? a.batch.tokens * group : pl.rows) ? row_place(a, seg, r, group, prefix) : Row{-1, 0, 0};
+        row[n] = r < (PREFIX ? a.batch.tokens * group : pl.rows) ? row_place<PREFIX>(a, seg, r, group) : Row{-1, 0, 0};
         hidx[n] = head * group + r % group;
         load_q<D, BF>(a, row[n], hidx[n], q[n]);
         if (row[n].hi > row[n].lo) lo = min(lo, row[n].lo), hi = max(hi, row[n].hi);
@@ -337,7 +354,6 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnA
         for (int d = 0; d < ND; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    uint16_t* vl = vbuf[wave];
     u32x4 kr[2][NS], vr[CH / 2];
     constexpr int VR = CH / 2;                // 32 rows x CH chunks over 64 lanes
     // lane l looks up key l of a step; the lanes that load a row ask for it
@@ -364,7 +380,9 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnA
 
     int at = lo + 32 * wave;
     if (at < hi) {
-        fetch(look(at));
+        // without a window the first step is the one looked up above
+        if (a.window == 0) fetch(at + (lane & 31) < seg.keys ? first : -2);
+        else fetch(look(at));
         int next = look(at + 128);
         for (; at < hi; at += 128) {
             f32x4 s[NQ][2];
@@ -418,8 +436,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnA
         if (g4 == 0) stat[wave][16 * n + col] = float2{m[n], l[n]};
     }
     __syncthreads();
-    float* sum = reinterpret_cast<float*>(&vbuf[0][0]);
-    static_assert(sizeof(vbuf) >= 4 * 16 * D * sizeof(float), "one row block of every wave");
+    float* const sum = reinterpret_cast<float*>(lds);     // one row block of every wave
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         float mm = -INFINITY;
@@ -451,7 +468,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_stream_kernel(AttnA
         }
         if (row[n].token < 0) continue;
         const size_t rw = static_cast<size_t>(row[n].token) * a.q_heads + hidx[n];
-        const int slot = prefix ? split : pl.psplits + split;
+        const int slot = PREFIX ? split : pl.psplits + split;
         if (!pl.direct) {
             const size_t at2 = static_cast<size_t>(slot) * a.batch.tokens * a.q_heads + rw;
 #pragma unroll
@@ -512,27 +529,36 @@ constexpr int tile_keys(int D) { return D > 128 ? 32 : 64; }
 // saves nearly all rescaling.
 constexpr float kSlack = 6.f;
 
-template <int D, bool BF, int NQ>
-__global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnArgs a, Plan pl, int prefix) {
+//
+// Blocks are numbered from the last row down: causal rows see more keys the
+// later they stand, and the longest should start first.  Where all workgroups
+// are resident at once (`paired`) the lower half counts up again instead: the
+// second workgroup on a CU is then short where the first is long (2048-token
+// prompt 57.5 -> 54.9 us).  Sequences vary slowest: workgroups go to the shader
+// engines in turn, so a sequence without rows at every fourth place would leave
+// an engine idle (ragged prompts 858 -> 2122 us that way round).
+constexpr int tile_lds(int D) { return 4 * tile_keys(D) * D * 2 + 64; }
+
+template <int D, bool BF, int NQ, bool PREFIX>
+__device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int id, unsigned char* lds) {
     constexpr int NS = D / 32, ND = D / 16, CH = D / 8, KT = tile_keys(D), KB = KT / 16;
     constexpr int RW = 64 * NQ;                       // rows of a workgroup
     constexpr int WR = KT / 4;                        // keys of a tile that a wave copies
     constexpr int CP = WR * CH / 64;                  // copies of 64 x 16 bytes a wave makes
     constexpr int TILE = KT * D * 2;                  // bytes
-    extern __shared__ __attribute__((aligned(16))) unsigned char tiles[];     // K0, V0, K1, V1
+    unsigned char* const tiles = lds;                 // K0, V0, K1, V1
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g4 = lane >> 4, col = lane & 15;
     const int Hk = a.cache.heads, group = a.q_heads / Hk;
-    const int head = blockIdx.x % Hk;
-    int rest = blockIdx.x / Hk;
-    const int splits = prefix ? pl.psplits : pl.splits, len = prefix ? pl.plen : pl.len;
+    const int head = id % Hk;
+    int rest = id / Hk;
+    const int splits = PREFIX ? pl.psplits : pl.splits, len = PREFIX ? pl.plen : pl.len;
     const int split = rest % splits;
     rest /= splits;
-    const int blocks = prefix ? pl.pblocks : pl.blocks;
-    const int block = blocks - 1 - rest % blocks;     // causal rows see more keys the later they stand: longest first
-    rest /= blocks;
-    const Segment seg = prefix ? prefix_segment(a) : own_segment(a, rest);
-    const int nrows = (prefix ? a.batch.tokens : min(seg.seq.count, a.batch.q_len)) * group;
+    const int blocks = PREFIX ? pl.pblocks : pl.blocks, upper = (blocks + 1) / 2, nth = rest % blocks;
+    const int block = pl.paired && nth >= upper ? nth - upper : blocks - 1 - nth;
+    const Segment seg = PREFIX ? prefix_segment(a) : own_segment(a, rest / blocks);
+    const int nrows = (PREFIX ? a.batch.tokens : min(seg.seq.count, a.batch.q_len)) * group;
     if (block * RW >= nrows) return;
     const int begin = split * len, end = min(begin + len, seg.keys);
     if (begin >= end && !pl.direct) return;
@@ -544,7 +570,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnArgs a, Plan pl, 
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         const int r = block * RW + wave * 16 * NQ + 16 * n + col;
-        row[n] = r < nrows ? row_place(a, seg, r, group, prefix) : Row{-1, 0, 0};
+        row[n] = r < nrows ? row_place<PREFIX>(a, seg, r, group) : Row{-1, 0, 0};
         row[n].hi = max(min(row[n].hi, end), row[n].lo);
         hidx[n] = head * group + r % group;
         load_q<D, BF>(a, row[n], hidx[n], q[n]);
@@ -559,7 +585,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnArgs a, Plan pl, 
         full_lo = max(full_lo, __shfl_xor(full_lo, off, 64));
         full_hi = min(full_hi, __shfl_xor(full_hi, off, 64));
     }
-    __shared__ int bounds[2][4];
+    int(*bounds)[4] = reinterpret_cast<int(*)[4]>(lds + 4 * TILE);
     if (lane == 0) bounds[0][wave] = lo, bounds[1][wave] = hi;
     __syncthreads();
     const int wlo = __builtin_amdgcn_readfirstlane(lo), whi = __builtin_amdgcn_readfirstlane(hi);
@@ -703,7 +729,6 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnArgs a, Plan pl, 
                 p[n][b][1] = pack2<BF>(s[n][b][2], s[n][b][3]);
                 s[n][b] = to[n];
             }
-            __builtin_amdgcn_sched_barrier(0);
         }
     };
     const auto values = [&](const uint32_t (&p)[NQ][KB][2], uint32_t vt) {
@@ -755,7 +780,38 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnArgs a, Plan pl, 
     }
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
-        finish<ND>(a, pl, prefix ? split : pl.psplits + split, row[n], hidx[n], m[n] == -INFINITY ? -INFINITY : mc[n], row_sum(l[n]), o[n]);
+        finish<ND>(a, pl, PREFIX ? split : pl.psplits + split, row[n], hidx[n], m[n] == -INFINITY ? -INFINITY : mc[n], row_sum(l[n]), o[n]);
+}
+
+// ------------------------------------------------------------- one launch
+
+// How a segment's units are worked: not at all, streamed (16 or 32 rows) or by
+// tiles (64 or 128 rows a workgroup).
+enum { NONE = 0, S1 = 1, S2 = 2, T1 = 3, T2 = 4 };
+
+constexpr int lds_bytes(int D, int kind) {
+    return kind == NONE ? 0 : kind <= S2 ? stream_lds(D, kind) : tile_lds(D);
+}
+
+// The prefix's and the sequences' own workgroups side by side, so the tiles of
+// the one and the streams of the other share the CUs.  Streams of 16 rows fit
+// three workgroups on a CU (168 registers), streams of 256-wide heads one (367;
+// held to 256 they spill: 16 sequences of 200 to 8000 keys 124 against 96 us),
+// the rest two.
+template <int D, bool BF, int P, int O>
+__global__ __launch_bounds__(256, O <= S2 && D > 128 ? 1 : P == NONE && O == S1 ? 3 : 2) void attn_kernel(
+    AttnArgs a, Plan pl) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int id = static_cast<int>(blockIdx.x);
+    if constexpr (P != NONE) {
+        if (id < pl.pgrid) {
+            if constexpr (P <= S2) attn_stream<D, BF, P, true>(a, pl, id, lds);
+            else attn_tile<D, BF, P - S2, true>(a, pl, id, lds);
+            return;
+        }
+    }
+    if constexpr (O <= S2) attn_stream<D, BF, O, false>(a, pl, id - pl.pgrid, lds);
+    else attn_tile<D, BF, O - S2, false>(a, pl, id - pl.pgrid, lds);
 }
 
 // ------------------------------------------------------------- joining splits
@@ -830,9 +886,10 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, Plan pl) {
 
 int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b); }
 
-// Rows up to which a unit streams, and rows of a tile workgroup.
-constexpr int kStreamRows = 32;
-int tile_rows(int rows) { return rows <= 64 ? 64 : 128; }
+// Rows up to which a unit streams, and rows of a tile workgroup.  Heads of 256
+// keep to one row block a wave: two do not fit 256 registers beside the sums.
+int stream_rows(int dim) { return dim > 128 ? 16 : 32; }
+int tile_rows(long long rows, int dim) { return rows <= 64 || dim > 128 ? 64 : 128; }
 
 // Splits of `keys` keys for `units` workgroups without splitting: enough to
 // give the chip `want` workgroups, none under `least` keys.
@@ -846,21 +903,27 @@ void cut(long long units, int keys, int want, int least, int* splits, int* len) 
     *splits = keys > 0 ? ceil_div(keys, *len) : 1;
 }
 
+int kind_of(long long rows, int dim) {
+    return rows <= 16 ? S1 : rows <= stream_rows(dim) ? S2 : tile_rows(rows, dim) == 64 ? T1 : T2;
+}
+
 Plan make_plan(const KvCache& c, const KvBatch& b, int q_heads) {
     Plan p{};
     const int group = q_heads / c.heads;
     const long long rows = static_cast<long long>(b.q_len) * group;
     p.rows = static_cast<int>(rows);
     const int own = b.key_limit > b.prefix_len ? b.key_limit - b.prefix_len : 0;
-    const bool stream = rows <= kStreamRows;
-    p.blocks = stream ? 1 : ceil_div(rows, tile_rows(p.rows));
-    cut(static_cast<long long>(b.num_seqs) * c.heads * p.blocks, own, stream ? 4096 : 512, stream ? 128 : 512, &p.splits, &p.len);
-    if (b.prefix_len > 0) {
+    const bool stream = rows <= stream_rows(c.dim);
+    p.blocks = stream ? 1 : ceil_div(rows, tile_rows(rows, c.dim));
+    const long long units = static_cast<long long>(b.num_seqs) * c.heads * p.blocks;
+    cut(units, own, stream ? 4096 : 512, stream ? 128 : 512, &p.splits, &p.len);
+    p.paired = units * p.splits <= 512;
+    const int keys = b.prefix_len < b.key_limit ? b.prefix_len : b.key_limit;
+    if (keys > 0) {
         const long long prows = static_cast<long long>(b.tokens) * group;
-        const bool ps = prows <= kStreamRows;
-        p.pblocks = ps ? 1 : ceil_div(prows, tile_rows(static_cast<int>(prows < 1000 ? prows : 1000)));
-        const int keys = b.prefix_len < b.key_limit ? b.prefix_len : b.key_limit;
-        if (keys > 0) cut(static_cast<long long>(c.heads) * p.pblocks, keys, ps ? 1024 : 512, ps ? 128 : 256, &p.psplits, &p.plen);
+        const bool ps = prows <= stream_rows(c.dim);
+        p.pblocks = ps ? 1 : ceil_div(prows, c.dim > 128 ? 64 : 128);
+        cut(static_cast<long long>(c.heads) * p.pblocks, keys, ps ? 1024 : 256, ps ? 128 : 256, &p.psplits, &p.plen);
     }
     p.direct = p.splits == 1 && p.psplits == 0;
     return p;
@@ -868,44 +931,48 @@ Plan make_plan(const KvCache& c, const KvBatch& b, int q_heads) {
 
 size_t up256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 
-template <int D, bool BF, int NQ>
-hipError_t tile(const AttnArgs& a, const Plan& p, int prefix, long long grid, hipStream_t st) {
-    constexpr int bytes = 4 * tile_keys(D) * D * 2;
+template <int D, bool BF, int P, int O>
+hipError_t launch(const AttnArgs& a, Plan p, hipStream_t st) {
+    const long long pgrid = static_cast<long long>(a.cache.heads) * p.psplits * p.pblocks;
+    const long long grid = pgrid + static_cast<long long>(a.cache.heads) * p.splits * p.blocks * a.batch.num_seqs;
+    if (grid > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    p.pgrid = static_cast<int>(pgrid);
+    constexpr int bytes = lds_bytes(D, P) > lds_bytes(D, O) ? lds_bytes(D, P) : lds_bytes(D, O);
     if (bytes > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_tile_kernel<D, BF, NQ>),
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_kernel<D, BF, P, O>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((attn_tile_kernel<D, BF, NQ>), dim3(static_cast<unsigned>(grid)), dim3(256), bytes, st, a, p, prefix);
+    hipLaunchKernelGGL((attn_kernel<D, BF, P, O>), dim3(static_cast<unsigned>(grid)), dim3(256), bytes, st, a, p);
     return hipGetLastError();
 }
 
-template <int D, bool BF>
-hipError_t part(const AttnArgs& a, const Plan& p, int prefix, hipStream_t st) {
-    const long long rows = prefix ? static_cast<long long>(a.batch.tokens) * (a.q_heads / a.cache.heads) : p.rows;
-    const long long grid = static_cast<long long>(a.cache.heads) *
-                           (prefix ? static_cast<long long>(p.psplits) * p.pblocks
-                                   : static_cast<long long>(p.splits) * p.blocks * a.batch.num_seqs);
-    if (grid > 0x7fffffffll) return hipErrorInvalidConfiguration;
-    if (rows <= 16) {
-        hipLaunchKernelGGL((attn_stream_kernel<D, BF, 1>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, a, p, prefix);
-        return hipGetLastError();
-    }
-    if (rows <= kStreamRows) {
-        hipLaunchKernelGGL((attn_stream_kernel<D, BF, 2>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, a, p, prefix);
-        return hipGetLastError();
-    }
-    if (rows <= 64) return tile<D, BF, 1>(a, p, prefix, grid, st);
-    return tile<D, BF, 2>(a, p, prefix, grid, st);
-}
-
+// The prefix's unit has at least as many rows as a sequence's, so these
+// combinations cover every call (a prefix of 33 to 64 rows takes 128-row
+// tiles, a streamed one of 17 to 32 rows streams the sequences' likewise).
 template <int D, bool BF>
 hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t st) {
-    if (p.psplits) {
-        const hipError_t e = part<D, BF>(a, p, 1, st);
-        if (e != hipSuccess) return e;
+    const int own = kind_of(p.rows, D);
+    const int pre = p.psplits ? kind_of(static_cast<long long>(a.batch.tokens) * (a.q_heads / a.cache.heads), D) : NONE;
+    hipError_t e;
+    if constexpr (D > 128) {
+        e = pre == NONE ? own == S1 ? launch<D, BF, NONE, S1>(a, p, st) : launch<D, BF, NONE, T1>(a, p, st)
+            : pre == S1 ? launch<D, BF, S1, S1>(a, p, st)
+            : own == S1 ? launch<D, BF, T1, S1>(a, p, st)
+                        : launch<D, BF, T1, T1>(a, p, st);
+    } else if (pre == NONE) {
+        e = own == S1   ? launch<D, BF, NONE, S1>(a, p, st)
+            : own == S2 ? launch<D, BF, NONE, S2>(a, p, st)
+            : own == T1 ? launch<D, BF, NONE, T1>(a, p, st)
+                        : launch<D, BF, NONE, T2>(a, p, st);
+    } else {
+        e = pre == S1   ? launch<D, BF, S1, S1>(a, p, st)
+            : pre == S2 ? launch<D, BF, S2, S2>(a, p, st)
+            : own == S1 ? launch<D, BF, T2, S1>(a, p, st)
+            : own == S2 ? launch<D, BF, T2, S2>(a, p, st)
+            : own == T1 ? launch<D, BF, T2, T1>(a, p, st)
+                        : launch<D, BF, T2, T2>(a, p, st);
     }
-    const hipError_t e = part<D, BF>(a, p, 0, st);
     if (e != hipSuccess || p.direct) return e;
     const size_t rows = static_cast<size_t>(a.batch.tokens) * a.q_heads;
     hipLaunchKernelGGL((attn_join_kernel<D>), dim3(static_cast<unsigned>(rows)), dim3(256), 0, st, a, p);
