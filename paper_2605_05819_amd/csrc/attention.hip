@@ -97,7 +97,11 @@ __device__ __forceinline__ float row_sum(float v) {
     return b[0] + b[1];
 }
 
-// How a call is cut; every field follows from the host's sizes alone.
+// How a call is cut; every field follows from the host's sizes alone.  A
+// sequence's unit has splits | 1 places in the grid: workgroups go to the four
+// shader engines of an XCD in turn, and where sequences end early an even
+// period would leave the same engines without work each time (16 sequences of
+// 1 to 8192 keys 25.1 -> 23.6 us).
 struct Plan {
     int rows;              // most rows of a unit
     int blocks;            // row blocks of a unit
@@ -304,8 +308,10 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
     const int head = id % Hk;
     int rest = id / Hk;
     const int splits = PREFIX ? pl.psplits : pl.splits, len = PREFIX ? pl.plen : pl.len;
-    const int split = rest % splits;
-    rest /= splits;
+    const int places = PREFIX ? splits : splits | 1;  // see Plan
+    const int split = rest % places;
+    rest /= places;
+    if (split >= splits) return;
     const int begin = split * len;
     // the first step's pages, looked up beside the lengths (entries are in
     // bounds up to the host's limit; what stands behind a length is not used)
@@ -553,8 +559,10 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
     const int head = id % Hk;
     int rest = id / Hk;
     const int splits = PREFIX ? pl.psplits : pl.splits, len = PREFIX ? pl.plen : pl.len;
-    const int split = rest % splits;
-    rest /= splits;
+    const int places = PREFIX ? splits : splits | 1;
+    const int split = rest % places;
+    rest /= places;
+    if (split >= splits) return;
     const int blocks = PREFIX ? pl.pblocks : pl.blocks, upper = (blocks + 1) / 2, nth = rest % blocks;
     const int block = pl.paired && nth >= upper ? nth - upper : blocks - 1 - nth;
     const Segment seg = PREFIX ? prefix_segment(a) : own_segment(a, rest / blocks);
@@ -916,7 +924,17 @@ Plan make_plan(const KvCache& c, const KvBatch& b, int q_heads) {
     const bool stream = rows <= stream_rows(c.dim);
     p.blocks = stream ? 1 : ceil_div(rows, tile_rows(rows, c.dim));
     const long long units = static_cast<long long>(b.num_seqs) * c.heads * p.blocks;
-    cut(units, own, stream ? 4096 : 512, stream ? 128 : 512, &p.splits, &p.len);
+    // Streams: splits of at least 128 keys, one step of each wave, while units
+    // are few; 256 from 256 units on (64 under a prefix 38.8 -> 37.1 us, where
+    // one sequence of 2049 keys would take 12.2 for 10.7), and then one split
+    // without a join up to 512 keys (64 sequences of 10 to 300 keys 14.8 -> 11.0
+    // us; one of 500 would take 11.8 for 9.9).  4096 workgroups in all where
+    // three fit a CU (16 ragged sequences 23.6 us, 26.5 with 2048), else 2048
+    // (256-wide heads 92 -> 81 us, 24 rows a unit 52 -> 48).
+    const bool many = units >= 256;
+    const int least = !many ? 128 : own <= 512 && b.prefix_len == 0 ? 512 : 256;
+    const int want = rows <= 16 && c.dim <= 128 ? 4096 : 2048;
+    cut(units, own, stream ? want : 512, stream ? least : 512, &p.splits, &p.len);
     p.paired = units * p.splits <= 512;
     const int keys = b.prefix_len < b.key_limit ? b.prefix_len : b.key_limit;
     if (keys > 0) {
@@ -934,7 +952,7 @@ size_t up256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 template <int D, bool BF, int P, int O>
 hipError_t launch(const AttnArgs& a, Plan p, hipStream_t st) {
     const long long pgrid = static_cast<long long>(a.cache.heads) * p.psplits * p.pblocks;
-    const long long grid = pgrid + static_cast<long long>(a.cache.heads) * p.splits * p.blocks * a.batch.num_seqs;
+    const long long grid = pgrid + static_cast<long long>(a.cache.heads) * (p.splits | 1) * p.blocks * a.batch.num_seqs;
     if (grid > 0x7fffffffll) return hipErrorInvalidConfiguration;
     p.pgrid = static_cast<int>(pgrid);
     constexpr int bytes = lds_bytes(D, P) > lds_bytes(D, O) ? lds_bytes(D, P) : lds_bytes(D, O);
