@@ -713,19 +713,39 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
     };
     // this tile's scores to probabilities, block by block, each block's place
     // taken by the next tile's scores as it becomes free (behind the last tile
-    // they are of whatever the buffer holds, and nothing uses them)
-    const auto turn = [&](uint32_t (&p)[NQ][KB][2], uint32_t kt) {
+    // they are of whatever the buffer holds, and nothing uses them).  LDS is
+    // read ahead of its use: K a block of 16 keys, V^T kAhead operands, since a
+    // wave that waits for each read leaves both units idle; the scheduling
+    // barriers keep the compiler from sinking the reads to their uses.
+    constexpr int kAhead = 4, VF = KB / 2 * ND;
+    u32x4 kf[2][NS], vf[kAhead];
+    const auto read_k = [&](u32x4 (&f)[NS], uint32_t kt, int b) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i) f[i] = *(const lds_u32x4*)((const lds_byte*)(uintptr_t)(kt + kat[i]) + 32 * D * b);
+    };
+    const auto read_v = [&](uint32_t vt, int n) {
+        lds_byte* at = (lds_byte*)(uintptr_t)(vt + (vat ^ (32 * (n % ND)))) + 64 * D * (n / ND);
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 32 * D));
+        const u32x2 ux = __builtin_bit_cast(u32x2, x), uy = __builtin_bit_cast(u32x2, y);
+        return u32x4{ux[0], ux[1], uy[0], uy[1]};
+    };
+    const auto turn = [&](uint32_t (&p)[NQ][KB][2], uint32_t kt, uint32_t vt) {
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
+            if (b + 1 < KB) {
+                read_k(kf[(b + 1) & 1], kt, b + 1);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) vf[i] = read_v(vt, i);
+            }
             f32x4 to[NQ];
 #pragma unroll
             for (int n = 0; n < NQ; ++n) to[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                const u32x4 kf = *(const lds_u32x4*)((const lds_byte*)(uintptr_t)(kt + kat[i]) + 32 * D * b);
+            for (int i = 0; i < NS; ++i)
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) to[n] = mma<BF>(kf, q[n][i], to[n]);
-            }
+                for (int n = 0; n < NQ; ++n) to[n] = mma<BF>(kf[b & 1][i], q[n][i], to[n]);
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
 #pragma unroll
@@ -737,23 +757,20 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
                 p[n][b][1] = pack2<BF>(s[n][b][2], s[n][b][3]);
                 s[n][b] = to[n];
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
     const auto values = [&](const uint32_t (&p)[NQ][KB][2], uint32_t vt) {
 #pragma unroll
-        for (int kk = 0; kk < KB / 2; ++kk)
+        for (int i = 0; i < VF; ++i) {
+            const int kk = i / ND, d = i % ND;
 #pragma unroll
-            for (int d = 0; d < ND; ++d) {
-                lds_byte* at = (lds_byte*)(uintptr_t)(vt + (vat ^ (32 * d))) + 64 * D * kk;
-                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-                const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 32 * D));
-                const u32x2 ux = __builtin_bit_cast(u32x2, x), uy = __builtin_bit_cast(u32x2, y);
-                const u32x4 vf = {ux[0], ux[1], uy[0], uy[1]};
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-                    o[n][d] = mma<BF>(vf, u32x4{p[n][2 * kk][0], p[n][2 * kk][1], p[n][2 * kk + 1][0], p[n][2 * kk + 1][1]},
-                                      o[n][d]);
-            }
+            for (int n = 0; n < NQ; ++n)
+                o[n][d] = mma<BF>(vf[i % kAhead], u32x4{p[n][2 * kk][0], p[n][2 * kk][1], p[n][2 * kk + 1][0], p[n][2 * kk + 1][1]},
+                                  o[n][d]);
+            if (i + kAhead < VF) vf[i % kAhead] = read_v(vt, i + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
 
     if (lo < hi) {
@@ -777,9 +794,10 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
             page_k = page_of(at + 3 * KT);
             const uint32_t kt = base + 2 * (buf ^ 1) * TILE, vt = base + (2 * buf + 1) * TILE;
             if (mine(at)) {
+                read_k(kf[0], kt, 0);
                 settle(at);
                 uint32_t p[NQ][KB][2];
-                turn(p, kt);
+                turn(p, kt, vt);
                 values(p, vt);
             } else if (mine(at + KT)) {
                 scores(kt);
