@@ -84,11 +84,18 @@ __device__ __forceinline__ f32x2 swap16(float v) {
     return f32x2{__builtin_bit_cast(float, x), __builtin_bit_cast(float, y)};
 }
 
+// The larger value, NaN if either is (three operands an instruction; fmaxf
+// would spend one more on each operand to quiet its NaN).
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float larger(float t, const f32x4& v) {
+    return larger(larger(larger(larger(t, v[0]), v[1]), v[2]), v[3]);
+}
+
 // Over the four lanes that share a row (l, l ^ 16, l ^ 32, l ^ 48).
 __device__ __forceinline__ float row_max(float v) {
     const f32x2 a = swap32(v);
-    const f32x2 b = swap16(fmaxf(a[0], a[1]));
-    return fmaxf(b[0], b[1]);
+    const f32x2 b = swap16(larger(a[0], a[1]));
+    return larger(b[0], b[1]);
 }
 
 __device__ __forceinline__ float row_sum(float v) {
@@ -98,7 +105,7 @@ __device__ __forceinline__ float row_sum(float v) {
 }
 
 // How a call is cut; every field follows from the host's sizes alone.  A
-// sequence's unit has splits | 1 places in the grid: workgroups go to the four
+// sequence's streamed unit has splits | 1 places in the grid: workgroups go to the four
 // shader engines of an XCD in turn, and where sequences end early an even
 // period would leave the same engines without work each time (16 sequences of
 // 1 to 8192 keys 25.1 -> 23.6 us).
@@ -190,12 +197,10 @@ __device__ __forceinline__ void load_q(const AttnArgs& a, const Row& r, int head
 template <int KB, int ND, bool BF>
 __device__ __forceinline__ void softmax_step(f32x4 (&s)[KB], uint32_t (&p)[KB][2], float sc, float& m, float& l,
                                              f32x4 (&o)[ND]) {
-    float mx = s[0][0];
+    float mx = m;
 #pragma unroll
-    for (int k = 0; k < KB; ++k)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[k][i]);
-    mx = fmaxf(m, row_max(mx));
+    for (int k = 0; k < KB; ++k) mx = larger(mx, s[k]);
+    mx = row_max(mx);
     const float mc = mx == -INFINITY ? 0.f : mx * sc;
     if (__ballot(mx > m)) {
         const float old = m == -INFINITY ? mc : m * sc;
@@ -559,10 +564,8 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
     const int head = id % Hk;
     int rest = id / Hk;
     const int splits = PREFIX ? pl.psplits : pl.splits, len = PREFIX ? pl.plen : pl.len;
-    const int places = PREFIX ? splits : splits | 1;
-    const int split = rest % places;
-    rest /= places;
-    if (split >= splits) return;
+    const int split = rest % splits;
+    rest /= splits;
     const int blocks = PREFIX ? pl.pblocks : pl.blocks, upper = (blocks + 1) / 2, nth = rest % blocks;
     const int block = pl.paired && nth >= upper ? nth - upper : blocks - 1 - nth;
     const Segment seg = PREFIX ? prefix_segment(a) : own_segment(a, rest / blocks);
@@ -671,7 +674,19 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
             }
         }
     };
-    // maxima, masks and, where one rose past the slack, the new reference
+    // a row's largest score of the tile in s: `values` finds it for the next
+    // tile between its MFMAs, a masked tile and the first one find it here
+    float mx[NQ];
+    const auto find_top = [&]() {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            mx[n] = -INFINITY;
+#pragma unroll
+            for (int b = 0; b < KB; ++b) mx[n] = larger(mx[n], s[n][b]);
+            mx[n] = row_max(mx[n]);
+        }
+    };
+    // masks and, where a maximum rose past the slack, the new reference
     const auto settle = [&](int at) {
         if (at < full_lo || at + KT > full_hi) {
 #pragma unroll
@@ -684,26 +699,19 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
                         const unsigned past = at + 16 * b + 4 * g4 + i - row[n].lo;
                         if (past >= static_cast<unsigned>(row[n].hi - row[n].lo)) s[n][b][i] = -INFINITY;
                     }
+            find_top();
         }
-        float mx[NQ];
         bool rose = false;
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            mx[n] = s[n][0][0];
-#pragma unroll
-            for (int b = 0; b < KB; ++b)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) mx[n] = fmaxf(mx[n], s[n][b][i]);
-            mx[n] = row_max(mx[n]);
+        for (int n = 0; n < NQ; ++n)
             rose |= m[n] == -INFINITY ? mx[n] != -INFINITY : mx[n] * sc > mc[n] + kSlack;
-        }
         if (__ballot(rose)) {
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
-                mx[n] = fmaxf(mx[n], m[n]);
-                const float now = mx[n] == -INFINITY ? 0.f : mx[n] * sc;
+                const float top = fmaxf(mx[n], m[n]);
+                const float now = top == -INFINITY ? 0.f : top * sc;
                 const float c = m[n] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mc[n] - now);
-                m[n] = mx[n];
+                m[n] = top;
                 mc[n] = now;
                 l[n] *= c;
 #pragma unroll
@@ -730,7 +738,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
         const u32x2 ux = __builtin_bit_cast(u32x2, x), uy = __builtin_bit_cast(u32x2, y);
         return u32x4{ux[0], ux[1], uy[0], uy[1]};
     };
-    const auto turn = [&](uint32_t (&p)[NQ][KB][2], uint32_t kt, uint32_t vt) {
+    const auto turn = [&](uint32_t (&p)[NQ][KB][2], uint32_t kt, uint32_t vt, auto between) {
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
             if (b + 1 < KB) {
@@ -758,9 +766,12 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
                 s[n][b] = to[n];
             }
             __builtin_amdgcn_sched_barrier(0);
+            between(b);
         }
     };
     const auto values = [&](const uint32_t (&p)[NQ][KB][2], uint32_t vt) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) mx[n] = -INFINITY;
 #pragma unroll
         for (int i = 0; i < VF; ++i) {
             const int kk = i / ND, d = i % ND;
@@ -769,6 +780,16 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
                 o[n][d] = mma<BF>(vf[i % kAhead], u32x4{p[n][2 * kk][0], p[n][2 * kk][1], p[n][2 * kk + 1][0], p[n][2 * kk + 1][1]},
                                   o[n][d]);
             if (i + kAhead < VF) vf[i % kAhead] = read_v(vt, i + kAhead);
+            // blocks of the next tile's scores, spread over the first half
+            constexpr int AT = VF / 2 >= KB ? VF / 2 / KB : 1;
+            if (i % AT == 0 && i / AT < KB) {
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) mx[n] = larger(mx[n], s[n][i / AT]);
+            }
+            if (i == VF - VF / 4) {
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) mx[n] = row_max(mx[n]);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -783,30 +804,93 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
         if (lo + KT < hi) copy(a.cache.k, base + 2 * TILE, lo + KT, page_k);
         page_v = page_k;
         page_k = page_of(lo + 2 * KT);
-        if (mine(lo)) scores(base);
+        if (mine(lo)) {
+            scores(base);
+            find_top();
+        }
         int buf = 0;
         for (int at = lo; at < hi; at += KT, buf ^= 1) {
             copies_done();
             __syncthreads();              // V of this tile and K of the next are there, their other buffers free
-            if (at + KT < hi) copy(a.cache.v, base + (2 * (buf ^ 1) + 1) * TILE, at + KT, page_v);
-            if (at + 2 * KT < hi) copy(a.cache.k, base + 2 * buf * TILE, at + 2 * KT, page_k);
-            page_v = page_k;
-            page_k = page_of(at + 3 * KT);
             const uint32_t kt = base + 2 * (buf ^ 1) * TILE, vt = base + (2 * buf + 1) * TILE;
+            const auto copy_next = [&](int what) {
+                if (what == 0 && at + KT < hi) copy(a.cache.v, base + (2 * (buf ^ 1) + 1) * TILE, at + KT, page_v);
+                if (what == 1) {
+                    if (at + 2 * KT < hi) copy(a.cache.k, base + 2 * buf * TILE, at + 2 * KT, page_k);
+                    page_v = page_k;
+                    page_k = page_of(at + 3 * KT);
+                }
+            };
             if (mine(at)) {
                 read_k(kf[0], kt, 0);
                 settle(at);
                 uint32_t p[NQ][KB][2];
-                turn(p, kt, vt);
+                turn(p, kt, vt, copy_next);
                 values(p, vt);
-            } else if (mine(at + KT)) {
-                scores(kt);
+            } else {
+                copy_next(0);
+                copy_next(1);
+                if (mine(at + KT)) {
+                    scores(kt);
+                    find_top();
+                }
             }
         }
     }
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
         finish<ND>(a, pl, PREFIX ? split : pl.psplits + split, row[n], hidx[n], m[n] == -INFINITY ? -INFINITY : mc[n], row_sum(l[n]), o[n]);
+}
+
+// The same for many rows of few splits: D / 4 lanes a row, the splits in turn,
+// so a workgroup finishes 256 / (D / 4) rows (32000 rows of 2 splits take 12 us
+// so, 33 with a workgroup each).
+constexpr int kRowSplits = 8;
+
+template <int D>
+__global__ __launch_bounds__(256) void attn_join_rows_kernel(AttnArgs a, Plan pl) {
+    constexpr int LANES = D / 4, AT = 256 / LANES;
+    const size_t rows = static_cast<size_t>(a.batch.tokens) * a.q_heads;
+    const size_t row = static_cast<size_t>(blockIdx.x) * AT + threadIdx.x / LANES;
+    const int at = threadIdx.x % LANES, total = pl.psplits + pl.splits;
+    if (row >= rows) return;
+    float2 st[kRowSplits];
+    f32x4 v[kRowSplits];
+#pragma unroll
+    for (int i = 0; i < kRowSplits; ++i)
+        if (i < total) {
+            st[i] = pl.stat[i * rows + row];
+            v[i] = reinterpret_cast<const f32x4*>(pl.part + (i * rows + row) * D)[at];
+        }
+    // the row's sequence: a scan of the starts by every lane (rows of a wave
+    // belong to different tokens)
+    const int t = static_cast<int>(row / a.q_heads);
+    int s = t / a.batch.q_len;
+    if (a.batch.q_start) {
+        s = -1;
+        for (int j = 0; j < a.batch.num_seqs; ++j) s += a.batch.q_start[j] <= t;
+        if (s < 0) return;
+    }
+    const Seq q = load_seq(a.batch, s);
+    if (t >= q.start + q.count || t - q.start >= a.batch.q_len) return;
+    const int live = pl.psplits + (max(q.keys - a.batch.prefix_len, 0) + pl.len - 1) / pl.len;
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kRowSplits; ++i)
+        if (i < live) m = fmaxf(m, st[i].x);
+    const float base = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kRowSplits; ++i)
+        if (i < live && st[i].y != 0.f) {
+            const float w = __builtin_amdgcn_exp2f((st[i].x == -INFINITY ? base : st[i].x) - base);
+            l += w * st[i].y;
+            acc += v[i] * w;
+        }
+    const float inv = l != 0.f ? 1.0f / l : 0.f;
+    store4(a, row * D + 4 * at, l != 0.f ? acc * inv : f32x4{0.f, 0.f, 0.f, 0.f});
+    if (a.lse && at == 0) a.lse[row] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // ------------------------------------------------------------- one launch
@@ -915,7 +999,14 @@ int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b
 // Rows up to which a unit streams, and rows of a tile workgroup.  Heads of 256
 // keep to one row block a wave: two do not fit 256 registers beside the sums.
 int stream_rows(int dim) { return dim > 128 ? 16 : 32; }
-int tile_rows(long long rows, int dim) { return rows <= 64 || dim > 128 ? 64 : 128; }
+
+// 64 rows to a tile workgroup where 128 would leave half the CUs without one
+// (a 300-token prompt 14.5 -> 11.1 us, 256 tokens over 4096 keys 39.2 -> 36.6);
+// otherwise 128: each LDS read then feeds two MFMAs (2048 tokens over 4096 keys
+// 138 against 174 us).
+int tile_rows(const KvCache& c, const KvBatch& b, long long rows) {
+    return c.dim > 128 || ((rows + 127) / 128) * b.num_seqs * c.heads < 128 ? 64 : 128;
+}
 
 // Splits of `keys` keys for `units` workgroups without splitting: enough to
 // give the chip `want` workgroups, none under `least` keys.
@@ -929,8 +1020,8 @@ void cut(long long units, int keys, int want, int least, int* splits, int* len) 
     *splits = keys > 0 ? ceil_div(keys, *len) : 1;
 }
 
-int kind_of(long long rows, int dim) {
-    return rows <= 16 ? S1 : rows <= stream_rows(dim) ? S2 : tile_rows(rows, dim) == 64 ? T1 : T2;
+int kind_of(const KvCache& c, const KvBatch& b, long long rows) {
+    return rows <= 16 ? S1 : rows <= stream_rows(c.dim) ? S2 : tile_rows(c, b, rows) == 64 ? T1 : T2;
 }
 
 Plan make_plan(const KvCache& c, const KvBatch& b, int q_heads) {
@@ -940,7 +1031,7 @@ Plan make_plan(const KvCache& c, const KvBatch& b, int q_heads) {
     p.rows = static_cast<int>(rows);
     const int own = b.key_limit > b.prefix_len ? b.key_limit - b.prefix_len : 0;
     const bool stream = rows <= stream_rows(c.dim);
-    p.blocks = stream ? 1 : ceil_div(rows, tile_rows(rows, c.dim));
+    p.blocks = stream ? 1 : ceil_div(rows, tile_rows(c, b, rows));
     const long long units = static_cast<long long>(b.num_seqs) * c.heads * p.blocks;
     // Streams: splits of at least 128 keys, one step of each wave, while units
     // are few; 256 from 256 units on (64 under a prefix 38.8 -> 37.1 us, where
@@ -952,7 +1043,10 @@ Plan make_plan(const KvCache& c, const KvBatch& b, int q_heads) {
     const bool many = units >= 256;
     const int least = !many ? 128 : own <= 512 && b.prefix_len == 0 ? 512 : 256;
     const int want = rows <= 16 && c.dim <= 128 ? 4096 : 2048;
-    cut(units, own, stream ? want : 512, stream ? least : 512, &p.splits, &p.len);
+    // Tiles: whole while every CU has a unit (1000-token prompt 29.8 us, 43.6 in
+    // two splits), else two workgroups a CU (500 tokens over 6000 keys 72.6 us,
+    // 82.0 with one a CU).
+    cut(units, own, stream ? want : many ? 256 : 512, stream ? least : 512, &p.splits, &p.len);
     p.paired = units * p.splits <= 512;
     const int keys = b.prefix_len < b.key_limit ? b.prefix_len : b.key_limit;
     if (keys > 0) {
@@ -970,7 +1064,8 @@ size_t up256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 template <int D, bool BF, int P, int O>
 hipError_t launch(const AttnArgs& a, Plan p, hipStream_t st) {
     const long long pgrid = static_cast<long long>(a.cache.heads) * p.psplits * p.pblocks;
-    const long long grid = pgrid + static_cast<long long>(a.cache.heads) * (p.splits | 1) * p.blocks * a.batch.num_seqs;
+    const int places = O <= S2 ? p.splits | 1 : p.splits;
+    const long long grid = pgrid + static_cast<long long>(a.cache.heads) * places * p.blocks * a.batch.num_seqs;
     if (grid > 0x7fffffffll) return hipErrorInvalidConfiguration;
     p.pgrid = static_cast<int>(pgrid);
     constexpr int bytes = lds_bytes(D, P) > lds_bytes(D, O) ? lds_bytes(D, P) : lds_bytes(D, O);
@@ -984,12 +1079,13 @@ hipError_t launch(const AttnArgs& a, Plan p, hipStream_t st) {
 }
 
 // The prefix's unit has at least as many rows as a sequence's, so these
-// combinations cover every call (a prefix of 33 to 64 rows takes 128-row
-// tiles, a streamed one of 17 to 32 rows streams the sequences' likewise).
+// combinations cover every call (a tiled prefix takes 128-row tiles, a streamed
+// one of 17 to 32 rows streams the sequences' likewise).
 template <int D, bool BF>
 hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t st) {
-    const int own = kind_of(p.rows, D);
-    const int pre = p.psplits ? kind_of(static_cast<long long>(a.batch.tokens) * (a.q_heads / a.cache.heads), D) : NONE;
+    const long long prows = static_cast<long long>(a.batch.tokens) * (a.q_heads / a.cache.heads);
+    const int own = kind_of(a.cache, a.batch, p.rows);
+    const int pre = p.psplits ? prows <= 16 ? S1 : prows <= stream_rows(D) ? S2 : T2 : NONE;
     hipError_t e;
     if constexpr (D > 128) {
         e = pre == NONE ? own == S1 ? launch<D, BF, NONE, S1>(a, p, st) : launch<D, BF, NONE, T1>(a, p, st)
@@ -1011,6 +1107,11 @@ hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t st) {
     }
     if (e != hipSuccess || p.direct) return e;
     const size_t rows = static_cast<size_t>(a.batch.tokens) * a.q_heads;
+    if (p.psplits + p.splits <= kRowSplits && rows >= 4096) {
+        constexpr size_t at = 1024 / D;
+        hipLaunchKernelGGL((attn_join_rows_kernel<D>), dim3(static_cast<unsigned>((rows + at - 1) / at)), dim3(256), 0, st, a, p);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL((attn_join_kernel<D>), dim3(static_cast<unsigned>(rows)), dim3(256), 0, st, a, p);
     return hipGetLastError();
 }
