@@ -841,6 +841,10 @@ class Rope:
 
 def _token_rows(t, name, dtype, tokens, heads, dim):
     """[tokens][heads][dim] with a token's heads contiguous; the token stride."""
+    if isinstance(t, torch.Tensor) and t.dtype == dtype and t.is_contiguous() and t.is_cuda:
+        s = t.shape                        # the dense case in as few steps as it takes
+        if len(s) == 3 and s[0] == tokens and s[2] == dim and (heads is None or s[1] == heads):
+            return s[1] * dim
     if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.dim() == 3 and t.is_cuda):
         _need(isinstance(t, torch.Tensor), "%s must be a torch.Tensor" % name)
         _need(t.dtype == dtype, "%s must have dtype %s (got %s)" % (name, dtype, t.dtype))
@@ -877,11 +881,17 @@ def kv_append(cache, batch, k, v, q=None, rope=None, q_norm=None, k_norm=None, e
         _dev_tensor(k_norm, "k_norm", (dt,), (D,))
     if positions is not None:
         _dev_tensor(positions, "positions", _I32, (n,))
-    _check(_call("cl_kv_append")(cache._bytes, batch._bytes, None if rope is None else rope._bytes, _opt_ptr(q), qs,
-                                 heads, k.data_ptr(), ks, v.data_ptr(), vs, _opt_ptr(q_norm), _opt_ptr(k_norm), eps,
-                                 _opt_ptr(positions), _opt_ptr(q_out) if q is not None else None,
-                                 _raw_stream(stream)))
-    return q_out if q is not None else None
+    if q is None:
+        q_out = None
+    st = _call("cl_kv_append")(cache._bytes, batch._bytes, None if rope is None else rope._bytes,
+                               None if q is None else q.data_ptr(), qs, heads, k.data_ptr(), ks, v.data_ptr(), vs,
+                               None if q_norm is None else q_norm.data_ptr(),
+                               None if k_norm is None else k_norm.data_ptr(), eps,
+                               None if positions is None else positions.data_ptr(),
+                               None if q_out is None else q_out.data_ptr(), _raw_stream(stream))
+    if st:
+        _check(st)
+    return q_out
 
 
 def attention_workspace(cache, batch, q_heads):
