@@ -627,9 +627,9 @@ cl_status cl_kv_append(const cl_kv_cache* cache, const cl_kv_batch* batch, const
  * for every token and head over the keys it sees (query heads
  * h (q_heads / kv_heads) .. share key head h).  With n keys, a token at
  * position p sees key j < n, only j <= p if causal, and only j > p - window if
- * window > 0.  A token that sees no key gets zeros and lse = -inf.  A hidden
- * key's or value's contents do not matter if it stands at or behind n; those
- * of the sequence itself must be finite.
+ * window > 0.  A token that sees no key gets zeros and lse = -inf.  What stands
+ * in a key or value that a token does not see, infinities and NaN included,
+ * does not reach its result.
  * One call serves single tokens, drafted tokens and prompts, mixed as they
  * come; the keys of a shared prefix are read once for all sequences.
  *

@@ -45,6 +45,9 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // Most splits of a call (the prefix's and a sequence's own together).
 constexpr int kMaxSplits = 128;
@@ -269,7 +272,6 @@ __device__ __forceinline__ int swz(int row, int chunk) {
 // Operand of V^T: 16 dims (block d) x 32 keys (rows 32 kk ..) of a tile in LDS.
 template <int D>
 __device__ __forceinline__ u32x4 load_vt(const uint16_t* v, int kk, int d) {
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     const int lane = threadIdx.x & 63, g = lane >> 4, i = lane & 15;
     u32x4 r;
 #pragma unroll
@@ -283,6 +285,71 @@ __device__ __forceinline__ u32x4 load_vt(const uint16_t* v, int kk, int d) {
         r[2 * half + 1] = u[1];
     }
     return r;
+}
+
+// Values that are infinite or NaN.  0 times one of them is no zero, so where
+// not every row sees every key of a tile, such values become zeros in LDS
+// before the second product, and a pass over these tiles at the end adds them
+// to the rows that see them (each is the whole result of its row and dim,
+// whatever its probability).  Other tiles are not looked at, and the pass runs
+// only where there were such values.
+//
+// The halves of a word whose exponent is all ones, as ones in bits 0 and 16.
+template <bool BF>
+__device__ __forceinline__ uint32_t not_finite(uint32_t v) {
+    constexpr uint32_t kMask = BF ? 0x7f807f80u : 0x7c007c00u, kOne = BF ? 0x00800080u : 0x04000400u;
+    return ((v & kMask) + kOne) >> 15 & 0x00010001u;
+}
+
+// v with such values as zeros; `bad` collects that there were some.
+template <bool BF>
+__device__ __forceinline__ u32x4 finite_or_zero(u32x4 v, uint32_t& bad) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t vi = v[i], b = not_finite<BF>(vi);
+        v[i] = vi & ~((b << 16) - b);
+        bad |= b;
+    }
+    return v;
+}
+
+// Of the `count` x 64 16-byte pieces from `at` (an even count), which this wave
+// alone uses now.
+template <bool BF>
+__device__ __forceinline__ void clean_lds(uint32_t at, int count, uint32_t& bad) {
+    at += 16 * (threadIdx.x & 63);
+#pragma unroll 1
+    for (int i = 0; i < count; i += 2, at += 2048) {
+        lds_u32x4* const p = (lds_u32x4*)(uintptr_t)at;
+        const u32x4 x = p[0], y = p[64];
+        p[0] = finite_or_zero<BF>(x, bad);
+        p[64] = finite_or_zero<BF>(y, bad);
+    }
+}
+
+// The pass at the end for one row block over keys [from, to): o[d] holds dims
+// 16 (first + d) + 4 g4 ..
+template <int D, bool BF, int ND>
+__device__ void add_not_finite(const AttnArgs& a, const Segment& seg, int head, const Row& row, int from, int to, int first,
+                               f32x4 (&o)[ND]) {
+    const int g4 = (threadIdx.x & 63) >> 4;
+    for (int j = from; j < to; ++j) {
+        const int r = pool_row(a, seg, head, j);
+        if (r < 0) continue;
+        const uint16_t* v = a.cache.v + static_cast<size_t>(r) * D + 16 * first + 4 * g4;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            const u32x2 u = *reinterpret_cast<const u32x2*>(v + 16 * d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t ui = i & 2 ? u[1] : u[0];
+                const uint16_t h = static_cast<uint16_t>(i & 1 ? ui >> 16 : ui);
+                const float x = BF ? bf16_bits_to_f32(h) : f16_bits_to_f32(h);
+                if (not_finite<BF>(h) && j >= row.lo && j < row.hi) o[d][i] += x;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
 }
 
 __device__ __forceinline__ Segment own_segment(const AttnArgs& a, int s) {
@@ -300,10 +367,14 @@ __device__ __forceinline__ Segment prefix_segment(const AttnArgs& a) {
 
 // ------------------------------------------------------------- few rows
 
-// Bytes of LDS: every wave's V, then the statistics.
-constexpr int stream_lds(int D, int NQ) { return 256 * D + 512 * NQ; }
+// Bytes of LDS: every wave's V, then the statistics and a flag of each.
+constexpr int stream_lds(int D, int NQ) { return 256 * D + 512 * NQ + 16; }
 
-template <int D, bool BF, int NQ, bool PREFIX>
+//
+// SAME: every row of a unit sees the same keys (one token a sequence and no
+// window), so only the last step has a mask and no value is hidden from a row
+// that its neighbours see.
+template <int D, bool BF, int NQ, bool PREFIX, bool SAME>
 __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, int id, unsigned char* lds) {
     constexpr int NS = D / 32, ND = D / 16, CH = D / 8;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g4 = lane >> 4, col = lane & 15;
@@ -335,7 +406,7 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
     Row row[NQ];
     u32x4 q[NQ][NS];
     int hidx[NQ];
-    int lo = 0x7fffffff, hi = 0;
+    int lo = 0x7fffffff, hi = 0, full_lo = 0, full_hi = 0x7fffffff;
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         const int r = 16 * n + col;
@@ -343,13 +414,19 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
         hidx[n] = head * group + r % group;
         load_q<D, BF>(a, row[n], hidx[n], q[n]);
         if (row[n].hi > row[n].lo) lo = min(lo, row[n].lo), hi = max(hi, row[n].hi);
+        if (row[n].token >= 0) full_lo = max(full_lo, row[n].lo), full_hi = min(full_hi, row[n].hi);
     }
-    // the wave's steps cover the keys that any of its rows sees
+    // the wave's steps cover the keys that any of its rows sees; between full_lo
+    // and full_hi every row sees them all
 #pragma unroll
     for (int off = 1; off < 16; off <<= 1) {
         lo = min(lo, __shfl_xor(lo, off, 64));
         hi = max(hi, __shfl_xor(hi, off, 64));
+        full_lo = max(full_lo, __shfl_xor(full_lo, off, 64));
+        full_hi = min(full_hi, __shfl_xor(full_hi, off, 64));
     }
+    full_lo = __builtin_amdgcn_readfirstlane(full_lo);
+    full_hi = __builtin_amdgcn_readfirstlane(full_hi);
     lo = max(lo, begin) & ~31;
     hi = min(hi, end);
     if (hi <= lo) lo = hi = 0;                        // nothing to see here
@@ -389,6 +466,9 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
         }
     };
 
+    const auto masked = [&](int step) { return step < full_lo || min(step + 32, seg.keys) > full_hi; };
+    const uint32_t vat = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte*)vl));
+    uint32_t unseen = 0;
     int at = lo + 32 * wave;
     if (at < hi) {
         // without a window the first step is the one looked up above
@@ -410,6 +490,7 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
                 const int c = lane + 64 * i;
                 *reinterpret_cast<u32x4*>(vl + 8 * swz<D>(c / CH, c % CH)) = vr[i];
             }
+            if (!SAME && masked(at)) clean_lds<BF>(vat, VR, unseen);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             const int cur = at;
             if (at + 128 < hi) {
@@ -419,13 +500,15 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
             uint32_t p[NQ][2][2];
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
+                if (!SAME || cur + 32 > hi) {
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                    for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key = cur + 16 * b + 4 * g4 + i;
-                        if (key < row[n].lo || key >= min(row[n].hi, end)) s[n][b][i] = -INFINITY;
-                    }
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = cur + 16 * b + 4 * g4 + i;
+                            if ((!SAME && key < row[n].lo) || key >= (SAME ? hi : min(row[n].hi, end))) s[n][b][i] = -INFINITY;
+                        }
+                }
                 softmax_step<2, ND, BF>(s[n], p[n], sc, m[n], l[n], o[n]);
             }
 #pragma unroll
@@ -446,7 +529,11 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
         l[n] = row_sum(l[n]);
         if (g4 == 0) stat[wave][16 * n + col] = float2{m[n], l[n]};
     }
+    uint32_t* const unclean = reinterpret_cast<uint32_t*>(lds + 256 * D + 512 * NQ);
+    const bool mine = __ballot(unseen) != 0;
+    if (lane == 0) unclean[wave] = mine;
     __syncthreads();
+    const bool dirty = (unclean[0] | unclean[1] | unclean[2] | unclean[3]) != 0;
     float* const sum = reinterpret_cast<float*>(lds);     // one row block of every wave
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
@@ -468,15 +555,17 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
         __syncthreads();
         // wave w adds the quarter of the dims it stores
         constexpr int PER = ND / 4;
-        f32x4 r[ND];
-#pragma unroll
-        for (int d = 0; d < ND; ++d) r[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+        f32x4 r[PER];
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
+            r[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < 4; ++w)
                 r[j] += *reinterpret_cast<const f32x4*>(sum + (w * 16 + col) * D + 4 * ((4 * (wave * PER + j) + g4) ^ col));
         }
+        if (!SAME && dirty)
+            for (int step = lo; step < hi; step += 32)
+                if (masked(step)) add_not_finite<D, BF>(a, seg, head, row[n], step, min(step + 32, hi), wave * PER, r);
         if (row[n].token < 0) continue;
         const size_t rw = static_cast<size_t>(row[n].token) * a.q_heads + hidx[n];
         const int slot = PREFIX ? split : pl.psplits + split;
@@ -499,10 +588,6 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
 }
 
 // ------------------------------------------------------------- many rows
-
-typedef __attribute__((address_space(3))) unsigned char lds_byte;
-typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // What a lane copies for a key that is not there: zeros for one past the
 // segment, NaN for one whose page is outside the pool.
@@ -597,11 +682,19 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
         full_hi = min(full_hi, __shfl_xor(full_hi, off, 64));
     }
     int(*bounds)[4] = reinterpret_cast<int(*)[4]>(lds + 4 * TILE);
-    if (lane == 0) bounds[0][wave] = lo, bounds[1][wave] = hi;
+    if (lane == 0) bounds[0][wave] = lo, bounds[1][wave] = hi, bounds[2][wave] = full_lo, bounds[3][wave] = full_hi;
     __syncthreads();
     const int wlo = __builtin_amdgcn_readfirstlane(lo), whi = __builtin_amdgcn_readfirstlane(hi);
+    int all_lo = 0, all_hi = 0x7fffffff;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) lo = min(lo, bounds[0][w]), hi = max(hi, bounds[1][w]);
+    for (int w = 0; w < 4; ++w) {
+        lo = min(lo, bounds[0][w]);
+        hi = max(hi, bounds[1][w]);
+        all_lo = max(all_lo, bounds[2][w]);
+        all_hi = min(all_hi, bounds[3][w]);
+    }
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
     lo = __builtin_amdgcn_readfirstlane(max(lo, begin) & ~(KT - 1));
     hi = __builtin_amdgcn_readfirstlane(hi);
     full_lo = __builtin_amdgcn_readfirstlane(full_lo);
@@ -686,9 +779,12 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
             mx[n] = row_max(mx[n]);
         }
     };
+    const auto masked = [&](int at) { return at < full_lo || at + KT > full_hi; };
+    const auto hides = [&](int at) { return at < all_lo || min(at + KT, seg.keys) > all_hi; };     // of the workgroup's rows
+    uint32_t unseen = 0;
     // masks and, where a maximum rose past the slack, the new reference
     const auto settle = [&](int at) {
-        if (at < full_lo || at + KT > full_hi) {
+        if (masked(at)) {
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -811,6 +907,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
         int buf = 0;
         for (int at = lo; at < hi; at += KT, buf ^= 1) {
             copies_done();
+            if (hides(at)) clean_lds<BF>(base + (2 * buf + 1) * TILE + WR * wave * D * 2, CP, unseen);
             __syncthreads();              // V of this tile and K of the next are there, their other buffers free
             const uint32_t kt = base + 2 * (buf ^ 1) * TILE, vt = base + (2 * buf + 1) * TILE;
             const auto copy_next = [&](int what) {
@@ -837,9 +934,17 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
             }
         }
     }
+    const bool found = __ballot(unseen) != 0;
+    if (lane == 0) bounds[0][wave] = found;
+    __syncthreads();
+    const bool dirty = (bounds[0][0] | bounds[0][1] | bounds[0][2] | bounds[0][3]) != 0;
 #pragma unroll
-    for (int n = 0; n < NQ; ++n)
+    for (int n = 0; n < NQ; ++n) {
+        if (dirty)
+            for (int at = lo; at < hi; at += KT)
+                if (hides(at)) add_not_finite<D, BF>(a, seg, head, row[n], at, min(at + KT, hi), 0, o[n]);
         finish<ND>(a, pl, PREFIX ? split : pl.psplits + split, row[n], hidx[n], m[n] == -INFINITY ? -INFINITY : mc[n], row_sum(l[n]), o[n]);
+    }
 }
 
 // The same for many rows of few splits: D / 4 lanes a row, the splits in turn,
@@ -895,12 +1000,12 @@ __global__ __launch_bounds__(256) void attn_join_rows_kernel(AttnArgs a, Plan pl
 
 // ------------------------------------------------------------- one launch
 
-// How a segment's units are worked: not at all, streamed (16 or 32 rows) or by
-// tiles (64 or 128 rows a workgroup).
-enum { NONE = 0, S1 = 1, S2 = 2, T1 = 3, T2 = 4 };
+// How a segment's units are worked: not at all, streamed (16 or 32 rows, S0 of
+// 16 that all see the same keys) or by tiles (64 or 128 rows a workgroup).
+enum { NONE = 0, S1 = 1, S2 = 2, T1 = 3, T2 = 4, S0 = 5 };
 
 constexpr int lds_bytes(int D, int kind) {
-    return kind == NONE ? 0 : kind <= S2 ? stream_lds(D, kind) : tile_lds(D);
+    return kind == NONE ? 0 : kind == S0 ? stream_lds(D, 1) : kind <= S2 ? stream_lds(D, kind) : tile_lds(D);
 }
 
 // The prefix's and the sequences' own workgroups side by side, so the tiles of
@@ -909,18 +1014,19 @@ constexpr int lds_bytes(int D, int kind) {
 // held to 256 they spill: 16 sequences of 200 to 8000 keys 124 against 96 us),
 // the rest two.
 template <int D, bool BF, int P, int O>
-__global__ __launch_bounds__(256, O <= S2 && D > 128 ? 1 : P == NONE && O == S1 ? 3 : 2) void attn_kernel(
+__global__ __launch_bounds__(256, (O <= S2 || O == S0) && D > 128 ? 1 : P == NONE && O == S0 ? 3 : 2) void attn_kernel(
     AttnArgs a, Plan pl) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int id = static_cast<int>(blockIdx.x);
     if constexpr (P != NONE) {
         if (id < pl.pgrid) {
-            if constexpr (P <= S2) attn_stream<D, BF, P, true>(a, pl, id, lds);
+            if constexpr (P <= S2) attn_stream<D, BF, P, true, false>(a, pl, id, lds);
             else attn_tile<D, BF, P - S2, true>(a, pl, id, lds);
             return;
         }
     }
-    if constexpr (O <= S2) attn_stream<D, BF, O, false>(a, pl, id - pl.pgrid, lds);
+    if constexpr (O == S0) attn_stream<D, BF, 1, false, true>(a, pl, id - pl.pgrid, lds);
+    else if constexpr (O <= S2) attn_stream<D, BF, O, false, false>(a, pl, id - pl.pgrid, lds);
     else attn_tile<D, BF, O - S2, false>(a, pl, id - pl.pgrid, lds);
 }
 
@@ -1064,7 +1170,7 @@ size_t up256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 template <int D, bool BF, int P, int O>
 hipError_t launch(const AttnArgs& a, Plan p, hipStream_t st) {
     const long long pgrid = static_cast<long long>(a.cache.heads) * p.psplits * p.pblocks;
-    const int places = O <= S2 ? p.splits | 1 : p.splits;
+    const int places = O <= S2 || O == S0 ? p.splits | 1 : p.splits;
     const long long grid = pgrid + static_cast<long long>(a.cache.heads) * places * p.blocks * a.batch.num_seqs;
     if (grid > 0x7fffffffll) return hipErrorInvalidConfiguration;
     p.pgrid = static_cast<int>(pgrid);
@@ -1084,22 +1190,30 @@ hipError_t launch(const AttnArgs& a, Plan p, hipStream_t st) {
 template <int D, bool BF>
 hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t st) {
     const long long prows = static_cast<long long>(a.batch.tokens) * (a.q_heads / a.cache.heads);
-    const int own = kind_of(a.cache, a.batch, p.rows);
+    int own = kind_of(a.cache, a.batch, p.rows);
+    if (own == S1 && a.batch.q_len == 1 && a.window == 0) own = S0;
     const int pre = p.psplits ? prows <= 16 ? S1 : prows <= stream_rows(D) ? S2 : T2 : NONE;
     hipError_t e;
     if constexpr (D > 128) {
-        e = pre == NONE ? own == S1 ? launch<D, BF, NONE, S1>(a, p, st) : launch<D, BF, NONE, T1>(a, p, st)
-            : pre == S1 ? launch<D, BF, S1, S1>(a, p, st)
-            : own == S1 ? launch<D, BF, T1, S1>(a, p, st)
-                        : launch<D, BF, T1, T1>(a, p, st);
+        if (pre == NONE)
+            e = own == S0   ? launch<D, BF, NONE, S0>(a, p, st)
+                : own == S1 ? launch<D, BF, NONE, S1>(a, p, st)
+                            : launch<D, BF, NONE, T1>(a, p, st);
+        else
+            e = pre == S1   ? launch<D, BF, S1, S1>(a, p, st)
+                : own == S0 ? launch<D, BF, T1, S0>(a, p, st)
+                : own == S1 ? launch<D, BF, T1, S1>(a, p, st)
+                            : launch<D, BF, T1, T1>(a, p, st);
     } else if (pre == NONE) {
-        e = own == S1   ? launch<D, BF, NONE, S1>(a, p, st)
+        e = own == S0   ? launch<D, BF, NONE, S0>(a, p, st)
+            : own == S1 ? launch<D, BF, NONE, S1>(a, p, st)
             : own == S2 ? launch<D, BF, NONE, S2>(a, p, st)
             : own == T1 ? launch<D, BF, NONE, T1>(a, p, st)
                         : launch<D, BF, NONE, T2>(a, p, st);
     } else {
         e = pre == S1   ? launch<D, BF, S1, S1>(a, p, st)
             : pre == S2 ? launch<D, BF, S2, S2>(a, p, st)
+            : own == S0 ? launch<D, BF, T2, S0>(a, p, st)
             : own == S1 ? launch<D, BF, T2, S1>(a, p, st)
             : own == S2 ? launch<D, BF, T2, S2>(a, p, st)
             : own == T1 ? launch<D, BF, T2, T1>(a, p, st)

@@ -258,3 +258,35 @@ def test_workspace_is_checked_and_sized_by_the_descriptors():
     out = cl.attention(c.cache, c.batch, c.q.cuda(), ws=ws)
     torch.cuda.synchronize()
     assert out.isfinite().all() and (ws[need:] == 255).all()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["fp16", "bf16"])
+@pytest.mark.parametrize("q,kv,D,window", [([4], [40], 128, 0), ([8, 3], [100, 70], 64, 20), ([130], [200], 128, 0),
+                                           ([100, 40], [100, 300], 64, 33), ([90], [90], 256, 0), ([3], [600], 256, 500)])
+def test_infinities_and_nan_reach_only_the_rows_that_see_them(q, kv, D, window, dtype):
+    """Some keys and values of the sequences are NaN or infinite: rows that do not see them equal those of
+    finite contents, rows that see a value of that kind have it in that dim, and NaN everywhere for a NaN key."""
+    c = Case(q, kv, 8, 2, D, 16, dtype, seed=D + window)
+    clean = cl.attention(c.cache, c.batch, c.q.cuda(), window=window, out_dtype=F32)
+    bad = [(0, kv[0] - 2, "v", float("inf"), 5), (0, kv[0] - q[0] // 2 - 1, "v", float("nan"), D - 1)]
+    bad += [(len(q) - 1, kv[-1] - 1, "k", float("nan"), 3), (0, max(0, kv[0] - q[0] - 10), "v", float("-inf"), 0)]
+    for b, j, what, x, dim in bad:
+        page = c.table[b, j // 16].long()
+        getattr(c.cache, what)[page, 1, j % 16, dim] = x                          # the second key head's
+    out = cl.attention(c.cache, c.batch, c.q.cuda(), window=window, out_dtype=F32)
+    torch.cuda.synchronize()
+    at = 0
+    for b, (a, n) in enumerate(zip(q, kv)):
+        for i in range(a):
+            p, row, ref = n - a + i, out[at + i].cpu(), clean[at + i].cpu()
+            touched = torch.zeros(8, D, dtype=torch.bool)
+            for bb, j, what, x, dim in bad:
+                if bb == b and j <= p and (not window or j > p - window):
+                    if what == "k":
+                        touched[4:] = True
+                        assert row[4:].isnan().all()
+                    else:
+                        touched[4:, dim] = True
+                        assert not row[4:, dim].isfinite().any()
+            assert torch.allclose(row[~touched], ref[~touched], rtol=2.0 ** -20, atol=2.0 ** -20), (b, i)
+        at += a
