@@ -613,7 +613,7 @@ cl_status cl_rope_frequencies(int32_t rot_dim, double base, int32_t kind, double
  * A token at a position below prefix_len (the shared pages are never
  * written), or below 0, is not stored; its query is rotated all the same.
  * Errors: CL_EINVAL for bad descriptors, null or misaligned pointers (2
- * bytes; 8 and strides of 4 take wider accesses), strides shorter than a
+ * bytes; 16 and strides of 8 elements take wider accesses), strides shorter than a
  * token's heads; CL_EUNSUPPORTED for a head_dim that the cache does not take.
  */
 cl_status cl_kv_append(const cl_kv_cache* cache, const cl_kv_batch* batch, const cl_rope* rope, const void* q,
@@ -747,8 +747,8 @@ typedef struct cl_norm {
  *  residual     device [T][d] of h_dtype, or NULL: none
  *  h            device [T][d] of h_dtype (may be residual), or NULL: not written
  *  out          device [T][d] of out_dtype; may not overlap an input
- * T >= 1; d 1..32768 (CL_EUNSUPPORTED beyond).  Any d and element alignment;
- * d a multiple of 8 with 16-byte aligned arrays takes wide accesses.
+ * T >= 1; d 1..32768 (CL_EUNSUPPORTED beyond); any d, arrays aligned to their
+ * elements.
  * Errors: CL_EINVAL, CL_EUNSUPPORTED, CL_EHIP.
  */
 cl_status cl_residual_norm(const cl_norm* norm, const void* y, int32_t y_dtype, int32_t slots,
