@@ -640,7 +640,7 @@ constexpr float kSlack = 6.f;
 // prompt 57.5 -> 54.9 us).  Sequences vary slowest: workgroups go to the shader
 // engines in turn, so a sequence without rows at every fourth place would leave
 // an engine idle (ragged prompts 858 -> 2122 us that way round).
-constexpr int tile_lds(int D) { return 4 * tile_keys(D) * D * 2 + 64; }
+constexpr int tile_lds(int D) { return 4 * tile_keys(D) * D * 2; }
 
 template <int D, bool BF, int NQ, bool PREFIX>
 __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int id, unsigned char* lds) {
@@ -688,7 +688,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
         full_lo = max(full_lo, __shfl_xor(full_lo, off, 64));
         full_hi = min(full_hi, __shfl_xor(full_hi, off, 64));
     }
-    int(*bounds)[4] = reinterpret_cast<int(*)[4]>(lds + 4 * TILE);
+    int(*bounds)[4] = reinterpret_cast<int(*)[4]>(lds);         // ahead of the first tile and behind the last
     if (lane == 0) bounds[0][wave] = lo, bounds[1][wave] = hi, bounds[2][wave] = full_lo, bounds[3][wave] = full_hi;
     __syncthreads();
     const int wlo = __builtin_amdgcn_readfirstlane(lo), whi = __builtin_amdgcn_readfirstlane(hi);
@@ -702,6 +702,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
     }
     all_lo = __builtin_amdgcn_readfirstlane(all_lo);
     all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+    __syncthreads();
     lo = __builtin_amdgcn_readfirstlane(max(lo, begin) & ~(KT - 1));
     hi = __builtin_amdgcn_readfirstlane(hi);
     full_lo = __builtin_amdgcn_readfirstlane(full_lo);
@@ -942,6 +943,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
         }
     }
     const bool found = __ballot(unseen) != 0;
+    __syncthreads();
     if (lane == 0) bounds[0][wave] = found;
     __syncthreads();
     const bool dirty = (bounds[0][0] | bounds[0][1] | bounds[0][2] | bounds[0][3]) != 0;
