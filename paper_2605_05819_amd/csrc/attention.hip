@@ -29,13 +29,13 @@
 //    V: each wave streams keys of its own, 32 at a time, K straight into
 //    operand registers, V through its own slice of LDS; nothing in the loop
 //    waits for another wave.  Four sequences of 100 k to 131 k keys, 4 tokens
-//    each: 355 us, 5.3 TB/s; 64 sequences of 1500 to 2500 keys 102 us, 4.9 TB/s.
+//    each: 356 us, 5.3 TB/s; 64 sequences of 1500 to 2500 keys 102 us, 4.9 TB/s.
 //  * attn_tile: more rows (prompts, a shared prefix under many sequences).
 //    Bound by the issue of MFMA and softmax instructions (per 32 rows x 64 keys
 //    and wave 64 MFMAs, 1024 cycles, and about 200 others, 900 cycles, of which
 //    two resident waves overlap half): four waves of 16 NQ rows share tiles of
 //    64 keys in LDS, double-buffered.  Prompts of up to 7001 tokens over 9001
-//    keys: 852 us, 1.01 PFLOP/s (a library product of 8192^3 runs at 1.21).
+//    keys: 858 us, 1.00 PFLOP/s (a library product of 8192^3 runs at 1.21).
 //
 // Rounding: probabilities enter the second product as the cache's type (2^-9 or
 // 2^-12 of each, at random, beside the output's own); sums, maxima, O and the
@@ -629,8 +629,11 @@ constexpr int tile_keys(int D) { return D > 128 ? 32 : 64; }
 // two buffers each, filled by direct copies to LDS that are issued a step
 // ahead.  A maximum within 2^kSlack of the one in use leaves it in use
 // (probabilities up to 2^kSlack; every result divides by their sum), which
-// saves nearly all rescaling.
-constexpr float kSlack = 6.f;
+// saves nearly all rescaling but rounds a row's largest probability, that a
+// current maximum makes exactly 1.  With a slack of 0, 3 and 6 ragged prompts
+// take 910, 878 and 870 us, and their error against 64 bits is 1.10, 1.16 and
+// 1.26 times that of one final rounding.
+constexpr float kSlack = 3.f;
 
 //
 // Blocks are numbered from the last row down: causal rows see more keys the
