@@ -839,6 +839,15 @@ class Rope:
         return self._bytes
 
 
+def _empty(shape, dtype, device, stream):
+    """A new tensor for work on ``stream`` (None: the current one): memory that
+    earlier work of another stream may still use is not handed to this one."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _token_rows(t, name, dtype, tokens, heads, dim):
     """[tokens][heads][dim] with a token's heads contiguous; the token stride."""
     if isinstance(t, torch.Tensor) and t.dtype == dtype and t.is_contiguous() and t.is_cuda:
@@ -872,7 +881,7 @@ def kv_append(cache, batch, k, v, q=None, rope=None, q_norm=None, k_norm=None, e
         qs = _token_rows(q, "q", dt, n, None, D)
         heads = q.shape[1]
         if q_out is None:
-            q_out = torch.empty((n, heads, D), dtype=dt, device=q.device)
+            q_out = _empty((n, heads, D), dt, q.device, stream)
         else:
             _dev_tensor(q_out, "q_out", (dt,), q.shape)
     if q_norm is not None:
@@ -908,14 +917,14 @@ def attention(cache, batch, q, scale=None, causal=True, window=0, out=None, out_
     qs = _token_rows(q, "q", cache.dtype, n, None, D)
     heads = q.shape[1]
     if out is None:
-        out = torch.empty((n, heads, D), dtype=out_dtype or q.dtype, device=q.device)
+        out = _empty((n, heads, D), out_dtype or q.dtype, q.device, stream)
     else:
         _dev_tensor(out, "out", _OUT, q.shape)
     if lse is not None:
         _dev_tensor(lse, "lse", (torch.float32,), (n, heads))
     if ws is None:
         need = _call("cl_attention_workspace")(cache._bytes, batch._bytes, heads)
-        ws = workspace(need, q.device) if need else None
+        ws = _empty((need,), torch.uint8, q.device, stream) if need else None
     else:
         _dev_tensor(ws, "ws", (torch.uint8,))
     _check(_call("cl_attention")(cache._bytes, batch._bytes, q.data_ptr(), qs, heads,
@@ -952,18 +961,18 @@ def moe_route(router, logits, expert_ranks=(), levels=(), ids=None, weights=None
     _need(logits.dim() == 2 and logits.shape[1] == router.num_experts, "logits must be [T][num_experts]")
     T, k = logits.shape[0], router.k
     if ids is None:
-        ids = torch.empty((T, k), dtype=torch.int32, device=logits.device)
+        ids = _empty((T, k), torch.int32, logits.device, stream)
     else:
         _dev_tensor(ids, "ids", _I32, (T, k))
     if weights is None:
-        weights = torch.empty((T, k), dtype=torch.float32, device=logits.device)
+        weights = _empty((T, k), torch.float32, logits.device, stream)
     else:
         _dev_tensor(weights, "weights", (torch.float32,), (T, k))
     n = len(expert_ranks)
     er = lv = sr = None
     if n:
         if slot_ranks is None:
-            slot_ranks = [torch.empty((T, k), dtype=torch.int32, device=logits.device) for _ in range(n)]
+            slot_ranks = [_empty((T, k), torch.int32, logits.device, stream) for _ in range(n)]
         _need(len(slot_ranks) == n, "one slot-rank table per expert-rank table")
         for i in range(n):
             _dev_tensor(expert_ranks[i], "expert_ranks[%d]" % i, _I32, (router.num_experts,))
@@ -1008,11 +1017,11 @@ def residual_norm(y, weight, residual=None, slot_weights=None, post_weight=None,
         _dev_tensor(residual, "residual", _OUT, (T, d))
         ht = residual.dtype
     if h is None:
-        h = torch.empty((T, d), dtype=ht, device=y.device)
+        h = _empty((T, d), ht, y.device, stream)
     elif h is not False:
         _dev_tensor(h, "h", (ht,), (T, d))
     if out is None:
-        out = torch.empty((T, d), dtype=out_dtype or ht, device=y.device)
+        out = _empty((T, d), out_dtype or ht, y.device, stream)
     else:
         _dev_tensor(out, "out", _OUT, (T, d))
     nb = _PACK_NORM(weight.data_ptr(), 0 if bias is None else bias.data_ptr(),

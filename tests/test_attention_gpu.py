@@ -290,3 +290,23 @@ def test_infinities_and_nan_reach_only_the_rows_that_see_them(q, kv, D, window, 
                         assert not row[4:, dim].isfinite().any()
             assert torch.allclose(row[~touched], ref[~touched], rtol=2.0 ** -20, atol=2.0 ** -20), (b, i)
         at += a
+
+
+def test_a_stream_of_its_own_beside_a_busy_one():
+    """Calls on another stream allocate for that stream: memory freed on the current one, where long work is
+    still queued that reads it, is not taken for their workspace or results."""
+    c = Case([1, 2, 1], [5000, 3000, 4000], 8, 2, 128, 16, F16)
+    q = c.q.cuda()
+    want = cl.attention(c.cache, c.batch, q, out_dtype=F32)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    big = torch.ones((4096, 4096), device="cuda")
+    for _ in range(5):
+        x = torch.full((cl.attention_workspace(c.cache, c.batch, 8) // 4,), 3.0, device="cuda")
+        for _ in range(20):
+            big = (big @ big).clamp_(max=1.0)
+        keep = x * 2                                   # queued behind the products
+        del x                                          # its memory is free for the current stream
+        got = cl.attention(c.cache, c.batch, q, out_dtype=F32, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and bool((keep == 6.0).all())
