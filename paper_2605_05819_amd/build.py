@@ -79,13 +79,14 @@ def sanitizer_runtime_dir():
 
 def build_ubsan(out_dir, verbose=False):
     """Build ``out_dir/libcl.so`` with undefined-behaviour checks on the host
-    code (every check fatal) and unoptimised device code."""
+    code (every check fatal).  Device code is compiled at -O1: at -O0 the compiler
+    does not keep uniform values in scalar registers, which some instructions need."""
     os.makedirs(out_dir, exist_ok=True)
     rt = sanitizer_runtime_dir()
     host = ["-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-fno-sanitize-recover=undefined",
             "-Xarch_host", "-fno-omit-frame-pointer"]
     flags = ["-O1", "-g", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH,
-             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Xarch_device", "-O0"] + host
+             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Xarch_device", "-O1"] + host
 
     def one(src):
         obj = os.path.join(out_dir, src.replace(".hip", ".o"))
