@@ -128,9 +128,11 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a, int step) 
     // the token's place: the same for the whole workgroup
     const int s = seq_of(a.batch, t);
     int pos = 0, page = -1, row = 0;
+    bool owned = false;                               // the token is some sequence's
     if (s >= 0) {
         const Seq q = load_seq(a.batch, s);
         if (t < q.start + q.count) {
+            owned = true;
             pos = q.keys - q.count + (t - q.start);
             const int mine = pos - a.batch.prefix_len;
             if (mine >= 0) {
@@ -207,7 +209,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a, int step) 
                 v.v[i + 1] = p * sn[2 + i / 2] + q * cs[2 + i / 2];
             }
         }
-        if (live && (is_q || stored)) {
+        if (live && (is_q ? owned : stored)) {
             store8<VEC, (HP > 1)>(dst, lo, hi, half, narrow(u, dt), narrow(v, dt));
         }
     }

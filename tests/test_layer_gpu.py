@@ -131,6 +131,32 @@ def test_append_skips_pages_outside_the_pool():
     assert torch.equal(cache.k.cpu(), kv0[0]) and torch.equal(cache.v.cpu(), kv0[1])
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("norm", [False, True])
+def test_append_leaves_rows_of_no_sequence_alone(norm, in_place):
+    """Tokens ahead of the first sequence, between q_start's last entry and the end, and past a start that was
+    cut: their queries are not written, and the caches hold nothing of them."""
+    cache, batch, _, kv0, q, k, v = _append_case([2, 3], [40, 50], 4, 2, 64, 16, F16)
+    g = np.random.default_rng(8)
+    pad = lambda t: torch.cat([rnd(g, (1, *t.shape[1:]), F16), t, rnd(g, (2, *t.shape[1:]), F16)]).cuda()  # noqa: E731
+    qd, kd, vd = pad(q), pad(k), pad(v)
+    wide = cl.KvBatch(batch.kv_len, batch.page_table, 8, q_len=3, q_start=i32([1, 3, 6]), max_kv_len=50)
+    args = dict(rope=cl.Rope(cl.rope_frequencies(64)[0].cuda()))
+    if norm:
+        args.update(q_norm=rnd(g, (64,), F16).cuda(), k_norm=rnd(g, (64,), F16).cuda())
+    want = cl.kv_append(cache, batch, k.cuda(), v.cuda(), q=q.cuda(), **args)
+    pools = cache.k.clone(), cache.v.clone()
+    cache.k.copy_(kv0[0]), cache.v.copy_(kv0[1])
+    for positions in (None, torch.full((8,), 5, dtype=torch.int32, device="cuda")):
+        out = qd.clone() if in_place else torch.full_like(qd, 7.0)
+        before = out.clone()
+        cl.kv_append(cache, wide, kd, vd, q=out if in_place else qd, q_out=out, positions=positions, **args)
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], before[0]) and torch.equal(out[6:], before[6:])
+        if positions is None:
+            assert torch.equal(out[1:6], want) and torch.equal(cache.k, pools[0]) and torch.equal(cache.v, pools[1])
+
+
 # ---------------------------------------------------------------------- route
 
 ROUTES = [
