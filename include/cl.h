@@ -664,7 +664,8 @@ enum { CL_SOFTMAX = 1, CL_SIGMOID = 2 };
  *  score       CL_SOFTMAX over all experts, or CL_SIGMOID of each
  *  groups      experts in `groups` (1..64) runs of equal length, of which the
  *              top_groups with the highest sum of their group_best (1 or 2)
- *              best biased scores stay open; 1 and 1 for none
+ *              best biased scores stay open (the one score of a group of one);
+ *              1 and 1 for none
  *  renormalize divide the chosen weights by their sum
  *  scale       factor of the weights at the end
  */

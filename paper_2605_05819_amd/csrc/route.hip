@@ -133,7 +133,7 @@ __global__ __launch_bounds__(256) void moe_route_kernel(RouteArgs a) {
         // lane g carries on for group g
         b1 = __shfl(b1, min(lane * per, 63), 64);
         b2 = __shfl(b2, min(lane * per, 63), 64);
-        uint32_t gk = lane < a.groups ? order_key(a.group_best == 2 ? b1 + b2 : b1) : kTaken;
+        uint32_t gk = lane < a.groups ? order_key(a.group_best == 2 && size > 1 ? b1 + b2 : b1) : kTaken;
         uint64_t open = 0;
         for (int j = 0; j < a.top_groups; ++j) {
             const uint32_t best = wave_max_u32(gk);

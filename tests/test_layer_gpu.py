@@ -198,6 +198,22 @@ def test_route_against_oracle(i):
             assert np.array_equal(table.cpu().numpy(), wl.dynamic_slot_ranks(ids, got[1].cpu().numpy(), x, levels, 32))
 
 
+@pytest.mark.parametrize("bias", [False, True], ids=["plain", "bias"])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,groups,top,k", [(64, 64, 8, 8), (64, 64, 9, 4), (7, 7, 3, 3), (48, 24, 5, 6)])
+def test_route_by_two_best_of_groups_of_one_and_two_experts(E, groups, top, k, score, bias):
+    """A group of one has one best score, which then is its sum."""
+    g = np.random.default_rng(E + top)
+    logits = rnd(g, (40, E), F32, 2.0)
+    b = rnd(g, (E,), F32, 0.1) if bias else None
+    ids, w = cl.moe_route(cl.Router(E, k, score, None if b is None else b.cuda(), groups, top, 2), logits.cuda())
+    torch.cuda.synchronize()
+    rid, rw, gap = layer.route(logits.double().numpy(), k, score, None if b is None else b.double().numpy(), groups, top, 2)
+    sure = gap > 1e-5
+    assert sure.mean() > 0.5 and np.array_equal(ids.cpu().numpy()[sure], rid[sure])
+    assert (np.abs(w.double().cpu().numpy() - rw)[sure] <= 4e-6 * np.abs(rw[sure]) + 1e-9).all()
+
+
 def test_route_ties_infinities_and_nan():
     E = 130
     x = torch.zeros((6, E))
