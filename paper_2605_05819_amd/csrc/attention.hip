@@ -378,9 +378,10 @@ __device__ __forceinline__ Segment prefix_segment(const AttnArgs& a) {
 constexpr int stream_lds(int D, int NQ) { return 256 * D + 512 * NQ + 16; }
 
 //
-// SAME: every row of a unit sees the same keys (one token a sequence and no
-// window), so only the last step has a mask and no value is hidden from a row
-// that its neighbours see.
+// SAME: every row of a unit sees the same keys, [0, hi) (one token a sequence and
+// no window), so only the last step has a mask and no value is hidden from a row
+// that its neighbours see.  Keys from hi on, which there are where a sequence
+// has more new tokens than are attended for, are taken as past the end.
 template <int D, bool BF, int NQ, bool PREFIX, bool SAME>
 __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, int id, unsigned char* lds) {
     constexpr int NS = D / 32, ND = D / 16, CH = D / 8;
@@ -452,7 +453,8 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
     u32x4 kr[2][NS], vr[CH / 2];
     constexpr int VR = CH / 2;                // 32 rows x CH chunks over 64 lanes
     // lane l looks up key l of a step; the lanes that load a row ask for it
-    const auto look = [&](int at) { return at + (lane & 31) < seg.keys ? pool_row(a, seg, head, at + (lane & 31)) : -2; };
+    const int there = SAME ? hi : seg.keys;
+    const auto look = [&](int at) { return at + (lane & 31) < there ? pool_row(a, seg, head, at + (lane & 31)) : -2; };
     const auto fetch = [&](int where) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -479,7 +481,7 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
     int at = lo + 32 * wave;
     if (at < hi) {
         // without a window the first step is the one looked up above
-        if (a.window == 0) fetch(at + (lane & 31) < seg.keys ? first : -2);
+        if (a.window == 0) fetch(at + (lane & 31) < there ? first : -2);
         else fetch(look(at));
         int next = look(at + 128);
         for (; at < hi; at += 128) {

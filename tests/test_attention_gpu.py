@@ -310,3 +310,29 @@ def test_a_stream_of_its_own_beside_a_busy_one():
         got = cl.attention(c.cache, c.batch, q, out_dtype=F32, stream=side)
         torch.cuda.synchronize()
         assert torch.equal(got, want) and bool((keep == 6.0).all())
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["fp16", "bf16"])
+@pytest.mark.parametrize("n", [2, 31, 32, 33, 64, 200, 3000])
+def test_tokens_past_q_len_hide_their_keys_from_the_one_attended(n, dtype):
+    """q_len 1 and a range of three tokens: the first alone is attended for, and it does not see the last two
+    keys, whose values (and one key) are infinite and NaN."""
+    c = Case([1], [n], 8, 2, 128, 16, dtype, seed=n)
+    room = torch.cat([c.table, torch.full((1, 2), -1, dtype=torch.int32, device="cuda")], 1)
+    used = set(room[0].tolist())
+    spare = [p for p in range(c.cache.num_pages) if p not in used]
+    for j, bad in ((n, float("nan")), (n + 1, float("inf"))):
+        if room[0, j // 16] < 0:
+            room[0, j // 16] = spare.pop()
+        page = room[0, j // 16].long()
+        c.cache.k[page, :, j % 16], c.cache.v[page, :, j % 16] = 1.0, bad
+    c.cache.k[page, 1, j % 16, 0] = float("nan")
+    b = cl.KvBatch(torch.tensor([n + 2], dtype=torch.int32, device="cuda"), room, 3, q_len=1,
+                   q_start=torch.tensor([0, 3], dtype=torch.int32, device="cuda"), max_kv_len=n + 2)
+    out = torch.full((3, 8, 128), 7.0, device="cuda")
+    cl.attention(c.cache, b, torch.cat([c.q, c.q * 2, c.q * 3]).cuda(), out=out)
+    torch.cuda.synchronize()
+    ref, _, A, most = c.oracle(128 ** -0.5, True, 0)
+    allow = A * (UNIT_ROUNDOFF[dtype] + 2.0 ** -24 * (2 * 128 * most + 2 * n + 16)[..., None] + 2.0 ** -21) * 1.01
+    allow = allow + (2.0 ** -25 * n * np.abs(c.vs[0]).max() if dtype == F16 else 0)
+    assert (np.abs(out_to_numpy(out[:1]) - ref) <= allow).all() and (out[1:] == 7).all()
