@@ -1087,9 +1087,10 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, Plan pl) {
 #pragma unroll
     for (int j = 0; j < kMaxSplits / 64; ++j)
         if (64 * j < live) {
-            // l = 0: no key seen there, whatever its sums hold
+            // l = 0: no key seen there, whatever its sums hold (weight -1); a
+            // weight that is 0 itself still counts, as sums may be infinite
             const bool used = 64 * j + lane < live && st[j].y != 0.f;
-            const float w = used ? __builtin_amdgcn_exp2f((st[j].x == -INFINITY ? base : st[j].x) - base) : 0.f;
+            const float w = used ? __builtin_amdgcn_exp2f((st[j].x == -INFINITY ? base : st[j].x) - base) : -1.f;
             if (tid < 64) weight[64 * j + lane] = w;
             l += used ? w * st[j].y : 0.f;
         }
@@ -1103,7 +1104,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, Plan pl) {
     for (int i = part; i < live; i += AT) {
         const float w = weight[i];
         const f32x4 v = from[i * step];
-        if (w != 0.f) acc += v * w;
+        if (w != -1.f) acc += v * w;
     }
     sums[part][at] = acc;
     __syncthreads();

@@ -336,3 +336,17 @@ def test_tokens_past_q_len_hide_their_keys_from_the_one_attended(n, dtype):
     allow = A * (UNIT_ROUNDOFF[dtype] + 2.0 ** -24 * (2 * 128 * most + 2 * n + 16)[..., None] + 2.0 ** -21) * 1.01
     allow = allow + (2.0 ** -25 * n * np.abs(c.vs[0]).max() if dtype == F16 else 0)
     assert (np.abs(out_to_numpy(out[:1]) - ref) <= allow).all() and (out[1:] == 7).all()
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("q_len,kv", [(1, 9000), (3, 9000), (40, 9000), (1100, 3000)])
+def test_seen_infinities_stay_in_results_of_split_keys(q_len, kv, bad):
+    """A value that is not finite among keys whose whole split is e^-1024 of another: its dim is not finite,
+    whichever kernel joins the splits."""
+    c = Case([q_len], [kv], 4, 1, 64, 16, BF16, seed=q_len, kstd=0.0)
+    j = torch.arange(kv - q_len, device="cuda")             # seen by every row
+    c.cache.k[c.table[0, j // 16].long(), 0, j % 16] = -16.0
+    c.cache.v[c.table[0, 0].long(), 0, 3, 11] = bad
+    out = cl.attention(c.cache, c.batch, torch.ones_like(c.q).cuda(), scale=1.0, out_dtype=F32)
+    torch.cuda.synchronize()
+    assert not out[:, :, 11].isfinite().any() and out[:, :, :11].isfinite().all() and out[:, :, 12:].isfinite().all()
