@@ -37,9 +37,11 @@
 //    64 keys in LDS, double-buffered.  Prompts of up to 7001 tokens over 9001
 //    keys: 858 us, 1.00 PFLOP/s (a library product of 8192^3 runs at 1.21).
 //
-// Rounding: probabilities enter the second product as the cache's type (2^-9 or
-// 2^-12 of each, at random, beside the output's own); sums, maxima, O and the
-// partial results are fp32, and l is summed from the unrounded probabilities.
+// Rounding: probabilities enter the second product as the cache's type, to
+// nearest (off by 2^-8 of each at most in bf16, 2^-11 in fp16, and there by 2^-37
+// of the row's largest where that is more; see kLift), beside the output's own rounding; sums,
+// maxima, O and the partial results are fp32, and l is summed from the unrounded
+// probabilities.
 
 #include "cl_device.h"
 #include "cl_internal.h"
@@ -69,6 +71,18 @@ __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
     else
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
+
+// Probabilities are formed as 2^kLift of themselves.  fp16 keeps 11 bits of a
+// number down to 2^-14 and none below 2^-25, so beside a row's largest (1; up to
+// 2^3 in tiles, see kSlack) a long tail of small ones would lose its mass,
+// always downward, while their sum l kept it.  2^12 keeps the largest below fp16's 65504 and
+// moves that edge to 2^-37 of it.  The lift is taken off O and l together at
+// the end of a unit, exactly, and takes no time (2048-token prompt 55.9 us without, 55.5
+// with).  bf16 has the range of fp32.
+template <bool BF>
+constexpr float kLift = BF ? 0.f : 12.f;
+template <bool BF>
+constexpr float kUnlift = BF ? 1.f : 1.f / 4096.f;
 
 // Two floats to two 16-bit values, round to nearest even (one instruction).
 template <bool BF>
@@ -203,7 +217,8 @@ __device__ __forceinline__ void load_q(const AttnArgs& a, const Row& r, int head
 
 // Running softmax of one row block over KB 16-key blocks of scores: s becomes
 // probabilities (packed into p), m and l move on, o and l are rescaled if the
-// maximum rose.  sc > 0 is |scale| log2 e; m is in the scores' own units.
+// maximum rose.  sc > 0 is |scale| log2 e; m is in the scores' own units; p, l and
+// o carry the lift.
 template <int KB, int ND, bool BF>
 __device__ __forceinline__ void softmax_step(f32x4 (&s)[KB], uint32_t (&p)[KB][2], float sc, float& m, float& l,
                                              f32x4 (&o)[ND]) {
@@ -211,9 +226,9 @@ __device__ __forceinline__ void softmax_step(f32x4 (&s)[KB], uint32_t (&p)[KB][2
 #pragma unroll
     for (int k = 0; k < KB; ++k) mx = larger(mx, s[k]);
     mx = row_max(mx);
-    const float mc = mx == -INFINITY ? 0.f : mx * sc;
+    const float mc = mx == -INFINITY ? 0.f : mx * sc - kLift<BF>;
     if (__ballot(mx > m)) {
-        const float old = m == -INFINITY ? mc : m * sc;
+        const float old = m == -INFINITY ? mc : m * sc - kLift<BF>;
         const float c = __builtin_amdgcn_exp2f(old - mc);
         l *= c;
 #pragma unroll
@@ -243,8 +258,9 @@ __device__ __forceinline__ void store4(const AttnArgs& a, size_t at, f32x4 v) {
     }
 }
 
-// Results of a row block (m in bits): o[d] holds dims 16 d + 4 g + 0..3 of the lane's row.
-template <int ND>
+// Results of a row block (m in bits, l without the lift): o[d] holds dims
+// 16 d + 4 g + 0..3 of the lane's row, with it.
+template <int ND, bool BF>
 __device__ __forceinline__ void finish(const AttnArgs& a, const Plan& pl, int slot, const Row& r, int head, float m,
                                        float l, const f32x4 (&o)[ND]) {
     if (r.token < 0) return;
@@ -255,11 +271,11 @@ __device__ __forceinline__ void finish(const AttnArgs& a, const Plan& pl, int sl
         const size_t at = static_cast<size_t>(slot) * a.batch.tokens * a.q_heads + row;
         float* to = pl.part + at * D + 4 * g;
 #pragma unroll
-        for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4*>(to + 16 * d) = o[d];
+        for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4*>(to + 16 * d) = o[d] * kUnlift<BF>;
         if (g == 0) pl.stat[at] = float2{m, l};
         return;
     }
-    const float inv = l != 0.f ? 1.0f / l : 0.f;
+    const float inv = l != 0.f ? kUnlift<BF> / l : 0.f;
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
         store4(a, row * D + 16 * d + 4 * g, l != 0.f ? o[d] * inv : f32x4{0.f, 0.f, 0.f, 0.f});
@@ -549,14 +565,18 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
         float mm = -INFINITY;
 #pragma unroll
         for (int w = 0; w < 4; ++w) mm = fmaxf(mm, stat[w][16 * n + col].x);
-        const float mc = mm == -INFINITY ? 0.f : mm * sc;
+        // what the lifted sums are multiples of: the exponent that softmax_step took off
+        const auto taken = [&](float t) { return t * sc - kLift<BF>; };
+        const float mc = mm == -INFINITY ? 0.f : taken(mm);
+        const float top = mm == -INFINITY ? -INFINITY : mc + kLift<BF>;
         float ll = 0.f;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const float2 t = stat[w][16 * n + col];
-            if (t.x != -INFINITY || t.y != 0.f) ll += t.y * __builtin_amdgcn_exp2f((t.x == -INFINITY ? mc : t.x * sc) - mc);
+            if (t.x != -INFINITY || t.y != 0.f) ll += t.y * __builtin_amdgcn_exp2f((t.x == -INFINITY ? mc : taken(t.x)) - mc);
         }
-        const float c = __builtin_amdgcn_exp2f((m[n] == -INFINITY ? mc : m[n] * sc) - mc);
+        ll *= kUnlift<BF>;
+        const float c = __builtin_amdgcn_exp2f((m[n] == -INFINITY ? mc : taken(m[n])) - mc) * kUnlift<BF>;
         if (n) __syncthreads();
 #pragma unroll
         for (int d = 0; d < ND; ++d)
@@ -583,7 +603,7 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
 #pragma unroll
             for (int j = 0; j < PER; ++j)
                 *reinterpret_cast<f32x4*>(pl.part + at2 * D + 16 * (wave * PER + j) + 4 * g4) = r[j];
-            if (g4 == 0 && wave == 0) pl.stat[at2] = float2{mm * sc, ll};
+            if (g4 == 0 && wave == 0) pl.stat[at2] = float2{top, ll};
         } else {
             const float inv = ll != 0.f ? 1.0f / ll : 0.f;
 #pragma unroll
@@ -591,7 +611,7 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
                 store4(a, rw * D + 16 * (wave * PER + j) + 4 * g4, ll != 0.f ? r[j] * inv : f32x4{0.f, 0.f, 0.f, 0.f});
             }
             if (a.lse && g4 == 0 && wave == 0)
-                a.lse[rw] = ll != 0.f ? (mm * sc + __builtin_amdgcn_logf(ll)) * kLn2 : -INFINITY;
+                a.lse[rw] = ll != 0.f ? (top + __builtin_amdgcn_logf(ll)) * kLn2 : -INFINITY;
         }
     }
 }
@@ -714,7 +734,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
     full_hi = __builtin_amdgcn_readfirstlane(full_hi);
     const float sc = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f;
 
-    float m[NQ], mc[NQ], l[NQ];                       // mc = m sc, 0 before any key
+    float m[NQ], mc[NQ], l[NQ];                       // mc = m sc - lift, 0 before any key
     f32x4 o[NQ][ND], s[NQ][KB];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
@@ -813,12 +833,12 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
         bool rose = false;
 #pragma unroll
         for (int n = 0; n < NQ; ++n)
-            rose |= m[n] == -INFINITY ? mx[n] != -INFINITY : mx[n] * sc > mc[n] + kSlack;
+            rose |= m[n] == -INFINITY ? mx[n] != -INFINITY : mx[n] * sc > mc[n] + (kLift<BF> + kSlack);
         if (__ballot(rose)) {
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
                 const float top = fmaxf(mx[n], m[n]);
-                const float now = top == -INFINITY ? 0.f : top * sc;
+                const float now = top == -INFINITY ? 0.f : top * sc - kLift<BF>;
                 const float c = m[n] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mc[n] - now);
                 m[n] = top;
                 mc[n] = now;
@@ -957,7 +977,8 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
         if (dirty)
             for (int at = lo; at < hi; at += KT)
                 if (hides(at)) add_not_finite<D, BF>(a, seg, head, row[n], at, min(at + KT, hi), 0, o[n]);
-        finish<ND>(a, pl, PREFIX ? split : pl.psplits + split, row[n], hidx[n], m[n] == -INFINITY ? -INFINITY : mc[n], row_sum(l[n]), o[n]);
+        finish<ND, BF>(a, pl, PREFIX ? split : pl.psplits + split, row[n], hidx[n], m[n] == -INFINITY ? -INFINITY : mc[n] + kLift<BF>,
+                       row_sum(l[n]) * kUnlift<BF>, o[n]);
     }
 }
 

@@ -350,3 +350,60 @@ def test_seen_infinities_stay_in_results_of_split_keys(q_len, kv, bad):
     out = cl.attention(c.cache, c.batch, torch.ones_like(c.q).cuda(), scale=1.0, out_dtype=F32)
     torch.cuda.synchronize()
     assert not out[:, :, 11].isfinite().any() and out[:, :, :11].isfinite().all() and out[:, :, 12:].isfinite().all()
+
+
+class Tail:
+    """One sequence of n keys of one head, of which every `every`-th from the first is a sink that all queries
+    score 0, and the others -low to -high; values of one sign, 0 at the sinks."""
+
+    def __init__(self, a, n, every, low, high, D, dtype, prefix=0):
+        g = np.random.default_rng(n + a + D)
+        sink = np.arange(n) % every == 0
+        k = np.zeros((n, D))
+        k[:, 0] = np.where(sink, 0.0, -g.uniform(low, high, n))
+        v = np.where(sink[:, None], 0.0, g.uniform(0.5, 1.0, (n, D)))
+        k, v = (torch.from_numpy(x).to(dtype) for x in (k, v))
+        self.a, self.n, self.sinks = a, n, sink
+        q = torch.zeros((a, 1, D), dtype=dtype)
+        q[:, :, 0] = 1.0
+        page, pages = 64, -(-n // 64)
+        pool = torch.zeros((2, pages * page, D), dtype=dtype)
+        pool[0, :n], pool[1, :n] = k, v
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+        self.cache = cl.KvCache(*(x.view(pages, 1, page, D).cuda() for x in pool))
+        table = torch.arange(pages, dtype=torch.int32, device="cuda")
+        shared = prefix // page
+        self.batch = cl.KvBatch(i32([n]), table[None, shared:].contiguous(), a, q_len=a, max_kv_len=n,
+                                prefix_table=table[:shared].contiguous() if shared else None, prefix_len=shared * page)
+        self.q, self.k, self.v = q, k.double().numpy(), v.double().numpy()
+
+    def check(self, dtype):
+        lse = torch.empty((self.a, 1), device="cuda")
+        out = cl.attention(self.cache, self.batch, self.q.cuda(), scale=1.0, out_dtype=F32, lse=lse)
+        torch.cuda.synchronize()
+        for i in sorted({0, self.a // 2, self.a - 1}):
+            see = self.n - self.a + i + 1
+            p = np.exp(self.k[:see, 0])
+            want = p @ self.v[:see] / p.sum()
+            # every p once by the type's unit, or in fp16 by 2^-25 of 2^-12 of the maximum (1, and one sink at least
+            # is in the sum); scores of one exact product; a lane sums see / 4 terms at most
+            allow = want * (UNIT_ROUNDOFF[dtype] + 2.0 ** -24 * (see / 4 + 64)) * 1.01
+            if dtype == F16:
+                allow = allow + 2.0 ** -37 * see / self.sinks[:see].sum()
+            err = np.abs(out[i, 0].double().cpu().numpy() - want)
+            assert (err <= allow).all(), (i, (err / allow).max(), (err / want).max())
+            assert abs(lse[i, 0].item() - np.log(p.sum())) <= 2.0 ** -24 * (see / 4 + 64)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["fp16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("a,n", [(1, 1000), (2, 1000), (20, 1000), (40, 1500), (300, 700), (700, 2100)])
+def test_small_probabilities_beside_sinks_keep_their_mass(a, n, D, dtype):
+    """Keys at e^-17 to e^-20 of the largest, in every wave's share a sink: single tokens, a few, tiles of 64 and
+    128 rows, in one split and in several."""
+    Tail(a, n, 32, 17.0, 20.0, D, dtype).check(dtype)
+
+
+@pytest.mark.parametrize("a,prefix", [(1, 0), (24, 0), (40, 0), (1, 1024), (40, 1024)])
+def test_one_sink_over_a_long_diffuse_tail(a, prefix):
+    Tail(a, 100001, 100001, 17.0, 19.0, 64, F16, prefix).check(F16)
