@@ -19,10 +19,12 @@ namespace cl {
 namespace {
 
 // Keys: larger for larger floats; every number is at least 0x007fffff (-inf).
-constexpr uint32_t kTaken = 0, kClosed = 1, kNaN = 2;
+// A NaN logit stands behind a NaN score: one NaN logit makes every score of a
+// softmax NaN, and it is still the last to be chosen.
+constexpr uint32_t kTaken = 0, kClosed = 1, kNaN = 2, kNaNScore = 3;
 
-__device__ __forceinline__ uint32_t order_key(float v) {
-    if (v != v) return kNaN;
+__device__ __forceinline__ uint32_t order_key(float v, uint32_t nan = kNaN) {
+    if (v != v) return nan;
     const uint32_t u = __builtin_bit_cast(uint32_t, v + 0.0f);   // -0 compares equal to 0
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
@@ -90,7 +92,7 @@ __global__ __launch_bounds__(256) void moe_route_kernel(RouteArgs a) {
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
             const int e = 64 * i + lane;
-            if (e < a.E) key[i] = order_key(p[i] + a.bias[e]);
+            if (e < a.E && key[i] != kNaN) key[i] = order_key(p[i] + a.bias[e], kNaNScore);
         }
     }
 
@@ -103,7 +105,7 @@ __global__ __launch_bounds__(256) void moe_route_kernel(RouteArgs a) {
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
             const uint32_t u = key[i];
-            const float v = u == kNaN ? -INFINITY
+            const float v = u <= kNaNScore ? -INFINITY
                             : scores  ? p[i]
                                       : __builtin_bit_cast(float, u & 0x80000000u ? u & 0x7fffffffu : ~u);
             c[64 * i + lane] = v;

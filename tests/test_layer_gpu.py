@@ -238,6 +238,21 @@ def test_route_ties_infinities_and_nan():
     assert ids[0].tolist() == [3, 1, 2, 0]                     # NaN last, -inf before it
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("at", [0, 3, 129])
+def test_route_with_a_bias_takes_a_nan_logit_last(at, score):
+    """By softmax every score is NaN then, and equal in that: the lower ids, and the NaN logit behind them all."""
+    x = torch.linspace(2.0, -2.0, 130).repeat(2, 1)
+    x[0, at] = math.nan
+    bias = torch.zeros(130)
+    want = [e for e in range(130) if e != at]
+    ids, w = cl.moe_route(cl.Router(130, 6, score, bias.cuda()), x.cuda())
+    some, _ = cl.moe_route(cl.Router(5, 5, score, bias[:5].cuda()), x[:1, [at, 7, 8, 9, 10]].cuda())
+    torch.cuda.synchronize()
+    assert ids[0].tolist() == want[:6] and ids[1].tolist() == [0, 1, 2, 3, 4, 5] and some[0].tolist() == [1, 2, 3, 4, 0]
+    assert w[0].isnan().all() if score == "softmax" else w[0].isfinite().all()
+
+
 def test_route_scores_are_the_plain_ones_bit_for_bit():
     """The biased choice compares fp32 sums, so ids agree with torch's where its operations round alike."""
     g = torch.Generator(device="cuda").manual_seed(3)
