@@ -68,8 +68,10 @@ class Dense:
 @dataclass
 class Experts:
     """The routed experts of a MoE layer.  ``router`` [experts][hidden] is the
-    (unquantized) routing weight in the activations' dtype; with ``levels`` the
-    slots' ranks follow their routing weights (the expert-activation term)."""
+    (unquantized) routing weight in the activations' dtype; its logits stay in
+    fp32, since 16 bits would tie many and decide those by the lower id.  With
+    ``levels`` the slots' ranks follow their routing weights (the
+    expert-activation term)."""
     router: torch.Tensor
     rule: cl.Router
     gate: cl.MoeExperts
@@ -80,7 +82,7 @@ class Experts:
     def __call__(self, n):
         if n.shape[0] > DECODE_TOKENS:
             raise ValueError("a MoE layer takes at most %d tokens a step" % DECODE_TOKENS)
-        logits = n @ self.router.t()
+        logits = torch.mm(n, self.router.t(), out_dtype=torch.float32)
         projections = (self.gate, self.up, self.down)
         if self.levels:
             ids, weights, ranks = cl.moe_route(self.rule, logits, [p.ranks for p in projections], self.levels)

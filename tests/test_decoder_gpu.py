@@ -157,3 +157,23 @@ def test_captured_decode_step_replays_like_the_eager_one(moe):
         torch.cuda.synchronize()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
         assert all(torch.equal(a, b) for a, b in ((caches[0].k, caches[1].k), (caches[0].v, caches[1].v)))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["fp16", "bf16"])
+def test_experts_are_chosen_by_unrounded_logits(dtype):
+    """Logits of 64 and 64 + 2^-6, which 16 bits cannot tell apart: the larger one decides, not the lower id."""
+    E, hidden, ffn = 8, 256, 128
+    router = torch.zeros((E, hidden))
+    router[2], router[5] = 0.25, 0.25
+    router[5, 17] += 2.0 ** -6
+    gate, og, ranks = _experts(E, ffn, hidden, 300)
+    up, ou, _ = _experts(E, ffn, hidden, 301)
+    down, od, _ = _experts(E, hidden, ffn, 302)
+    block = decoder.Experts(router.to(dtype).cuda(), cl.Router(E, 1), gate, up, down)
+    n = torch.ones((3, hidden), dtype=dtype, device="cuda")
+    y, w = block(n)
+    torch.cuda.synchronize()
+    ids = np.full((3, 1), 5)
+    g, u = (omoe.forward(p, ranks, n.double().cpu().numpy(), ids, False) for p in (og, ou))
+    want = omoe.forward(od, ranks, olin.silu(g) * u, ids, True)
+    assert rel_l2(y.double().cpu().numpy(), want) <= 1e-2 and (w == 1).all()
