@@ -60,8 +60,10 @@ class Dense:
         if n.shape[0] <= DECODE_TOKENS:
             g = cl.linear_decode_glu([self.gate.w, self.up.w], [self.gate.c, self.up.c], n, n.dtype)
         else:
-            g, u = window([self.gate, self.up], n, n.dtype)
-            g = torch.nn.functional.silu(g).mul_(u)
+            # fp32 as in the decode call's epilogue: one rounding, of the product (a
+            # 2048-token block of 14336 takes 886 us so, 833 with g and u in 16 bits)
+            g, u = window([self.gate, self.up], n, torch.float32)
+            g = torch.mul(torch.nn.functional.silu(g, inplace=True), u, out=torch.empty_like(g, dtype=n.dtype))
         return linear(self.down, g, n.dtype), None
 
 

@@ -177,3 +177,19 @@ def test_experts_are_chosen_by_unrounded_logits(dtype):
     g, u = (omoe.forward(p, ranks, n.double().cpu().numpy(), ids, False) for p in (og, ou))
     want = omoe.forward(od, ranks, olin.silu(g) * u, ids, True)
     assert rel_l2(y.double().cpu().numpy(), want) <= 1e-2 and (w == 1).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["fp16", "bf16"])
+@pytest.mark.parametrize("tokens", [65, 200])
+def test_gated_activation_is_rounded_once(tokens, dtype, monkeypatch):
+    """SiLU(g) u of a prompt, as the decode call does: one rounding of the fp32 value (2^-20 of it for fp32 itself)."""
+    ls = [_linear(FFN, HIDDEN, 200)[0], _linear(FFN, HIDDEN, 201)[0]]
+    x = torch.from_numpy(np.random.default_rng(4).standard_normal((tokens, HIDDEN))).to(dtype).cuda()
+    monkeypatch.setattr(decoder, "linear", lambda lin, a, out_dtype: a)
+    got, none = decoder.Dense(*ls, None)(x)
+    g, u = (t.double() for t in decoder.window(ls, x, torch.float32))
+    torch.cuda.synchronize()
+    want = g / (1 + torch.exp(-g)) * u
+    u16 = 2.0 ** (-11 if dtype == torch.float16 else -8)
+    assert none is None and got.dtype == dtype
+    assert ((got.double() - want).abs() <= (u16 + 2.0 ** -20) * want.abs() + 2.0 ** -25).all()
