@@ -643,7 +643,9 @@ cl_status cl_kv_append(const cl_kv_cache* cache, const cl_kv_batch* batch, const
  * Scores, softmax statistics and sums are float32; the probabilities enter the
  * second product as the cache's dtype.  Results do not depend on the order
  * in which workgroups run.
- * Errors: CL_EINVAL, CL_EUNSUPPORTED (head_dim), CL_EWORKSPACE, CL_EHIP.
+ * Errors: CL_EINVAL; CL_EUNSUPPORTED for a head_dim that the cache does not
+ * take, and where tokens * q_heads, or the launch (about
+ * num_seqs * q_len * q_heads / 64 workgroups), reaches 2^31; CL_EWORKSPACE, CL_EHIP.
  */
 cl_status cl_attention(const cl_kv_cache* cache, const cl_kv_batch* batch, const void* q, int64_t q_stride,
                        int32_t q_heads, float scale, int32_t causal, int32_t window, void* out, int32_t out_dtype,

@@ -616,7 +616,8 @@ size_t cl_attention_workspace(const cl_kv_cache* cache, const cl_kv_batch* batch
     cl::KvCache c;
     cl::KvBatch b;
     size_t bytes = 0;
-    if (check_kv(cache, batch, &c, &b, "") == CL_OK && q_heads >= c.heads && q_heads % c.heads == 0)
+    if (check_kv(cache, batch, &c, &b, "") == CL_OK && q_heads >= c.heads && q_heads % c.heads == 0 &&
+        cl::attention_size_ok(c, b, q_heads))
         bytes = cl::attention_workspace_bytes(c, b, q_heads);
     memcpy(g_err, saved, sizeof(g_err));
     return bytes;
@@ -636,8 +637,9 @@ cl_status cl_attention(const cl_kv_cache* cache, const cl_kv_batch* batch, const
         return fail(CL_EINVAL, "%s: q rows and out must be 16-byte aligned", who);
     if (q_stride < static_cast<int64_t>(q_heads) * cache->head_dim)
         return fail(CL_EINVAL, "%s: q_stride is shorter than a token's heads", who);
-    if (static_cast<long long>(batch->tokens) * q_heads > 0x7fffffffll)
-        return fail(CL_EUNSUPPORTED, "%s: tokens * q_heads must be below 2^31", who);
+    if (!cl::attention_size_ok(a.cache, a.batch, q_heads))
+        return fail(CL_EUNSUPPORTED, "%s: rows (tokens * q_heads) and workgroups (num_seqs * q_len * q_heads / 64) must be below 2^31",
+                    who);
     if (!isfinite(scale)) return fail(CL_EINVAL, "%s: scale must be finite", who);
     if (window < 0) return fail(CL_EINVAL, "%s: window must not be negative", who);
     if (!out_type(out_dtype)) return fail(CL_EINVAL, "%s: out_dtype must be CL_FP16, CL_BF16 or CL_FP32", who);

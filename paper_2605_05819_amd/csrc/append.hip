@@ -101,7 +101,7 @@ __device__ __forceinline__ Raw narrow(const Quad& q, int dt) {
 // of 8 (LG lanes of 8 values cover a head).
 template <int LG, bool VEC, int HP>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a, int step) {
-    const int t = blockIdx.x;
+    const int t = static_cast<int>(a.first + blockIdx.x);
     const int lane = threadIdx.x % LG;
     const int first = blockIdx.y * (blockDim.x / LG) + threadIdx.x / LG;
     const int D = a.cache.dim, dt = a.cache.dtype;
@@ -216,14 +216,14 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a, int step) 
 }
 
 template <int LG, int HP>
-hipError_t launch(const AppendArgs& a, bool vec, int blocks, hipStream_t st) {
-    const dim3 grid(a.batch.tokens, blocks);
+hipError_t launch(AppendArgs a, bool vec, int blocks, hipStream_t st) {
     const int step = blocks * (256 / LG);
-    if (vec)
-        hipLaunchKernelGGL((kv_append_kernel<LG, true, HP>), grid, dim3(256), 0, st, a, step);
-    else
-        hipLaunchKernelGGL((kv_append_kernel<LG, false, HP>), grid, dim3(256), 0, st, a, step);
-    return hipGetLastError();
+    return launch_all(a.batch.tokens, [&](unsigned first, unsigned count) {
+        a.first = first;
+        const dim3 grid(count, blocks);
+        if (vec) hipLaunchKernelGGL((kv_append_kernel<LG, true, HP>), grid, dim3(256), 0, st, a, step);
+        else hipLaunchKernelGGL((kv_append_kernel<LG, false, HP>), grid, dim3(256), 0, st, a, step);
+    });
 }
 
 // A lane group takes one head where workgroups are few (latency) and up to

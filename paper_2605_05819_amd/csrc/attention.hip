@@ -139,6 +139,7 @@ struct Plan {
     int splits, len;       // of a sequence's own keys: splits of `len` keys
     int pblocks, psplits, plen;      // of the shared prefix, whose unit has every token's rows
     int pgrid;             // workgroups of the prefix, ahead of the others
+    unsigned first;        // workgroup (of a join's kernels too) that the launch begins with
     int paired;            // order of the row blocks (see attn_tile)
     int direct;            // one split and no prefix: results go straight to out
     float* part;           // [psplits + splits][tokens * q_heads][dim], unnormalised
@@ -991,7 +992,7 @@ template <int D>
 __global__ __launch_bounds__(256) void attn_join_rows_kernel(AttnArgs a, Plan pl) {
     constexpr int LANES = D / 4, AT = 256 / LANES;
     const size_t rows = static_cast<size_t>(a.batch.tokens) * a.q_heads;
-    const size_t row = static_cast<size_t>(blockIdx.x) * AT + threadIdx.x / LANES;
+    const size_t row = static_cast<size_t>(pl.first + blockIdx.x) * AT + threadIdx.x / LANES;
     const int at = threadIdx.x % LANES, total = pl.psplits + pl.splits;
     if (row >= rows) return;
     float2 st[kRowSplits];
@@ -1052,7 +1053,7 @@ template <int D, bool BF, int P, int O>
 __global__ __launch_bounds__(256, (O <= S2 || O == S0) && D > 128 ? 1 : P == NONE && O == S0 ? 3 : 2) void attn_kernel(
     AttnArgs a, Plan pl) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    const int id = static_cast<int>(blockIdx.x);
+    const int id = static_cast<int>(pl.first + blockIdx.x);
     if constexpr (P != NONE) {
         if (id < pl.pgrid) {
             if constexpr (P <= S2) attn_stream<D, BF, P, true, false>(a, pl, id, lds);
@@ -1081,7 +1082,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, Plan pl) {
     __shared__ f32x4 sums[AT][LANES];
     const int tid = threadIdx.x, lane = tid & 63;
     const size_t rows = static_cast<size_t>(a.batch.tokens) * a.q_heads;
-    const size_t row = blockIdx.x;
+    const size_t row = pl.first + blockIdx.x;
     const int t = static_cast<int>(row / a.q_heads);
     const int total = pl.psplits + pl.splits;
     // the statistics of every split, read ahead of the length that says which count
@@ -1210,7 +1211,6 @@ hipError_t launch(const AttnArgs& a, Plan p, hipStream_t st) {
     const long long pgrid = static_cast<long long>(a.cache.heads) * p.psplits * p.pblocks;
     const int places = O <= S2 || O == S0 ? p.splits | 1 : p.splits;
     const long long grid = pgrid + static_cast<long long>(a.cache.heads) * places * p.blocks * a.batch.num_seqs;
-    if (grid > 0x7fffffffll) return hipErrorInvalidConfiguration;
     p.pgrid = static_cast<int>(pgrid);
     constexpr int bytes = lds_bytes(D, P) > lds_bytes(D, O) ? lds_bytes(D, P) : lds_bytes(D, O);
     if (bytes > 65536) {
@@ -1218,15 +1218,17 @@ hipError_t launch(const AttnArgs& a, Plan p, hipStream_t st) {
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((attn_kernel<D, BF, P, O>), dim3(static_cast<unsigned>(grid)), dim3(256), bytes, st, a, p);
-    return hipGetLastError();
+    return launch_all(grid, [&](unsigned first, unsigned count) {
+        p.first = first;
+        hipLaunchKernelGGL((attn_kernel<D, BF, P, O>), dim3(count), dim3(256), bytes, st, a, p);
+    });
 }
 
 // The prefix's unit has at least as many rows as a sequence's, so these
 // combinations cover every call (a tiled prefix takes 128-row tiles, a streamed
 // one of 17 to 32 rows streams the sequences' likewise).
 template <int D, bool BF>
-hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t st) {
+hipError_t run(const AttnArgs& a, Plan p, hipStream_t st) {
     const long long prows = static_cast<long long>(a.batch.tokens) * (a.q_heads / a.cache.heads);
     int own = kind_of(a.cache, a.batch, p.rows);
     if (own == S1 && a.batch.q_len == 1 && a.window == 0) own = S0;
@@ -1261,16 +1263,32 @@ hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t st) {
     const size_t rows = static_cast<size_t>(a.batch.tokens) * a.q_heads;
     if (p.psplits + p.splits <= kRowSplits && rows >= 4096) {
         constexpr size_t at = 1024 / D;
-        hipLaunchKernelGGL((attn_join_rows_kernel<D>), dim3(static_cast<unsigned>((rows + at - 1) / at)), dim3(256), 0, st, a, p);
-        return hipGetLastError();
+        return launch_all(static_cast<long long>((rows + at - 1) / at), [&](unsigned first, unsigned count) {
+            p.first = first;
+            hipLaunchKernelGGL((attn_join_rows_kernel<D>), dim3(count), dim3(256), 0, st, a, p);
+        });
     }
-    hipLaunchKernelGGL((attn_join_kernel<D>), dim3(static_cast<unsigned>(rows)), dim3(256), 0, st, a, p);
-    return hipGetLastError();
+    return launch_all(static_cast<long long>(rows), [&](unsigned first, unsigned count) {
+        p.first = first;
+        hipLaunchKernelGGL((attn_join_kernel<D>), dim3(count), dim3(256), 0, st, a, p);
+    });
 }
 
 }  // namespace
 
 bool attention_dim_ok(int dim) { return dim == 64 || dim == 128 || dim == 256; }
+
+// Row and workgroup numbers are 32-bit.  A sequence has workgroups for q_len
+// tokens whatever it holds, so many sequences beside one long prompt reach the
+// second limit first (2^63 is out of reach: heads times blocks is at most the
+// rows, as far as the first one holds).
+bool attention_size_ok(const KvCache& c, const KvBatch& b, int q_heads) {
+    constexpr long long most = 0x7fffffffll;
+    if (static_cast<long long>(b.tokens) * q_heads > most) return false;
+    const Plan p = make_plan(c, b, q_heads);
+    const long long units = static_cast<long long>(c.heads) * p.blocks * b.num_seqs;
+    return units <= most && units * (p.splits | 1) + static_cast<long long>(c.heads) * p.psplits * p.pblocks <= most;
+}
 
 size_t attention_workspace_bytes(const KvCache& c, const KvBatch& b, int q_heads) {
     const Plan p = make_plan(c, b, q_heads);

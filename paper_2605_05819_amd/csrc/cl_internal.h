@@ -64,6 +64,21 @@ hipError_t launch_moe_decode(int n, const QW* w, const uint16_t* const* A, const
 // stream, returns the record in *word (0: none) and clears it.
 hipError_t moe_take_routing_error(hipStream_t st, unsigned long long* word);
 
+// Launches of n < 2^31 workgroups of up to 1024 work items each.  HIP takes less
+// than 2^32 work items along a dimension, so there is a launch for every 2^21
+// workgroups: launch(first, count), `count` of them from number `first` on.
+// (A second grid dimension instead costs every launch 0.15 us.)
+template <class F>
+hipError_t launch_all(long long n, F launch) {
+    constexpr long long kMost = 1ll << 21;
+    for (long long first = 0; first < n; first += kMost) {
+        launch(static_cast<unsigned>(first), static_cast<unsigned>(n - first < kMost ? n - first : kMost));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 // Paged keys and values, validated: [num_pages][heads][page_size][dim] each,
 // page_size = 1 << page_shift.
 struct KvCache {
@@ -100,6 +115,7 @@ struct AppendArgs {
     long long q_stride, k_stride, v_stride;
     int q_heads;
     float eps;
+    unsigned first;                // token of the launch's first workgroup
 };
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t st);
 void rope_frequencies(int rot_dim, double base, int kind, double factor, double trained_len, double low, double high,
@@ -117,6 +133,7 @@ struct AttnArgs {
     float* lse;                    // may be null
 };
 bool attention_dim_ok(int dim);
+bool attention_size_ok(const KvCache& c, const KvBatch& b, int q_heads);   // every number of the launch fits
 size_t attention_workspace_bytes(const KvCache& c, const KvBatch& b, int q_heads);
 hipError_t launch_attention(const AttnArgs& a, void* ws, hipStream_t st);
 
@@ -145,8 +162,9 @@ struct RouteArgs {
     int tables, nlevels;
     int T, E, k, dtype, sigmoid, groups, top_groups, group_best, renormalize;
     float scale;
+    unsigned first;                // the launch's first workgroup
 };
-hipError_t launch_moe_route(const RouteArgs& a, hipStream_t st);
+hipError_t launch_moe_route(RouteArgs a, hipStream_t st);
 
 // Rank allocation (host code, ranks.hip): salient-set size and salience
 // ratio of one descending spectrum; ranks of one compensation window (cont,

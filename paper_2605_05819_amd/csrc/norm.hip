@@ -216,14 +216,26 @@ __global__ void residual_norm_kernel(NormArgs a) {
 }
 
 template <int NI, bool TAIL>
-hipError_t launch(const NormArgs& a, hipStream_t st) {
+hipError_t launch(NormArgs a, hipStream_t st) {
     const int lanes = (a.d + 8 * NI - 1) / (8 * NI);
     const int threads = (lanes + 63) / 64 * 64;
-    if (static_cast<long long>(a.T) * a.d >= 1 << 20)
-        hipLaunchKernelGGL((residual_norm_kernel<NI, TAIL, true>), dim3(a.T), dim3(threads), 0, st, a);
-    else
-        hipLaunchKernelGGL((residual_norm_kernel<NI, TAIL, false>), dim3(a.T), dim3(threads), 0, st, a);
-    return hipGetLastError();
+    const bool stream = static_cast<long long>(a.T) * a.d >= 1 << 20;
+    // a later launch takes its rows' arrays
+    const auto at = [](const void* p, size_t n, int dt) {
+        return p ? const_cast<char*>(static_cast<const char*>(p)) + n * (dt == DT_FP32 ? 4 : 2) : nullptr;
+    };
+    const NormArgs all = a;
+    return launch_all(a.T, [&](unsigned first, unsigned count) {
+        const size_t n = static_cast<size_t>(first) * a.d;
+        a.y = at(all.y, a.slots ? n * a.slots : n, a.y_dtype);
+        if (a.slots) a.slot_weights = all.slot_weights + static_cast<size_t>(first) * a.slots;
+        if (a.gate_per_token) a.gate = at(all.gate, n, a.w_dtype);
+        a.residual = at(all.residual, n, a.h_dtype);
+        a.h = at(all.h, n, a.h_dtype);
+        a.out = at(all.out, n, a.out_dtype);
+        if (stream) hipLaunchKernelGGL((residual_norm_kernel<NI, TAIL, true>), dim3(count), dim3(threads), 0, st, a);
+        else hipLaunchKernelGGL((residual_norm_kernel<NI, TAIL, false>), dim3(count), dim3(threads), 0, st, a);
+    });
 }
 
 template <bool TAIL>

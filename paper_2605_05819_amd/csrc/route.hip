@@ -50,8 +50,8 @@ template <int EPL>
 __global__ __launch_bounds__(256) void moe_route_kernel(RouteArgs a) {
     __shared__ float group_choice[4][EPL > 1 ? 64 * EPL : 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int t = blockIdx.x * (blockDim.x >> 6) + wave;
-    if (t >= a.T) return;
+    const unsigned t = 4 * (a.first + blockIdx.x) + wave;
+    if (t >= static_cast<unsigned>(a.T)) return;
 
     float p[EPL];
     uint32_t key[EPL];
@@ -191,14 +191,16 @@ __global__ __launch_bounds__(256) void moe_route_kernel(RouteArgs a) {
 
 }  // namespace
 
-hipError_t launch_moe_route(const RouteArgs& a, hipStream_t st) {
-    const dim3 grid((a.T + 3) / 4), block(256);
-    if (a.E <= 64) hipLaunchKernelGGL((moe_route_kernel<1>), grid, block, 0, st, a);
-    else if (a.E <= 128) hipLaunchKernelGGL((moe_route_kernel<2>), grid, block, 0, st, a);
-    else if (a.E <= 256) hipLaunchKernelGGL((moe_route_kernel<4>), grid, block, 0, st, a);
-    else if (a.E <= 512) hipLaunchKernelGGL((moe_route_kernel<8>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((moe_route_kernel<16>), grid, block, 0, st, a);
-    return hipGetLastError();
+hipError_t launch_moe_route(RouteArgs a, hipStream_t st) {
+    return launch_all((static_cast<long long>(a.T) + 3) / 4, [&](unsigned first, unsigned count) {
+        a.first = first;
+        const dim3 grid(count), block(256);
+        if (a.E <= 64) hipLaunchKernelGGL((moe_route_kernel<1>), grid, block, 0, st, a);
+        else if (a.E <= 128) hipLaunchKernelGGL((moe_route_kernel<2>), grid, block, 0, st, a);
+        else if (a.E <= 256) hipLaunchKernelGGL((moe_route_kernel<4>), grid, block, 0, st, a);
+        else if (a.E <= 512) hipLaunchKernelGGL((moe_route_kernel<8>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((moe_route_kernel<16>), grid, block, 0, st, a);
+    });
 }
 
 }  // namespace cl

@@ -407,3 +407,39 @@ def test_small_probabilities_beside_sinks_keep_their_mass(a, n, D, dtype):
 @pytest.mark.parametrize("a,prefix", [(1, 0), (24, 0), (40, 0), (1, 1024), (40, 1024)])
 def test_one_sink_over_a_long_diffuse_tail(a, prefix):
     Tail(a, 100001, 100001, 17.0, 19.0, 64, F16, prefix).check(F16)
+
+
+def test_launches_of_more_than_2_24_workgroups():
+    """A prompt beside 2048 sequences of one token: each sequence has the longest one's workgroups."""
+    seqs, n, heads, D = 2049, 16384, 64, 64
+    g = torch.Generator(device="cuda").manual_seed(1)
+    pages = n // 64 + seqs - 1
+    k, v = (torch.randn((pages, heads, 64, D), device="cuda", generator=g, dtype=F32).half() for _ in range(2))
+    table = torch.full((seqs, n // 64), -1, dtype=torch.int32, device="cuda")
+    table[0] = torch.arange(n // 64)
+    table[1:, 0] = torch.arange(n // 64, pages)
+    kv_len = torch.ones(seqs, dtype=torch.int32, device="cuda")
+    kv_len[0] = n
+    start = torch.cat([torch.zeros(1, dtype=torch.int32), torch.arange(n, n + seqs, dtype=torch.int32)]).cuda()
+    q = torch.randn((n + seqs - 1, heads, D), device="cuda", generator=g).half()
+    cache = cl.KvCache(k, v)
+    out = cl.attention(cache, cl.KvBatch(kv_len, table, n + seqs - 1, q_len=n, q_start=start, max_kv_len=n), q)
+    alone = cl.attention(cache, cl.KvBatch(kv_len[:1].contiguous(), table[:1].contiguous(), n, q_len=n, max_kv_len=n), q[:n])
+    torch.cuda.synchronize()
+    assert torch.equal(out[:n], alone) and torch.equal(out[n:], v[n // 64:, :, 0])      # one key: its value
+
+
+def test_joins_of_more_than_2_24_rows():
+    """2^25 + 2^18 rows of two splits, every sequence the same."""
+    seqs, q_len, heads, D = 129, 4096, 64, 64
+    g = torch.Generator(device="cuda").manual_seed(2)
+    cache = cl.KvCache(*(torch.randn((3, 1, 64, D), device="cuda", generator=g).half() for _ in range(2)))
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    one = torch.randn((q_len, heads, D), device="cuda", generator=g).half()
+    batch = lambda n: cl.KvBatch(i32(*[80] * n), i32(*[[1]] * n), n * q_len, q_len=q_len, max_kv_len=80,  # noqa: E731
+                                 prefix_table=i32(2), prefix_len=64)
+    out = cl.attention(cache, batch(seqs), one.repeat(seqs, 1, 1), causal=False).view(seqs, q_len, heads, D)
+    alone = cl.attention(cache, batch(1), one, causal=False)
+    torch.cuda.synchronize()
+    assert all(torch.equal(out[i], out[0]) for i in range(seqs))
+    assert (out[0].float() - alone.float()).abs().max() <= 2.0 ** -9 * cache.v.float().abs().max()

@@ -329,3 +329,27 @@ def test_residual_norm_of_zeros_and_infinities():
     torch.cuda.synchronize()
     assert (h == 0).all() and (out == 0).all()
     assert (out2[0] == 0).all() and h2[1, 7] == math.inf and out2[1].isnan().any()
+
+
+# ------------------------------------------- more than 2^32 work items a launch
+
+def test_append_of_more_than_2_24_tokens():
+    n = (1 << 24) + 1
+    pages = n // 1024 + 1
+    cache = cl.KvCache.empty(pages, 1024, 1, 64)
+    k = torch.randint(-100, 100, (n, 1, 64), dtype=torch.int8, device="cuda").half()
+    v = -k
+    table = torch.arange(pages, dtype=torch.int32, device="cuda")[None]
+    cl.kv_append(cache, cl.KvBatch(i32([n]), table, n, q_len=n, max_kv_len=n), k, v)
+    torch.cuda.synchronize()
+    for got, want in ((cache.k, k), (cache.v, v)):
+        assert torch.equal(got.view(-1, 64)[:n], want[:, 0])
+
+
+def test_norm_and_route_of_more_than_2_26_tokens():
+    n = (1 << 26) + 5
+    y = torch.randint(0, 2, (n, 1), dtype=torch.int8, device="cuda").half() * 2 - 1
+    out = cl.residual_norm(y, torch.ones(1, dtype=F16, device="cuda"), h=False, eps=0.0)
+    ids, w = cl.moe_route(cl.Router(2, 1), torch.cat([torch.zeros_like(y), y], 1))
+    torch.cuda.synchronize()
+    assert torch.equal(out, y) and torch.equal(ids, (y > 0).int()) and (w == 1).all()

@@ -71,6 +71,19 @@ def test_attention_arguments(kw, status, needle):
                                    a["window"], a["out"], a["dt"], a["lse"], FAKE, 1 << 30, None), status, needle)
 
 
+@pytest.mark.parametrize("heads,batch", [
+    (8, dict(tokens=1 << 28, num_seqs=1 << 28)),                                                    # rows
+    (8, dict(tokens=1 << 20, q_len=1 << 20, num_seqs=1 << 22, q_start=FAKE)),                       # workgroups
+    (1 << 12, dict(tokens=1 << 18, q_len=1 << 18, num_seqs=0x7fffffff, q_start=FAKE, max_kv_len=1 << 30))])
+def test_attention_beyond_32_bit_numbers(heads, batch):
+    cc, bb = _kv({}, batch)
+    lib = cl.lib()
+    _refused(lib.cl_attention(ctypes.byref(cc), ctypes.byref(bb), FAKE, heads * 128, heads, 0.1, 1, 0, FAKE, cl.CL_FP16, None,
+                              FAKE, (1 << 63) - 1, None), cl.CL_EUNSUPPORTED, "2^31")
+    before = lib.cl_last_error()
+    assert lib.cl_attention_workspace(ctypes.byref(cc), ctypes.byref(bb), heads) == 0 and lib.cl_last_error() == before
+
+
 @pytest.mark.parametrize("kw,needle", [
     (dict(k=0), "null k"), (dict(v=0), "null k or v"), (dict(q=0), "go together"), (dict(heads=0), "go together"),
     (dict(q_out=0), "q_out"), (dict(q=FAKE + 1), "misaligned"), (dict(ks=255), "shorter"), (dict(vs=0), "shorter"),
