@@ -521,7 +521,8 @@ typedef struct cl_kv_cache {
  *               every sequence has q_len of them (tokens = num_seqs * q_len)
  *  page_table   device int32 [num_seqs][table_width]: the pages of the keys
  *               behind the prefix, key prefix_len + i in row i % page_size of
- *               entry i / page_size.  Entries past kv_len are not read.
+ *               entry i / page_size.  Entries past kv_len are not used (up to
+ *               the host's bound they may be read)
  *  prefix_table device int32 [ceil(prefix_len / page_size)]: the pages of the
  *               first prefix_len keys, the same for every sequence; NULL with
  *               prefix_len 0
@@ -641,8 +642,9 @@ cl_status cl_kv_append(const cl_kv_cache* cache, const cl_kv_batch* batch, const
  *  ws         device workspace of cl_attention_workspace(...) bytes, 256-byte
  *             aligned (partial results of keys that were split over workgroups)
  * Scores, softmax statistics and sums are float32; the probabilities enter the
- * second product as the cache's dtype.  Results do not depend on the order
- * in which workgroups run.
+ * second product as the cache's dtype, each off by 2^-8 (CL_BF16) or 2^-11
+ * (CL_FP16; or 2^-37 of the row's largest, if that is more) of itself at
+ * most.  Results do not depend on the order in which workgroups run.
  * Errors: CL_EINVAL; CL_EUNSUPPORTED for a head_dim that the cache does not
  * take, and where tokens * q_heads, or the launch (about
  * num_seqs * q_len * q_heads / 64 workgroups), reaches 2^31; CL_EWORKSPACE, CL_EHIP.

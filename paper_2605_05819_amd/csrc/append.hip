@@ -2,10 +2,11 @@
 // rotated, k and v written to their pages, q to q_out, in one launch.
 //
 // The token at position p turns pair j of its first rot_dim values by the
-// angle p inv_freq[j].  The product is formed in fp64 (exact: 24 by 31 bits)
-// and reduced to a part of a turn there, so the angle is as exact at position
-// 10^6 as at 1; sine and cosine are fp32.  Everything is computed in fp32 and
-// rounded once.
+// angle p inv_freq[j].  The product is formed in fp64 (exact below position 2^29,
+// a factor of 24 bits and one of 29) and reduced to a part of a turn there, off
+// by 2^-51 of itself at most, so the angle is as good at position 10^6 as at 1;
+// sine and cosine are fp32.  Everything else is computed in fp32 and rounded
+// once.
 //
 // A group of LG lanes owns a head vector, a lane 4 pairs: values 4c.. and
 // rot_dim/2 + 4c.. (half layout) or 8c..8c+7 (interleaved, and the part that
@@ -13,9 +14,9 @@
 // head that the lane's group visits.
 //
 // Bound by memory: 8593 tokens of 32 + 8 + 8 heads of 128, with per-head norms,
-// 211 MB read and written in 52 us, 4.0 TB/s (36 us without norms where the
-// buffers stay in the last cache); a few tokens by the chain length -> page
-// -> store, 3 us.
+// 211 MB read and written in 51 to 52.5 us, 4.0 to 4.1 TB/s (36 us without norms
+// where the buffers stay in the last cache); a few tokens by the chain length ->
+// page -> store, 3 us.
 
 #include <math.h>
 
@@ -56,8 +57,10 @@ __device__ __forceinline__ void load8(const uint16_t* p, int lo, int hi, bool ap
     }
 }
 
-// STREAM: a prompt's results, more than the caches hold, go past them
-// (8593 tokens 56.5 -> 47.3 us).
+// STREAM: a prompt's results (four heads a group, see choose) are stored past the
+// L2 caches (8593 tokens 56.5 -> 47.3 us when it was changed).
+// Attention behind the call is no slower for it: 1500 tokens, both, 56.2 us
+// against 57.2 with ordinary stores, 3000 103.5 / 104.8, 8593 627 / 626.
 template <bool STREAM, class T>
 __device__ __forceinline__ void put(uint16_t* p, T v) {
     if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<T*>(p));

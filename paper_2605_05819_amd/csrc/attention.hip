@@ -29,18 +29,20 @@
 //    V: each wave streams keys of its own, 32 at a time, K straight into
 //    operand registers, V through its own slice of LDS; nothing in the loop
 //    waits for another wave.  Four sequences of 100 k to 131 k keys, 4 tokens
-//    each: 356 us, 5.3 TB/s; 64 sequences of 1500 to 2500 keys 102 us, 4.9 TB/s.
+//    each: 357 us, 5.3 TB/s; 64 sequences of 1500 to 2500 keys 105 us, 4.8 TB/s.
 //  * attn_tile: more rows (prompts, a shared prefix under many sequences).
 //    Bound by the issue of MFMA and softmax instructions (per 32 rows x 64 keys
 //    and wave 64 MFMAs, 1024 cycles, and about 200 others, 900 cycles, of which
 //    two resident waves overlap half): four waves of 16 NQ rows share tiles of
 //    64 keys in LDS, double-buffered.  Prompts of up to 7001 tokens over 9001
-//    keys: 858 us, 1.00 PFLOP/s (a library product of 8192^3 runs at 1.21).
+//    keys: 844 to 862 us, 1.0 PFLOP/s (one slower card: 932; a library product of
+//    8192^3 runs at 1.20 to 1.22).
 //
 // Rounding: probabilities enter the second product as the cache's type, to
 // nearest (off by 2^-8 of each at most in bf16, 2^-11 in fp16, and there by 2^-37
-// of the row's largest where that is more; see kLift), beside the output's own rounding; sums,
-// maxima, O and the partial results are fp32, and l is summed from the unrounded
+// of the row's largest where that is more; see kLift), beside the output's own
+// rounding.  The second product then runs at the 16-bit rate.  Sums, maxima, O
+// and the partial results are fp32, and l is summed from the unrounded
 // probabilities.
 
 #include "cl_device.h"
@@ -132,7 +134,7 @@ __device__ __forceinline__ float row_sum(float v) {
 // sequence's streamed unit has splits | 1 places in the grid: workgroups go to the four
 // shader engines of an XCD in turn, and where sequences end early an even
 // period would leave the same engines without work each time (16 sequences of
-// 1 to 8192 keys 25.1 -> 23.6 us).
+// 1 to 8192 keys 25.1 -> 23.6 us when it was changed).
 struct Plan {
     int rows;              // most rows of a unit
     int blocks;            // row blocks of a unit
@@ -654,7 +656,7 @@ constexpr int tile_keys(int D) { return D > 128 ? 32 : 64; }
 // (probabilities up to 2^kSlack; every result divides by their sum), which
 // saves nearly all rescaling but rounds a row's largest probability, that a
 // current maximum makes exactly 1.  With a slack of 0, 3 and 6 ragged prompts
-// take 910, 878 and 870 us, and their error against 64 bits is 1.10, 1.16 and
+// take 879, 845 and 833 us, and their error against 64 bits is 1.10, 1.16 and
 // 1.26 times that of one final rounding.
 constexpr float kSlack = 3.f;
 
@@ -1047,7 +1049,7 @@ constexpr int lds_bytes(int D, int kind) {
 // The prefix's and the sequences' own workgroups side by side, so the tiles of
 // the one and the streams of the other share the CUs.  Streams of 16 rows fit
 // three workgroups on a CU (168 registers), streams of 256-wide heads one (367;
-// held to 256 they spill: 16 sequences of 200 to 8000 keys 124 against 96 us),
+// held to 256 they spill: 16 sequences of 200 to 8000 keys 266 against 78 us),
 // the rest two.
 template <int D, bool BF, int P, int O>
 __global__ __launch_bounds__(256, (O <= S2 || O == S0) && D > 128 ? 1 : P == NONE && O == S0 ? 3 : 2) void attn_kernel(
@@ -1183,8 +1185,8 @@ Plan make_plan(const KvCache& c, const KvBatch& b, int q_heads) {
     // one sequence of 2049 keys would take 12.2 for 10.7), and then one split
     // without a join up to 512 keys (64 sequences of 10 to 300 keys 14.8 -> 11.0
     // us; one of 500 would take 11.8 for 9.9).  4096 workgroups in all where
-    // three fit a CU (16 ragged sequences 23.6 us, 26.5 with 2048), else 2048
-    // (256-wide heads 92 -> 81 us, 24 rows a unit 52 -> 48).
+    // three fit a CU (16 ragged sequences 23.0 us, 25.7 with 2048), else 2048
+    // (256-wide heads 88 -> 78 us, 24 rows a unit 53 -> 49).
     const bool many = units >= 256;
     const int least = !many ? 128 : own <= 512 && b.prefix_len == 0 ? 512 : 256;
     const int want = rows <= 16 && c.dim <= 128 ? 4096 : 2048;
