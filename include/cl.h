@@ -657,6 +657,72 @@ cl_status cl_attention(const cl_kv_cache* cache, const cl_kv_batch* batch, const
  * arrays are not read), 0 for rejected arguments. */
 size_t cl_attention_workspace(const cl_kv_cache* cache, const cl_kv_batch* batch, int32_t q_heads);
 
+/*
+ * cl_kv_cache8 -- a cache of 8-bit codes, half the bytes of a cl_kv_cache: a key's
+ * or value's element is e4m3(code) 2^(scale - 127), with a scale for each head and
+ * block of `block` rows of a page.
+ *  k, v       device [num_pages][kv_heads][page_size][head_dim] codes: sign, 4
+ *             bits of exponent (bias 7), 3 of fraction; 0x7f and 0xff are NaN.
+ *             16-byte aligned
+ *  k_scale, v_scale  device uint8 [num_pages][kv_heads][page_size / block]
+ *  block      rows that share a scale: a power of two, 1..page_size
+ *  dtype      CL_FP16 or CL_BF16: the type of queries and new tokens, in which
+ *             every element that cl_kv_append8 writes is a value exactly
+ *  the rest   as in cl_kv_cache
+ */
+typedef struct cl_kv_cache8 {
+    void* k;
+    void* v;
+    uint8_t* k_scale;
+    uint8_t* v_scale;
+    int32_t num_pages;
+    int32_t page_size;
+    int32_t kv_heads;
+    int32_t head_dim;
+    int32_t block;
+    int32_t dtype;
+} cl_kv_cache8;
+
+/*
+ * cl_kv_append8 -- cl_kv_append into a cache of 8 bits.  The new rows of a block
+ * are rounded to e4m3 (to nearest, ties to even) under 2^e, e the smallest with
+ * max |x| <= 448 2^e over them, within -15..8 (CL_FP16) or -117..120 (CL_BF16), and
+ * at least the exponent of the rows that stood in the block ahead of them; where
+ * that is the smaller one, those rows are rescaled (exactly, but for codes that
+ * come to stand below 2^-6, which are rounded again).  What stood behind the new
+ * rows of a block counts as gone.  Computed in float32 and rounded once.  Magnitudes above
+ * 1.875 2^15 (CL_FP16) or 1.875 2^127 are held as that; infinities and NaN as NaN,
+ * and they do not enter the maximum.
+ * A page that several sequences share has to be made a sequence's own before its
+ * tokens are appended (cl_kv_fork and cl_kv_reserve do).
+ * Arguments and errors: as cl_kv_append.
+ */
+cl_status cl_kv_append8(const cl_kv_cache8* cache, const cl_kv_batch* batch, const cl_rope* rope, const void* q,
+                        int64_t q_stride, int32_t q_heads, const void* k, int64_t k_stride, const void* v,
+                        int64_t v_stride, const void* q_norm, const void* k_norm, float eps,
+                        const int32_t* positions, void* q_out, void* stream);
+
+/*
+ * cl_attention8 -- cl_attention over a cache of 8 bits: the elements become values
+ * of the cache's dtype on their way (exactly, see cl_kv_cache8), and everything
+ * else is as there, the error bounds included.
+ */
+cl_status cl_attention8(const cl_kv_cache8* cache, const cl_kv_batch* batch, const void* q, int64_t q_stride,
+                        int32_t q_heads, float scale, int32_t causal, int32_t window, void* out, int32_t out_dtype,
+                        float* lse, void* ws, size_t ws_bytes, void* stream);
+size_t cl_attention8_workspace(const cl_kv_cache8* cache, const cl_kv_batch* batch, int32_t q_heads);
+
+/*
+ * cl_kv_read, cl_kv_read8 -- the batch's tokens' rows of the cache, dense and in its
+ * dtype (a batch whose q_start counts all keys reads whole sequences).
+ *  k, v  device [tokens][kv_heads][head_dim] of the cache's dtype, 16-byte aligned
+ * A token at a position below 0 gets zeros, one whose page is outside the pool
+ * NaN; rows of no sequence are left alone.
+ * Errors: CL_EINVAL, CL_EUNSUPPORTED, CL_EHIP.
+ */
+cl_status cl_kv_read(const cl_kv_cache* cache, const cl_kv_batch* batch, void* k, void* v, void* stream);
+cl_status cl_kv_read8(const cl_kv_cache8* cache, const cl_kv_batch* batch, void* k, void* v, void* stream);
+
 /* Scores of a router. */
 enum { CL_SOFTMAX = 1, CL_SIGMOID = 2 };
 

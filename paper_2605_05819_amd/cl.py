@@ -48,6 +48,13 @@ class KvCacheC(ctypes.Structure):
                 ("dtype", ctypes.c_int32)]
 
 
+class KvCache8C(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("block", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
 class KvBatchC(ctypes.Structure):
     _fields_ = [("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
                 ("prefix_table", ctypes.c_void_p), ("num_seqs", ctypes.c_int32), ("tokens", ctypes.c_int32),
@@ -150,6 +157,8 @@ _SIGNATURES = {
                                       ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_int32, ctypes.c_int32,
                                       ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p,
                                       ctypes.c_size_t, ctypes.c_void_p]),
+    "cl_kv_read": (ctypes.c_int32, [ctypes.POINTER(KvCacheC), ctypes.POINTER(KvBatchC), ctypes.c_void_p,
+                                    ctypes.c_void_p, ctypes.c_void_p]),
     "cl_moe_route": (ctypes.c_int32, [ctypes.POINTER(RouterC), ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32,
                                       ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
                                       ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p]),
@@ -158,6 +167,11 @@ _SIGNATURES = {
                                           ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                           ctypes.c_void_p]),
 }
+
+# the same calls over a cache of 8 bits
+for _name, _eight in (("cl_kv_append", "cl_kv_append8"), ("cl_attention", "cl_attention8"),
+                      ("cl_attention_workspace", "cl_attention8_workspace"), ("cl_kv_read", "cl_kv_read8")):
+    _SIGNATURES[_eight] = (_SIGNATURES[_name][0], [ctypes.POINTER(KvCache8C)] + _SIGNATURES[_name][1][1:])
 
 
 def lib():
@@ -184,7 +198,8 @@ def lib():
 
 _PACKED = ("cl_linear_decode", "cl_linear_decode_noalloc", "cl_linear_decode_window", "cl_linear_decode_glu",
            "cl_linear_prefill", "cl_linear_workspace", "cl_linear_window_workspace", "cl_prefill_workspace",
-           "cl_kv_append", "cl_attention", "cl_attention_workspace", "cl_moe_route", "cl_residual_norm")
+           "cl_kv_append", "cl_attention", "cl_attention_workspace", "cl_moe_route", "cl_residual_norm",
+           "cl_kv_append8", "cl_attention8", "cl_attention8_workspace", "cl_kv_read", "cl_kv_read8")
 _SCALARS = (ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float)
 _packed = {}
 
@@ -729,6 +744,7 @@ def build_compensation(W, w, r_max, stream=None):
 
 _KV = (torch.float16, torch.bfloat16)
 _PACK_CACHE = struct.Struct("PPiiiii").pack
+_PACK_CACHE8 = struct.Struct("PPPPiiiiii").pack
 _PACK_BATCH = struct.Struct("PPPPiiiiii").pack
 _PACK_ROPE = struct.Struct("Piif").pack
 _PACK_ROUTER = struct.Struct("Piiiiiiif").pack
@@ -745,6 +761,8 @@ def _opt_ptr(t):
 class KvCache:
     """A pool of pages: k and v [num_pages][kv_heads][page_size][head_dim],
     fp16 or bf16.  Checked once, when it is made."""
+
+    _append, _attention, _workspace, _read = "cl_kv_append", "cl_attention", "cl_attention_workspace", "cl_kv_read"
 
     def __init__(self, k, v):
         chk = _Checked()
@@ -766,6 +784,45 @@ class KvCache:
 
     def packed(self):
         """The bytes of a cl_kv_cache."""
+        return self._bytes
+
+
+class KvCache8:
+    """A pool of pages of 8-bit codes (cl_kv_cache8): k and v uint8
+    [num_pages][kv_heads][page_size][head_dim], k_scale and v_scale uint8
+    [num_pages][kv_heads][page_size / block]; dtype (fp16 or bf16) is that of
+    queries and new tokens.  It goes wherever a KvCache does.  Checked once, when
+    it is made."""
+
+    _append, _attention, _workspace, _read = "cl_kv_append8", "cl_attention8", "cl_attention8_workspace", "cl_kv_read8"
+
+    def __init__(self, k, v, k_scale, v_scale, dtype):
+        chk, u8 = _Checked(), (torch.uint8,)
+        _need(dtype in _KV, "dtype must be torch.float16 or torch.bfloat16 (got %s)" % dtype)
+        _dev_tensor(k, "k", u8, chk=chk)
+        _need(k.dim() == 4, "k must be [num_pages][kv_heads][page_size][head_dim]")
+        _dev_tensor(v, "v", u8, k.shape, chk)
+        _dev_tensor(k_scale, "k_scale", u8, chk=chk)
+        _need(k_scale.dim() == 3 and k_scale.shape[:2] == k.shape[:2] and k_scale.shape[2] > 0 and
+              k.shape[2] % k_scale.shape[2] == 0, "k_scale must be [num_pages][kv_heads][page_size / block]")
+        _dev_tensor(v_scale, "v_scale", u8, k_scale.shape, chk)
+        chk.on_gpu()
+        self.k, self.v, self.k_scale, self.v_scale, self.dtype = k, v, k_scale, v_scale, dtype
+        self.num_pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        self.block = self.page_size // k_scale.shape[2]
+        self._bytes = _PACK_CACHE8(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), self.num_pages,
+                                   self.page_size, self.kv_heads, self.head_dim, self.block, _DTYPE_CODE[dtype])
+
+    @classmethod
+    def empty(cls, num_pages, page_size, kv_heads, head_dim, block=16, dtype=torch.float16, device="cuda"):
+        """A new pool; its pages hold nothing until something is appended."""
+        _need(block > 0 and page_size % block == 0, "block must divide page_size")
+        new = lambda *s: torch.empty((num_pages, kv_heads) + s, dtype=torch.uint8, device=device)  # noqa: E731
+        return cls(new(page_size, head_dim), new(page_size, head_dim), new(page_size // block), new(page_size // block),
+                   dtype)
+
+    def packed(self):
+        """The bytes of a cl_kv_cache8."""
         return self._bytes
 
 
@@ -870,7 +927,7 @@ def _token_rows(t, name, dtype, tokens, heads, dim):
 
 def kv_append(cache, batch, k, v, q=None, rope=None, q_norm=None, k_norm=None, eps=1e-6, positions=None, q_out=None,
               stream=None):
-    """``cl_kv_append``: k, v [tokens][kv_heads][head_dim] into the cache, q
+    """``cl_kv_append``, and ``cl_kv_append8`` for a cache of 8 bits: k, v [tokens][kv_heads][head_dim] into the cache, q
     [tokens][q_heads][head_dim] rotated into q_out (returned; None without q).
     A token's heads are contiguous, tokens at any stride."""
     dt, D, n = cache.dtype, cache.head_dim, batch.tokens
@@ -892,7 +949,7 @@ def kv_append(cache, batch, k, v, q=None, rope=None, q_norm=None, k_norm=None, e
         _dev_tensor(positions, "positions", _I32, (n,))
     if q is None:
         q_out = None
-    st = _call("cl_kv_append")(cache._bytes, batch._bytes, None if rope is None else rope._bytes,
+    st = _call(cache._append)(cache._bytes, batch._bytes, None if rope is None else rope._bytes,
                                None if q is None else q.data_ptr(), qs, heads, k.data_ptr(), ks, v.data_ptr(), vs,
                                None if q_norm is None else q_norm.data_ptr(),
                                None if k_norm is None else k_norm.data_ptr(), eps,
@@ -904,12 +961,12 @@ def kv_append(cache, batch, k, v, q=None, rope=None, q_norm=None, k_norm=None, e
 
 
 def attention_workspace(cache, batch, q_heads):
-    return _call("cl_attention_workspace")(cache._bytes, batch._bytes, q_heads)
+    return _call(cache._workspace)(cache._bytes, batch._bytes, q_heads)
 
 
 def attention(cache, batch, q, scale=None, causal=True, window=0, out=None, out_dtype=None, lse=None, ws=None,
               stream=None):
-    """``cl_attention``: q [tokens][q_heads][head_dim] of the cache's dtype ->
+    """``cl_attention``, and ``cl_attention8`` for a cache of 8 bits: q [tokens][q_heads][head_dim] of the cache's dtype ->
     out of out_dtype (default: q's).  scale: head_dim ** -0.5 by default;
     ``lse``: None, or a float32 [tokens][q_heads] tensor to be filled."""
     D, n = cache.head_dim, batch.tokens
@@ -923,15 +980,32 @@ def attention(cache, batch, q, scale=None, causal=True, window=0, out=None, out_
     if lse is not None:
         _dev_tensor(lse, "lse", (torch.float32,), (n, heads))
     if ws is None:
-        need = _call("cl_attention_workspace")(cache._bytes, batch._bytes, heads)
+        need = _call(cache._workspace)(cache._bytes, batch._bytes, heads)
         ws = _empty((need,), torch.uint8, q.device, stream) if need else None
     else:
         _dev_tensor(ws, "ws", (torch.uint8,))
-    _check(_call("cl_attention")(cache._bytes, batch._bytes, q.data_ptr(), qs, heads,
-                                 D ** -0.5 if scale is None else scale, int(causal), window, out.data_ptr(),
-                                 _DTYPE_CODE[out.dtype], _opt_ptr(lse), _opt_ptr(ws),
-                                 0 if ws is None else ws.numel(), _raw_stream(stream)))
+    _check(_call(cache._attention)(cache._bytes, batch._bytes, q.data_ptr(), qs, heads,
+                                   D ** -0.5 if scale is None else scale, int(causal), window, out.data_ptr(),
+                                   _DTYPE_CODE[out.dtype], _opt_ptr(lse), _opt_ptr(ws),
+                                   0 if ws is None else ws.numel(), _raw_stream(stream)))
     return out
+
+
+def kv_read(cache, batch, k=None, v=None, stream=None):
+    """``cl_kv_read`` and ``cl_kv_read8``: the batch's tokens' rows of the cache,
+    (k, v) [tokens][kv_heads][head_dim] of its dtype."""
+    _check_prefix(cache, batch)
+    shape = (batch.tokens, cache.kv_heads, cache.head_dim)
+    if k is None:
+        k = _empty(shape, cache.dtype, cache.k.device, stream)
+    else:
+        _dev_tensor(k, "k", (cache.dtype,), shape)
+    if v is None:
+        v = _empty(shape, cache.dtype, cache.k.device, stream)
+    else:
+        _dev_tensor(v, "v", (cache.dtype,), shape)
+    _check(_call(cache._read)(cache._bytes, batch._bytes, k.data_ptr(), v.data_ptr(), _raw_stream(stream)))
+    return k, v
 
 
 class Router:

@@ -543,11 +543,112 @@ cl_status check_kv(const cl_kv_cache* c, const cl_kv_batch* b, cl::KvCache* oc, 
     if ((static_cast<long long>(c->num_pages) * c->kv_heads << shift) > 0x7fffffffll)
         return fail(CL_EUNSUPPORTED, "%s: num_pages * kv_heads * page_size must be below 2^31", who);
     *oc = {static_cast<uint16_t*>(c->k), static_cast<uint16_t*>(c->v), c->num_pages, shift, c->kv_heads, c->head_dim,
-           c->dtype};
+           c->dtype, nullptr, nullptr, 0};
     const int q_len = b->q_len < b->tokens ? b->q_len : b->tokens;
     *ob = {b->q_start, b->kv_len, b->page_table, b->prefix_table, b->num_seqs, b->tokens, q_len, b->table_width,
            b->prefix_len, static_cast<int>(limit)};
     return CL_OK;
+}
+
+cl_status check_kv8(const cl_kv_cache8* c, const cl_kv_batch* b, cl::KvCache* oc, cl::KvBatch* ob, const char* who) {
+    if (!c) return fail(CL_EINVAL, "%s: null cache or batch descriptor", who);
+    const cl_kv_cache rest{c->k, c->v, c->num_pages, c->page_size, c->kv_heads, c->head_dim, c->dtype};
+    const cl_status st = check_kv(&rest, b, oc, ob, who);
+    if (st) return st;
+    if (!c->k_scale || !c->v_scale) return fail(CL_EINVAL, "%s: null k_scale or v_scale", who);
+    if (c->block < 1 || c->block > c->page_size || (c->block & (c->block - 1)))
+        return fail(CL_EINVAL, "%s: block must be a power of two in 1..page_size (got %d)", who, c->block);
+    int shift = 0;
+    while ((1 << shift) < c->block) ++shift;
+    oc->k_scale = c->k_scale;
+    oc->v_scale = c->v_scale;
+    oc->block_shift = shift;
+    return CL_OK;
+}
+
+// The rest of the appends' checks; a.cache and a.batch have passed.
+cl_status append_checked(cl::AppendArgs& a, bool codes, const cl_rope* rope, const void* q, int64_t q_stride,
+                         int32_t q_heads, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                         const void* q_norm, const void* k_norm, float eps, const int32_t* positions, void* q_out,
+                         void* stream, const char* who) {
+    if (rope) {
+        if (!rope->inv_freq || !aligned(rope->inv_freq, 4)) return fail(CL_EINVAL, "%s: null or misaligned inv_freq", who);
+        if (rope->rot_dim < 8 || rope->rot_dim > a.cache.dim || rope->rot_dim % 8)
+            return fail(CL_EINVAL, "%s: rot_dim must be a multiple of 8 in 8..head_dim (got %d)", who, rope->rot_dim);
+        if (!isfinite(rope->magnitude)) return fail(CL_EINVAL, "%s: magnitude must be finite", who);
+        a.rope = {rope->inv_freq, rope->rot_dim, rope->interleaved ? 1 : 0, rope->magnitude};
+    }
+    if (q_heads < 0 || (q_heads > 0) != (q != nullptr)) return fail(CL_EINVAL, "%s: q and q_heads go together", who);
+    if (!k || !v) return fail(CL_EINVAL, "%s: null k or v", who);
+    if (q && !q_out) return fail(CL_EINVAL, "%s: null q_out", who);
+    if (!aligned(q, 2) || !aligned(k, 2) || !aligned(v, 2) || !aligned(q_out, 2) || !aligned(q_norm, 2) || !aligned(k_norm, 2))
+        return fail(CL_EINVAL, "%s: misaligned q, k, v, q_out or norm", who);
+    if (positions && !aligned(positions, 4)) return fail(CL_EINVAL, "%s: misaligned positions", who);
+    const int64_t D = a.cache.dim;
+    if ((q && q_stride < q_heads * D) || k_stride < a.cache.heads * D || v_stride < a.cache.heads * D)
+        return fail(CL_EINVAL, "%s: a token stride is shorter than the token's heads", who);
+    if ((q_norm || k_norm) && !(eps >= 0.f && isfinite(eps))) return fail(CL_EINVAL, "%s: eps must be finite and >= 0", who);
+    a.q = static_cast<const uint16_t*>(q);
+    a.k = static_cast<const uint16_t*>(k);
+    a.v = static_cast<const uint16_t*>(v);
+    a.q_norm = static_cast<const uint16_t*>(q_norm);
+    a.k_norm = static_cast<const uint16_t*>(k_norm);
+    a.positions = positions;
+    a.q_out = static_cast<uint16_t*>(q_out);
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.q_heads = q_heads;
+    a.eps = eps;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return hip_status(codes ? cl::launch_kv_append8(a, st) : cl::launch_kv_append(a, st), who);
+}
+
+cl_status attention_checked(cl::AttnArgs& a, bool codes, const void* q, int64_t q_stride, int32_t q_heads, float scale,
+                            int32_t causal, int32_t window, void* out, int32_t out_dtype, float* lse, void* ws,
+                            size_t ws_bytes, void* stream, const char* who) {
+    if (q_heads < 1 || q_heads % a.cache.heads)
+        return fail(CL_EINVAL, "%s: q_heads (%d) must be a positive multiple of kv_heads (%d)", who, q_heads, a.cache.heads);
+    if (!q || !out) return fail(CL_EINVAL, "%s: null q or out", who);
+    if (!aligned(q, 16) || q_stride % 8 || !aligned(out, 16))
+        return fail(CL_EINVAL, "%s: q rows and out must be 16-byte aligned", who);
+    if (q_stride < static_cast<int64_t>(q_heads) * a.cache.dim)
+        return fail(CL_EINVAL, "%s: q_stride is shorter than a token's heads", who);
+    if (!cl::attention_size_ok(a.cache, a.batch, q_heads))
+        return fail(CL_EUNSUPPORTED, "%s: rows (tokens * q_heads) and workgroups (num_seqs * q_len * q_heads / 64) must be below 2^31",
+                    who);
+    if (!isfinite(scale)) return fail(CL_EINVAL, "%s: scale must be finite", who);
+    if (window < 0) return fail(CL_EINVAL, "%s: window must not be negative", who);
+    if (!out_type(out_dtype)) return fail(CL_EINVAL, "%s: out_dtype must be CL_FP16, CL_BF16 or CL_FP32", who);
+    if (lse && !aligned(lse, 4)) return fail(CL_EINVAL, "%s: misaligned lse", who);
+    const size_t need = cl::attention_workspace_bytes(a.cache, a.batch, q_heads);
+    if (need > 0) {
+        if (!ws || ws_bytes < need)
+            return fail(CL_EWORKSPACE, "%s: workspace of %zu bytes needed (got %zu)", who, need, ws ? ws_bytes : 0);
+        if (!aligned(ws, 256)) return fail(CL_EINVAL, "%s: workspace must be 256-byte aligned", who);
+    }
+    a.q = static_cast<const uint16_t*>(q);
+    a.q_stride = q_stride;
+    a.q_heads = q_heads;
+    a.causal = causal ? 1 : 0;
+    a.window = window < kMaxKeys ? window : 0;         // a window of the longest sequence hides nothing
+    a.out_dtype = out_dtype;
+    a.scale = scale;
+    a.out = out;
+    a.lse = lse;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return hip_status(codes ? cl::launch_attention8(a, ws, st) : cl::launch_attention(a, ws, st), who);
+}
+
+// Of checked descriptors; 0 for rejected ones.
+size_t attention_bytes(cl_status st, const cl::KvCache& c, const cl::KvBatch& b, int q_heads) {
+    if (st != CL_OK || q_heads < c.heads || q_heads % c.heads || !cl::attention_size_ok(c, b, q_heads)) return 0;
+    return cl::attention_workspace_bytes(c, b, q_heads);
+}
+
+cl_status read_checked(const cl::ReadArgs& a, bool codes, const void* k, const void* v, void* stream, const char* who) {
+    if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) return fail(CL_EINVAL, "%s: k and v must be non-null and 16-byte aligned", who);
+    return hip_status(cl::launch_kv_read(a, codes, static_cast<hipStream_t>(stream)), who);
 }
 
 }  // namespace
@@ -576,38 +677,22 @@ cl_status cl_kv_append(const cl_kv_cache* cache, const cl_kv_batch* batch, const
                        const int32_t* positions, void* q_out, void* stream) {
     const char* who = "cl_kv_append";
     cl::AppendArgs a{};
-    cl_status st = check_kv(cache, batch, &a.cache, &a.batch, who);
+    const cl_status st = check_kv(cache, batch, &a.cache, &a.batch, who);
     if (st) return st;
-    if (rope) {
-        if (!rope->inv_freq || !aligned(rope->inv_freq, 4)) return fail(CL_EINVAL, "%s: null or misaligned inv_freq", who);
-        if (rope->rot_dim < 8 || rope->rot_dim > cache->head_dim || rope->rot_dim % 8)
-            return fail(CL_EINVAL, "%s: rot_dim must be a multiple of 8 in 8..head_dim (got %d)", who, rope->rot_dim);
-        if (!isfinite(rope->magnitude)) return fail(CL_EINVAL, "%s: magnitude must be finite", who);
-        a.rope = {rope->inv_freq, rope->rot_dim, rope->interleaved ? 1 : 0, rope->magnitude};
-    }
-    if (q_heads < 0 || (q_heads > 0) != (q != nullptr)) return fail(CL_EINVAL, "%s: q and q_heads go together", who);
-    if (!k || !v) return fail(CL_EINVAL, "%s: null k or v", who);
-    if (q && !q_out) return fail(CL_EINVAL, "%s: null q_out", who);
-    if (!aligned(q, 2) || !aligned(k, 2) || !aligned(v, 2) || !aligned(q_out, 2) || !aligned(q_norm, 2) || !aligned(k_norm, 2))
-        return fail(CL_EINVAL, "%s: misaligned q, k, v, q_out or norm", who);
-    if (positions && !aligned(positions, 4)) return fail(CL_EINVAL, "%s: misaligned positions", who);
-    const int64_t D = cache->head_dim;
-    if ((q && q_stride < q_heads * D) || k_stride < cache->kv_heads * D || v_stride < cache->kv_heads * D)
-        return fail(CL_EINVAL, "%s: a token stride is shorter than the token's heads", who);
-    if ((q_norm || k_norm) && !(eps >= 0.f && isfinite(eps))) return fail(CL_EINVAL, "%s: eps must be finite and >= 0", who);
-    a.q = static_cast<const uint16_t*>(q);
-    a.k = static_cast<const uint16_t*>(k);
-    a.v = static_cast<const uint16_t*>(v);
-    a.q_norm = static_cast<const uint16_t*>(q_norm);
-    a.k_norm = static_cast<const uint16_t*>(k_norm);
-    a.positions = positions;
-    a.q_out = static_cast<uint16_t*>(q_out);
-    a.q_stride = q_stride;
-    a.k_stride = k_stride;
-    a.v_stride = v_stride;
-    a.q_heads = q_heads;
-    a.eps = eps;
-    return hip_status(cl::launch_kv_append(a, static_cast<hipStream_t>(stream)), who);
+    return append_checked(a, false, rope, q, q_stride, q_heads, k, k_stride, v, v_stride, q_norm, k_norm, eps, positions, q_out,
+                          stream, who);
+}
+
+cl_status cl_kv_append8(const cl_kv_cache8* cache, const cl_kv_batch* batch, const cl_rope* rope, const void* q,
+                       int64_t q_stride, int32_t q_heads, const void* k, int64_t k_stride, const void* v,
+                       int64_t v_stride, const void* q_norm, const void* k_norm, float eps,
+                       const int32_t* positions, void* q_out, void* stream) {
+    const char* who = "cl_kv_append8";
+    cl::AppendArgs a{};
+    const cl_status st = check_kv8(cache, batch, &a.cache, &a.batch, who);
+    if (st) return st;
+    return append_checked(a, true, rope, q, q_stride, q_heads, k, k_stride, v, v_stride, q_norm, k_norm, eps, positions, q_out,
+                          stream, who);
 }
 
 size_t cl_attention_workspace(const cl_kv_cache* cache, const cl_kv_batch* batch, int32_t q_heads) {
@@ -615,10 +700,7 @@ size_t cl_attention_workspace(const cl_kv_cache* cache, const cl_kv_batch* batch
     memcpy(saved, g_err, sizeof(g_err));
     cl::KvCache c;
     cl::KvBatch b;
-    size_t bytes = 0;
-    if (check_kv(cache, batch, &c, &b, "") == CL_OK && q_heads >= c.heads && q_heads % c.heads == 0 &&
-        cl::attention_size_ok(c, b, q_heads))
-        bytes = cl::attention_workspace_bytes(c, b, q_heads);
+    const size_t bytes = attention_bytes(check_kv(cache, batch, &c, &b, ""), c, b, q_heads);
     memcpy(g_err, saved, sizeof(g_err));
     return bytes;
 }
@@ -628,38 +710,51 @@ cl_status cl_attention(const cl_kv_cache* cache, const cl_kv_batch* batch, const
                        float* lse, void* ws, size_t ws_bytes, void* stream) {
     const char* who = "cl_attention";
     cl::AttnArgs a{};
-    cl_status st = check_kv(cache, batch, &a.cache, &a.batch, who);
+    const cl_status st = check_kv(cache, batch, &a.cache, &a.batch, who);
     if (st) return st;
-    if (q_heads < 1 || q_heads % cache->kv_heads)
-        return fail(CL_EINVAL, "%s: q_heads (%d) must be a positive multiple of kv_heads (%d)", who, q_heads, cache->kv_heads);
-    if (!q || !out) return fail(CL_EINVAL, "%s: null q or out", who);
-    if (!aligned(q, 16) || q_stride % 8 || !aligned(out, 16))
-        return fail(CL_EINVAL, "%s: q rows and out must be 16-byte aligned", who);
-    if (q_stride < static_cast<int64_t>(q_heads) * cache->head_dim)
-        return fail(CL_EINVAL, "%s: q_stride is shorter than a token's heads", who);
-    if (!cl::attention_size_ok(a.cache, a.batch, q_heads))
-        return fail(CL_EUNSUPPORTED, "%s: rows (tokens * q_heads) and workgroups (num_seqs * q_len * q_heads / 64) must be below 2^31",
-                    who);
-    if (!isfinite(scale)) return fail(CL_EINVAL, "%s: scale must be finite", who);
-    if (window < 0) return fail(CL_EINVAL, "%s: window must not be negative", who);
-    if (!out_type(out_dtype)) return fail(CL_EINVAL, "%s: out_dtype must be CL_FP16, CL_BF16 or CL_FP32", who);
-    if (lse && !aligned(lse, 4)) return fail(CL_EINVAL, "%s: misaligned lse", who);
-    const size_t need = cl::attention_workspace_bytes(a.cache, a.batch, q_heads);
-    if (need > 0) {
-        if (!ws || ws_bytes < need)
-            return fail(CL_EWORKSPACE, "%s: workspace of %zu bytes needed (got %zu)", who, need, ws ? ws_bytes : 0);
-        if (!aligned(ws, 256)) return fail(CL_EINVAL, "%s: workspace must be 256-byte aligned", who);
-    }
-    a.q = static_cast<const uint16_t*>(q);
-    a.q_stride = q_stride;
-    a.q_heads = q_heads;
-    a.causal = causal ? 1 : 0;
-    a.window = window < kMaxKeys ? window : 0;         // a window of the longest sequence hides nothing
-    a.out_dtype = out_dtype;
-    a.scale = scale;
-    a.out = out;
-    a.lse = lse;
-    return hip_status(cl::launch_attention(a, ws, static_cast<hipStream_t>(stream)), who);
+    return attention_checked(a, false, q, q_stride, q_heads, scale, causal, window, out, out_dtype, lse, ws, ws_bytes, stream,
+                             who);
+}
+
+size_t cl_attention8_workspace(const cl_kv_cache8* cache, const cl_kv_batch* batch, int32_t q_heads) {
+    char saved[sizeof(g_err)];
+    memcpy(saved, g_err, sizeof(g_err));
+    cl::KvCache c;
+    cl::KvBatch b;
+    const size_t bytes = attention_bytes(check_kv8(cache, batch, &c, &b, ""), c, b, q_heads);
+    memcpy(g_err, saved, sizeof(g_err));
+    return bytes;
+}
+
+cl_status cl_attention8(const cl_kv_cache8* cache, const cl_kv_batch* batch, const void* q, int64_t q_stride,
+                       int32_t q_heads, float scale, int32_t causal, int32_t window, void* out, int32_t out_dtype,
+                       float* lse, void* ws, size_t ws_bytes, void* stream) {
+    const char* who = "cl_attention8";
+    cl::AttnArgs a{};
+    const cl_status st = check_kv8(cache, batch, &a.cache, &a.batch, who);
+    if (st) return st;
+    return attention_checked(a, true, q, q_stride, q_heads, scale, causal, window, out, out_dtype, lse, ws, ws_bytes, stream,
+                             who);
+}
+
+cl_status cl_kv_read(const cl_kv_cache* cache, const cl_kv_batch* batch, void* k, void* v, void* stream) {
+    const char* who = "cl_kv_read";
+    cl::ReadArgs a{};
+    const cl_status st = check_kv(cache, batch, &a.cache, &a.batch, who);
+    if (st) return st;
+    a.k = static_cast<uint16_t*>(k);
+    a.v = static_cast<uint16_t*>(v);
+    return read_checked(a, false, k, v, stream, who);
+}
+
+cl_status cl_kv_read8(const cl_kv_cache8* cache, const cl_kv_batch* batch, void* k, void* v, void* stream) {
+    const char* who = "cl_kv_read8";
+    cl::ReadArgs a{};
+    const cl_status st = check_kv8(cache, batch, &a.cache, &a.batch, who);
+    if (st) return st;
+    a.k = static_cast<uint16_t*>(k);
+    a.v = static_cast<uint16_t*>(v);
+    return read_checked(a, true, k, v, stream, who);
 }
 
 cl_status cl_moe_route(const cl_router* router, const void* logits, int32_t logits_dtype, int32_t T, int32_t* ids,

@@ -80,11 +80,16 @@ hipError_t launch_all(long long n, F launch) {
 }
 
 // Paged keys and values, validated: [num_pages][heads][page_size][dim] each,
-// page_size = 1 << page_shift.
+// page_size = 1 << page_shift.  A cache of 8 bits has codes behind k and v, a byte
+// each, and scales [num_pages][heads][page_size >> block_shift]: those of pool row
+// r (page, head and row as one number) stand at r >> block_shift.
 struct KvCache {
     uint16_t* k;
     uint16_t* v;
     int num_pages, page_shift, heads, dim, dtype;
+    uint8_t* k_scale;
+    uint8_t* v_scale;
+    int block_shift;
 };
 
 // Sequences of a call, validated.  key_limit is the most keys a sequence may
@@ -118,6 +123,16 @@ struct AppendArgs {
     unsigned first;                // token of the launch's first workgroup
 };
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t st);
+hipError_t launch_kv_append8(const AppendArgs& a, hipStream_t st);               // into a cache of 8 bits (append8.hip)
+
+// The new tokens' rows of the cache, dense, in its 16-bit type (append8.hip).
+struct ReadArgs {
+    KvCache cache;
+    KvBatch batch;
+    uint16_t *k, *v;               // [tokens][heads][dim]
+    unsigned first;                // token of the launch's first workgroup
+};
+hipError_t launch_kv_read(const ReadArgs& a, bool codes, hipStream_t st);
 void rope_frequencies(int rot_dim, double base, int kind, double factor, double trained_len, double low, double high,
                       float* inv_freq, float* magnitude);      // host code
 
@@ -136,6 +151,7 @@ bool attention_dim_ok(int dim);
 bool attention_size_ok(const KvCache& c, const KvBatch& b, int q_heads);   // every number of the launch fits
 size_t attention_workspace_bytes(const KvCache& c, const KvBatch& b, int q_heads);
 hipError_t launch_attention(const AttnArgs& a, void* ws, hipStream_t st);
+hipError_t launch_attention8(const AttnArgs& a, void* ws, hipStream_t st);      // of a cache of 8 bits
 
 // Residual add, gate, combination of slots and norms of one row (norm.hip).
 struct NormArgs {
