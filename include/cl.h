@@ -723,6 +723,168 @@ size_t cl_attention8_workspace(const cl_kv_cache8* cache, const cl_kv_batch* bat
 cl_status cl_kv_read(const cl_kv_cache* cache, const cl_kv_batch* batch, void* k, void* v, void* stream);
 cl_status cl_kv_read8(const cl_kv_cache8* cache, const cl_kv_batch* batch, void* k, void* v, void* stream);
 
+/*
+ * cl_page_pool -- the pages of a cache (of all layers that share their numbers) and
+ * how many table entries hold each.  The calls below keep the counts; a caller
+ * begins with zeros (all pages free) and counts what it holds outside of tables (a
+ * shared prefix) itself, by a table row of its own.
+ *  refs        device int32 [num_pages]; 0: free
+ *  missing     device int32, to which is added how many entries asked for a page
+ *              and got none; or NULL
+ *  buffers     host array: what moves with a page (k and v of every layer, the
+ *              scales of a cache of 8 bits), page p at base + p page_bytes; NULL
+ *              with num_buffers 0
+ *  num_buffers 0..4096;  num_pages >= 1;  page_size as the caches'
+ * Tables: device int32 [rows][width], entries outside 0..num_pages - 1 hold no
+ * page (write -1; the calls do).  Row b holds kv_len[b] keys, prefix_len of them in
+ * a shared prefix outside of the table, the others in its first entries;
+ * pages behind those are held ahead of their keys.
+ * All choices go by number (the lowest free page to the first entry in row
+ * order), so equal calls give equal tables.  A wrong count or entry cannot fail a
+ * call or reach outside the pool; it makes tables wrong.
+ */
+typedef struct cl_page_buffer {
+    void* base;
+    int64_t page_bytes;
+} cl_page_buffer;
+
+typedef struct cl_page_pool {
+    int32_t* refs;
+    int32_t* missing;
+    const cl_page_buffer* buffers;
+    int32_t num_buffers;
+    int32_t num_pages;
+    int32_t page_size;
+} cl_page_pool;
+
+/* Workspace bytes for cl_kv_fork (rows: num_new), cl_kv_reserve (num_seqs) and
+ * cl_kv_compact (1); 0 for rejected arguments. */
+size_t cl_pages_workspace(const cl_page_pool* pool, int32_t rows);
+
+/*
+ * cl_kv_fork -- sequences in place of others: new row i is the sequence of old row
+ * parents[i] (several of one: samples, beams that go on; none of a row: its pages
+ * are given back; a parent outside 0..num_seqs - 1: an empty row, which gets none).  Used pages are
+ * shared.  With room > 0 each row can take `room` more keys at once: a last page that is
+ * partly used becomes the row's own (the first child keeps it where no other row
+ * holds it, the others get copies), and pages are given for what is to come.  Pages
+ * held ahead go to the first child.
+ *  table, kv_len          device [num_seqs][width], [num_seqs]: the old rows, unchanged,
+ *                         whose holdings pass to the new ones
+ *  parents                device int32 [num_new]
+ *  new_table, new_kv_len  device [num_new][width], [num_new] (outputs; may not
+ *                         overlap the old ones)
+ *  room                   0..2^30
+ *  ws                     device workspace, 256-byte aligned
+ * An entry that got no page is -1 (attention over it gives NaN, appends do not
+ * store) and counted in pool->missing, as are keys past the width.
+ * Errors: CL_EINVAL, CL_EWORKSPACE, CL_EHIP.
+ */
+cl_status cl_kv_fork(const cl_page_pool* pool, const int32_t* table, const int32_t* kv_len, int32_t num_seqs,
+                     int32_t width, int32_t prefix_len, const int32_t* parents, int32_t num_new, int32_t room,
+                     int32_t* new_table, int32_t* new_kv_len, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * cl_kv_reserve -- pages for rows that are to grow: a row with want[b] > kv_len[b]
+ * gets what it lacks for want[b] keys, and a partly used last page of its own, a
+ * copy, if others hold it too.
+ *  table, kv_len  device [num_seqs][width] (in place), [num_seqs]
+ *  want           device int32 [num_seqs]
+ * The rest and errors: as cl_kv_fork.
+ */
+cl_status cl_kv_reserve(const cl_page_pool* pool, int32_t* table, const int32_t* kv_len, int32_t num_seqs,
+                        int32_t width, int32_t prefix_len, const int32_t* want, void* ws, size_t ws_bytes,
+                        void* stream);
+
+/*
+ * cl_kv_free -- rows give all their pages back: entries -1, kv_len 0.
+ *  rows  device int32 [num_rows] (others than 0..num_seqs - 1 are passed over; one
+ *        named twice is freed once), or NULL: every row
+ * Errors: CL_EINVAL, CL_EHIP.
+ */
+cl_status cl_kv_free(const cl_page_pool* pool, int32_t* table, int32_t* kv_len, int32_t num_seqs, int32_t width,
+                     const int32_t* rows, int32_t num_rows, void* stream);
+
+/*
+ * cl_kv_compact -- the pages in use become pages 0 .. L - 1: the k-th used page from
+ * number L on moves to the k-th free one below, in all buffers, counts and tables.
+ *  tables  host array [num_tables] (0..16) of device int32 arrays, every one that
+ *          holds pages of the pool (prefix tables too); sizes: host [num_tables],
+ *          their entries
+ *  ws      device workspace, 256-byte aligned
+ * Errors: CL_EINVAL, CL_EWORKSPACE, CL_EHIP.
+ */
+cl_status cl_kv_compact(const cl_page_pool* pool, int32_t num_tables, int32_t* const* tables, const int64_t* sizes,
+                        void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * cl_copy_pages -- page from[i] to page to[i] in all buffers, i < n.  No page may
+ * stand in `to` twice, or in both lists; pairs outside the pool are passed over.
+ * Counts and tables stay.
+ *  from, to  device int32 [n]
+ * Errors: CL_EINVAL, CL_EHIP.
+ */
+cl_status cl_copy_pages(const cl_page_pool* pool, const int32_t* from, const int32_t* to, int32_t n, void* stream);
+
+/*
+ * cl_gather_rows -- row index[i] of each source to row i of its destination, i < n:
+ * what follows beams beside their pages (token histories, states).
+ *  arrays  host array [num_arrays] (1..4096): src [src_rows] and dst [n] rows of
+ *          row_bytes, not overlapping
+ *  index   device int32 [n]; rows of an index outside 0..src_rows - 1 are left alone
+ * Errors: CL_EINVAL, CL_EHIP.
+ */
+typedef struct cl_row_array {
+    const void* src;
+    void* dst;
+    int64_t row_bytes;
+} cl_row_array;
+
+cl_status cl_gather_rows(int32_t num_arrays, const cl_row_array* arrays, int32_t src_rows, const int32_t* index,
+                         int32_t n, void* stream);
+
+/*
+ * cl_beams -- how a beam search goes on.
+ *  alpha  candidates are ranked by score / length^alpha (0: by score)
+ *  beams  1..64 rows a group;  picks  1..64 continuations a group
+ *  eos    the token that finishes a hypothesis, or -1: none
+ */
+typedef struct cl_beams {
+    double alpha;
+    int32_t beams;
+    int32_t picks;
+    int32_t eos;
+} cl_beams;
+
+/*
+ * cl_beam_select -- the best continuations of each group's beams: candidate (b, v)
+ * has the score  scores[b] + l[b][v] - ln sum_v e^{l[b][v]}  and the length
+ * lengths[b] + 1; a finished beam has its score and length at v = eos and -inf
+ * elsewhere.  Picks come by descending rank, ties by the lower beam, then by the
+ * larger logit, then by the lower token.  A beam whose score or whose logits are all
+ * -inf has candidates of -inf; a NaN among its logits, +inf there, or a score that is
+ * NaN or +inf makes all of them NaN, which are picked last.  Ranks are fp64, of sums off by about
+ * 2^-24; scores are rounded once to float32.
+ *  logits   device [groups * beams][vocab] of logits_dtype (CL_FP16, CL_BF16, CL_FP32),
+ *           logits_stride elements from row to row (>= vocab), aligned to its elements
+ *  vocab    1..2^19 (CL_EUNSUPPORTED beyond); picks <= beams * vocab
+ *  scores   device float32 [groups * beams]
+ *  lengths  device int32 [groups * beams], or NULL (alpha 0)
+ *  finished device int32 [groups * beams], not 0: finished; or NULL (needs eos)
+ *  out_scores, tokens, parents  device [groups][picks] float32, int32, int32; a
+ *           parent is a row of logits (cl_kv_fork and cl_gather_rows take them)
+ *  out_lengths, out_finished    device int32 [groups][picks], each or NULL
+ *           (out_lengths with lengths only); no output may overlap an input
+ *  ws       device workspace of cl_beam_workspace(...) bytes, 256-byte aligned
+ * Errors: CL_EINVAL; CL_EUNSUPPORTED, also for groups whose scan takes 2^24
+ * workgroups (of 8192 logits); CL_EWORKSPACE, CL_EHIP.
+ */
+cl_status cl_beam_select(const cl_beams* beams, const void* logits, int32_t logits_dtype, int64_t logits_stride,
+                         int32_t groups, int32_t vocab, const float* scores, const int32_t* lengths,
+                         const int32_t* finished, float* out_scores, int32_t* tokens, int32_t* parents,
+                         int32_t* out_lengths, int32_t* out_finished, void* ws, size_t ws_bytes, void* stream);
+size_t cl_beam_workspace(const cl_beams* beams, int32_t groups, int32_t vocab);
+
 /* Scores of a router. */
 enum { CL_SOFTMAX = 1, CL_SIGMOID = 2 };
 

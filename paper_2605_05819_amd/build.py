@@ -29,7 +29,7 @@ BUILD = os.path.join(os.path.dirname(HERE), "_build")
 LIB = os.path.join(HERE, "libcl.so")
 
 SOURCES = ["api.hip", "quant.hip", "decode.hip", "prefill.hip", "moe.hip", "comp.hip", "ranks.hip",
-           "attention.hip", "attention8.hip", "append.hip", "append8.hip", "norm.hip", "route.hip"]
+           "attention.hip", "attention8.hip", "append.hip", "append8.hip", "pages.hip", "beam.hip", "norm.hip", "route.hip"]
 EXTRA = {"quant.hip": ["-ffp-contract=off"], "comp.hip": ["-ffp-contract=off"], "ranks.hip": ["-ffp-contract=off"]}
 ARCH = "gfx950"
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH,

@@ -80,6 +80,24 @@ class NormC(ctypes.Structure):
                 ("beta", ctypes.c_float)]
 
 
+class PageBufferC(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("page_bytes", ctypes.c_int64)]
+
+
+class PagePoolC(ctypes.Structure):
+    _fields_ = [("refs", ctypes.c_void_p), ("missing", ctypes.c_void_p), ("buffers", ctypes.c_void_p),
+                ("num_buffers", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+
+
+class RowArrayC(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("row_bytes", ctypes.c_int64)]
+
+
+class BeamsC(ctypes.Structure):
+    _fields_ = [("alpha", ctypes.c_double), ("beams", ctypes.c_int32), ("picks", ctypes.c_int32),
+                ("eos", ctypes.c_int32)]
+
+
 _lib = None
 
 _SIGNATURES = {
@@ -159,6 +177,26 @@ _SIGNATURES = {
                                       ctypes.c_size_t, ctypes.c_void_p]),
     "cl_kv_read": (ctypes.c_int32, [ctypes.POINTER(KvCacheC), ctypes.POINTER(KvBatchC), ctypes.c_void_p,
                                     ctypes.c_void_p, ctypes.c_void_p]),
+    "cl_pages_workspace": (ctypes.c_size_t, [ctypes.POINTER(PagePoolC), ctypes.c_int32]),
+    "cl_kv_fork": (ctypes.c_int32, [ctypes.POINTER(PagePoolC), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
+                                    ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32,
+                                    ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+                                    ctypes.c_void_p]),
+    "cl_kv_reserve": (ctypes.c_int32, [ctypes.POINTER(PagePoolC), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
+                                       ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p,
+                                       ctypes.c_size_t, ctypes.c_void_p]),
+    "cl_kv_free": (ctypes.c_int32, [ctypes.POINTER(PagePoolC), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
+                                    ctypes.c_int32, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p]),
+    "cl_kv_compact": (ctypes.c_int32, [ctypes.POINTER(PagePoolC), ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p,
+                                       ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "cl_copy_pages": (ctypes.c_int32, [ctypes.POINTER(PagePoolC), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
+                                       ctypes.c_void_p]),
+    "cl_gather_rows": (ctypes.c_int32, [ctypes.c_int32, ctypes.POINTER(RowArrayC), ctypes.c_int32, ctypes.c_void_p,
+                                        ctypes.c_int32, ctypes.c_void_p]),
+    "cl_beam_workspace": (ctypes.c_size_t, [ctypes.POINTER(BeamsC), ctypes.c_int32, ctypes.c_int32]),
+    "cl_beam_select": (ctypes.c_int32, [ctypes.POINTER(BeamsC), ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
+                                        ctypes.c_int32, ctypes.c_int32] + [ctypes.c_void_p] * 9 +
+                       [ctypes.c_size_t, ctypes.c_void_p]),
     "cl_moe_route": (ctypes.c_int32, [ctypes.POINTER(RouterC), ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32,
                                       ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
                                       ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p]),
@@ -199,7 +237,9 @@ def lib():
 _PACKED = ("cl_linear_decode", "cl_linear_decode_noalloc", "cl_linear_decode_window", "cl_linear_decode_glu",
            "cl_linear_prefill", "cl_linear_workspace", "cl_linear_window_workspace", "cl_prefill_workspace",
            "cl_kv_append", "cl_attention", "cl_attention_workspace", "cl_moe_route", "cl_residual_norm",
-           "cl_kv_append8", "cl_attention8", "cl_attention8_workspace", "cl_kv_read", "cl_kv_read8")
+           "cl_kv_append8", "cl_attention8", "cl_attention8_workspace", "cl_kv_read", "cl_kv_read8",
+           "cl_pages_workspace", "cl_kv_fork", "cl_kv_reserve", "cl_kv_free", "cl_kv_compact", "cl_copy_pages",
+           "cl_gather_rows", "cl_beam_workspace", "cl_beam_select")
 _SCALARS = (ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float)
 _packed = {}
 
@@ -1006,6 +1046,220 @@ def kv_read(cache, batch, k=None, v=None, stream=None):
         _dev_tensor(v, "v", (cache.dtype,), shape)
     _check(_call(cache._read)(cache._bytes, batch._bytes, k.data_ptr(), v.data_ptr(), _raw_stream(stream)))
     return k, v
+
+
+# ------------------------------------------------- pages and who holds them
+
+_PACK_POOL = struct.Struct("PPPiii").pack
+
+
+class PagePool:
+    """The pages of one or more caches (a layer each) that share their numbers
+    (cl_page_pool): refs int32 [num_pages], how many table entries hold each page (0:
+    free; begin with zeros); missing: None, or an int32 [1] tensor to which the
+    calls add the entries that got no page.  Checked once, when it is made."""
+
+    def __init__(self, refs, page_size, caches=(), missing=None):
+        chk = _Checked()
+        _dev_tensor(refs, "refs", _I32, chk=chk)
+        _need(refs.dim() == 1 and refs.numel() > 0, "refs must be [num_pages]")
+        if missing is not None:
+            _dev_tensor(missing, "missing", _I32, (1,), chk)
+        self.refs, self.page_size, self.missing, self.caches = refs, int(page_size), missing, list(caches)
+        self.num_pages = refs.numel()
+        parts = []
+        for i, c in enumerate(self.caches):
+            _need(isinstance(c, (KvCache, KvCache8)), "caches[%d] must be a KvCache or KvCache8" % i)
+            _need(c.num_pages == self.num_pages and c.page_size == self.page_size,
+                  "caches[%d] must have %d pages of %d" % (i, self.num_pages, self.page_size))
+            parts += [c.k, c.v] + ([c.k_scale, c.v_scale] if isinstance(c, KvCache8) else [])
+        chk.on_gpu()
+        # the list that the descriptor points to
+        self._buffers = (PageBufferC * max(1, len(parts)))()
+        for b, t in zip(self._buffers, parts):
+            b.base, b.page_bytes = t.data_ptr(), t[0].numel() * t.element_size()
+        self._bytes = _PACK_POOL(refs.data_ptr(), 0 if missing is None else missing.data_ptr(),
+                                 ctypes.addressof(self._buffers) if parts else 0, len(parts), self.num_pages,
+                                 self.page_size)
+
+    @classmethod
+    def of(cls, caches, missing=None):
+        """A pool over ``caches`` with all pages free."""
+        c = caches[0]
+        return cls(torch.zeros(c.num_pages, dtype=torch.int32, device=c.k.device), c.page_size, caches, missing)
+
+    def packed(self):
+        """The bytes of a cl_page_pool."""
+        return self._bytes
+
+
+def _check_table(table, kv_len, name="table"):
+    _dev_tensor(table, name, _I32)
+    _need(table.dim() == 2, "%s must be [rows][width]" % name)
+    _dev_tensor(kv_len, "kv_len" if name == "table" else "kv_len_out", _I32, (table.shape[0],))
+
+
+def _room(need, ws, device, stream):
+    """A caller's workspace, or a new one."""
+    if ws is None:
+        return _empty((need,), torch.uint8, device, stream)
+    _check_ws(ws, need, None)
+    return ws
+
+
+def pages_workspace(pool, rows):
+    """Workspace bytes of kv_fork (its new rows), kv_reserve (its rows) and kv_compact (1)."""
+    return _call("cl_pages_workspace")(pool._bytes, rows)
+
+
+def kv_fork(pool, table, kv_len, parents, room=0, prefix_len=0, table_out=None, kv_len_out=None, ws=None, stream=None):
+    """``cl_kv_fork``: row i of the result is the sequence of row parents[i] of
+    table int32 [rows][width] and kv_len int32 [rows]; with room > 0 each can
+    take that many keys at once.  Returns (table_out, kv_len_out)."""
+    _check_table(table, kv_len)
+    _dev_tensor(parents, "parents", _I32)
+    n, width = parents.numel(), table.shape[1]
+    if table_out is None:
+        table_out = _empty((n, width), torch.int32, table.device, stream)
+    if kv_len_out is None:
+        kv_len_out = _empty((n,), torch.int32, table.device, stream)
+    _check_table(table_out, kv_len_out, "table_out")
+    _need(tuple(table_out.shape) == (n, width), "table_out must have shape %s" % ((n, width),))
+    ws = _room(pages_workspace(pool, n), ws, table.device, stream)
+    _check(_call("cl_kv_fork")(pool._bytes, table.data_ptr(), kv_len.data_ptr(), table.shape[0], width, prefix_len,
+                               parents.data_ptr(), n, room, table_out.data_ptr(), kv_len_out.data_ptr(), ws.data_ptr(),
+                               ws.numel(), _raw_stream(stream)))
+    return table_out, kv_len_out
+
+
+def kv_reserve(pool, table, kv_len, want, prefix_len=0, ws=None, stream=None):
+    """``cl_kv_reserve``: rows with want[b] > kv_len[b] (int32 [rows]) get the
+    pages they lack for want[b] keys, in place."""
+    _check_table(table, kv_len)
+    _dev_tensor(want, "want", _I32, (table.shape[0],))
+    ws = _room(pages_workspace(pool, table.shape[0]), ws, table.device, stream)
+    _check(_call("cl_kv_reserve")(pool._bytes, table.data_ptr(), kv_len.data_ptr(), table.shape[0], table.shape[1],
+                                  prefix_len, want.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(stream)))
+    return table
+
+
+def kv_free(pool, table, kv_len, rows=None, stream=None):
+    """``cl_kv_free``: the rows named in int32 ``rows`` (None: all) give their
+    pages back; their entries become -1, their kv_len 0."""
+    _check_table(table, kv_len)
+    if rows is not None:
+        _dev_tensor(rows, "rows", _I32)
+        if rows.numel() == 0:
+            return
+    _check(_call("cl_kv_free")(pool._bytes, table.data_ptr(), kv_len.data_ptr(), table.shape[0], table.shape[1],
+                               _opt_ptr(rows), 0 if rows is None else rows.numel(), _raw_stream(stream)))
+
+
+def kv_compact(pool, tables, ws=None, stream=None):
+    """``cl_kv_compact``: the pages in use become the lowest ones; ``tables``:
+    every int32 tensor that holds pages of the pool, renamed in place."""
+    for i, t in enumerate(tables):
+        _dev_tensor(t, "tables[%d]" % i, _I32)
+    tables = [t for t in tables if t.numel()]
+    ws = _room(pages_workspace(pool, 1), ws, pool.refs.device, stream)
+    n = len(tables)
+    at = struct.pack("%dP" % n, *[t.data_ptr() for t in tables]) if n else None
+    size = struct.pack("%dq" % n, *[t.numel() for t in tables]) if n else None
+    _check(_call("cl_kv_compact")(pool._bytes, n, at, size, ws.data_ptr(), ws.numel(), _raw_stream(stream)))
+
+
+def copy_pages(pool, src, dst, stream=None):
+    """``cl_copy_pages``: page src[i] to page dst[i] (int32 [n]) in every cache
+    of the pool.  No page may stand in dst twice, or in both."""
+    _dev_tensor(src, "src", _I32)
+    _need(src.dim() == 1, "src must be [n]")
+    _dev_tensor(dst, "dst", _I32, src.shape)
+    if src.numel():
+        _check(_call("cl_copy_pages")(pool._bytes, src.data_ptr(), dst.data_ptr(), src.numel(), _raw_stream(stream)))
+
+
+def gather_rows(arrays, index, outs=None, stream=None):
+    """``cl_gather_rows``: out[i] = array[index[i]] for each of ``arrays``
+    (contiguous tensors with the same number of rows; index int32).  Returns
+    the outs."""
+    _need(len(arrays) > 0, "one array at least")
+    _dev_tensor(index, "index", _I32)
+    n = index.numel()
+    if outs is None:
+        outs = [None] * len(arrays)
+    _need(len(outs) == len(arrays), "one out per array")
+    outs = list(outs)
+    packed = []
+    for i, t in enumerate(arrays):
+        _need(isinstance(t, torch.Tensor) and t.dim() >= 1 and t.numel() > 0, "arrays[%d] must be a tensor of rows" % i)
+        _dev_tensor(t, "arrays[%d]" % i, (t.dtype,))
+        _need(t.shape[0] == arrays[0].shape[0], "arrays[%d] must have %d rows" % (i, arrays[0].shape[0]))
+        shape = (n,) + tuple(t.shape[1:])
+        if outs[i] is None:
+            outs[i] = _empty(shape, t.dtype, t.device, stream)
+        else:
+            _dev_tensor(outs[i], "outs[%d]" % i, (t.dtype,), shape)
+        packed += [t.data_ptr(), outs[i].data_ptr(), t.numel() // t.shape[0] * t.element_size()]
+    if n:
+        _check(_call("cl_gather_rows")(len(arrays), struct.pack("PPq" * len(arrays), *packed), arrays[0].shape[0],
+                                       index.data_ptr(), n, _raw_stream(stream)))
+    return outs
+
+
+# ----------------------------------------------------------------- beam search
+
+class Beams:
+    """How a beam search goes on (cl_beams): ``beams`` rows a group, ``picks``
+    continuations of them (default: as many), ranked by score / length^alpha;
+    eos: the token that finishes a hypothesis, or -1."""
+
+    def __init__(self, beams, picks=None, eos=-1, alpha=0.0):
+        self.beams, self.picks = int(beams), int(beams if picks is None else picks)
+        self.eos, self.alpha = int(eos), float(alpha)
+        self._bytes = struct.pack("diii4x", self.alpha, self.beams, self.picks, self.eos)
+
+    def packed(self):
+        """The bytes of a cl_beams."""
+        return self._bytes
+
+
+def beam_workspace(rule, groups, vocab):
+    return _call("cl_beam_workspace")(rule._bytes, groups, vocab)
+
+
+def beam_select(rule, logits, scores, lengths=None, finished=None, out=None, ws=None, stream=None):
+    """``cl_beam_select``: logits [groups * beams][vocab] (rows at any stride),
+    scores float32 and lengths, finished int32 of groups * beams -> (scores
+    float32, tokens, parents, lengths, finished int32), each [groups][picks]
+    (lengths None without lengths).  out: such a tuple to be filled."""
+    _need(isinstance(logits, torch.Tensor) and logits.dtype in _OUT, "logits must be an fp16, bf16 or fp32 tensor")
+    _need(logits.dim() == 2 and logits.shape[0] > 0 and logits.shape[0] % max(1, rule.beams) == 0,
+          "logits must be [groups * beams][vocab]")
+    rows, vocab = logits.shape
+    a, b = logits.stride()
+    _need((b == 1 or vocab == 1) and (a >= vocab or rows == 1), "a row of logits must be contiguous")
+    _need(logits.is_cuda, "logits must be on the GPU (got %s)" % logits.device)
+    groups = rows // rule.beams
+    for t, name, dt in ((scores, "scores", torch.float32), (lengths, "lengths", torch.int32),
+                        (finished, "finished", torch.int32)):
+        if t is not None or name == "scores":
+            _dev_tensor(t, name, (dt,))
+            _need(t.numel() == rows, "%s must have %d values" % (name, rows))
+    shape, dts = (groups, rule.picks), (torch.float32,) + (torch.int32,) * 4
+    if out is None:
+        out = tuple(None if i == 3 and lengths is None else _empty(shape, dt, logits.device, stream)
+                    for i, dt in enumerate(dts))
+    else:
+        _need(len(out) == 5, "out must be (scores, tokens, parents, lengths, finished)")
+        for t, dt, name in zip(out, dts, ("scores", "tokens", "parents", "lengths", "finished")):
+            if t is not None or name in ("scores", "tokens", "parents"):
+                _dev_tensor(t, "out " + name, (dt,), shape)
+    need = beam_workspace(rule, groups, vocab)
+    ws = _room(max(need, 1), ws, logits.device, stream)
+    _check(_call("cl_beam_select")(rule._bytes, logits.data_ptr(), _DTYPE_CODE[logits.dtype], a if rows > 1 else vocab,
+                                   groups, vocab, scores.data_ptr(), _opt_ptr(lengths), _opt_ptr(finished),
+                                   *[_opt_ptr(t) for t in out], ws.data_ptr(), ws.numel(), _raw_stream(stream)))
+    return tuple(out)
 
 
 class Router:

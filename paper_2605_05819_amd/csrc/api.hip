@@ -6,6 +6,7 @@
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include <mutex>
@@ -863,6 +864,257 @@ cl_status cl_residual_norm(const cl_norm* norm, const void* y, int32_t y_dtype, 
     a.alpha = norm->alpha;
     a.beta = norm->beta;
     return hip_status(cl::launch_residual_norm(a, static_cast<hipStream_t>(stream)), who);
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------- pages and beams
+
+namespace {
+
+constexpr int kMaxBuffers = 4096;
+
+// The buffers of a pool, or none where memory for their list is out.
+struct Buffers {
+    cl::CopyBuffer few[256];
+    cl::CopyBuffer* many = nullptr;
+    cl::CopyBuffer* get(int n) {
+        if (n <= 256) return few;
+        many = static_cast<cl::CopyBuffer*>(malloc(static_cast<size_t>(n) * sizeof(cl::CopyBuffer)));
+        return many;
+    }
+    ~Buffers() { free(many); }
+};
+
+cl_status check_pool(const cl_page_pool* p, cl::Pool* out, Buffers* buffers, const char* who) {
+    if (!p) return fail(CL_EINVAL, "%s: null pool", who);
+    if (!p->refs || !aligned(p->refs, 4) || !aligned(p->missing, 4))
+        return fail(CL_EINVAL, "%s: null refs, or refs or missing misaligned", who);
+    if (p->num_pages < 1) return fail(CL_EINVAL, "%s: num_pages must be positive", who);
+    if (p->page_size < 1 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)))
+        return fail(CL_EINVAL, "%s: page_size must be a power of two in 1..1024 (got %d)", who, p->page_size);
+    if (p->num_buffers < 0 || p->num_buffers > kMaxBuffers || (p->num_buffers > 0 && !p->buffers))
+        return fail(CL_EINVAL, "%s: num_buffers must be in 0..%d, with their array", who, kMaxBuffers);
+    int shift = 0;
+    while ((1 << shift) < p->page_size) ++shift;
+    *out = {p->refs, p->missing, nullptr, p->num_buffers, p->num_pages, shift};
+    for (int n = 0; n < p->num_buffers; ++n)
+        if (!p->buffers[n].base || p->buffers[n].page_bytes < 1 || p->buffers[n].page_bytes > 0x7fffffffll)
+            return fail(CL_EINVAL, "%s: buffer %d: null base, or page_bytes not in 1..2^31 - 1", who, n);
+    if (!buffers || p->num_buffers == 0) return CL_OK;
+    cl::CopyBuffer* b = buffers->get(p->num_buffers);
+    if (!b) return fail(CL_EINVAL, "%s: no memory for the list of %d buffers", who, p->num_buffers);
+    for (int n = 0; n < p->num_buffers; ++n) {
+        char* base = static_cast<char*>(p->buffers[n].base);
+        b[n] = {base, base, p->buffers[n].page_bytes, 0};
+    }
+    out->buffers = b;
+    return CL_OK;
+}
+
+cl_status check_table(const void* table, const void* kv_len, int rows, int width, int prefix_len, const char* who) {
+    if (rows < 1 || width < 1) return fail(CL_EINVAL, "%s: rows and width must be positive (got %d, %d)", who, rows, width);
+    if (rows > (1 << 20)) return fail(CL_EINVAL, "%s: at most 2^20 rows (got %d)", who, rows);
+    if (prefix_len < 0) return fail(CL_EINVAL, "%s: prefix_len must not be negative", who);
+    if (!table || !kv_len || !aligned(table, 4) || !aligned(kv_len, 4))
+        return fail(CL_EINVAL, "%s: null or misaligned table or kv_len", who);
+    return CL_OK;
+}
+
+cl_status check_room(const void* ws, size_t bytes, size_t need, const char* who) {
+    if (!ws || bytes < need) return fail(CL_EWORKSPACE, "%s: workspace of %zu bytes needed (got %zu)", who, need, ws ? bytes : 0);
+    if (!aligned(ws, 256)) return fail(CL_EINVAL, "%s: workspace must be 256-byte aligned", who);
+    return CL_OK;
+}
+
+bool overlap(const void* a, size_t an, const void* b, size_t bn) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x <= y ? y - x < an : x - y < bn;
+}
+
+cl_status check_beams(const cl_beams* r, int groups, int vocab, cl::BeamArgs* a, const char* who) {
+    if (!r) return fail(CL_EINVAL, "%s: null beams", who);
+    if (!isfinite(r->alpha)) return fail(CL_EINVAL, "%s: alpha must be finite", who);
+    if (r->beams < 1 || r->beams > 64 || r->picks < 1 || r->picks > 64)
+        return fail(CL_EINVAL, "%s: beams and picks must be in 1..64 (got %d, %d)", who, r->beams, r->picks);
+    if (groups < 1 || vocab < 1) return fail(CL_EINVAL, "%s: groups and vocab must be positive (got %d, %d)", who, groups, vocab);
+    if (r->eos < -1 || r->eos >= vocab) return fail(CL_EINVAL, "%s: eos must be a token or -1 (got %d)", who, r->eos);
+    if (vocab > (1 << 19)) return fail(CL_EUNSUPPORTED, "%s: vocab must be at most 2^19 (got %d)", who, vocab);
+    if (r->picks > static_cast<long long>(r->beams) * vocab)
+        return fail(CL_EINVAL, "%s: %d picks of %d beams and %d tokens", who, r->picks, r->beams, vocab);
+    a->groups = groups;
+    a->beams = r->beams;
+    a->picks = r->picks;
+    a->vocab = vocab;
+    a->eos = r->eos;
+    a->alpha = r->alpha;
+    if (!cl::beam_fits(*a))
+        return fail(CL_EUNSUPPORTED, "%s: the scan of %d groups would take 2^24 workgroups", who, groups);
+    return CL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t cl_pages_workspace(const cl_page_pool* pool, int32_t rows) {
+    if (!pool || pool->num_pages < 1 || rows < 1 || rows > (1 << 20)) return 0;
+    return cl::pages_workspace_bytes(pool->num_pages, rows);
+}
+
+cl_status cl_kv_fork(const cl_page_pool* pool, const int32_t* table, const int32_t* kv_len, int32_t num_seqs,
+                     int32_t width, int32_t prefix_len, const int32_t* parents, int32_t num_new, int32_t room,
+                     int32_t* new_table, int32_t* new_kv_len, void* ws, size_t ws_bytes, void* stream) {
+    const char* who = "cl_kv_fork";
+    cl::Pool p;
+    Buffers buffers;
+    cl_status st = check_pool(pool, &p, &buffers, who);
+    if (!st) st = check_table(table, kv_len, num_seqs, width, prefix_len, who);
+    if (!st) st = check_table(new_table, new_kv_len, num_new, width, prefix_len, who);
+    if (st) return st;
+    if (!parents || !aligned(parents, 4)) return fail(CL_EINVAL, "%s: null or misaligned parents", who);
+    if (room < 0 || room > (1 << 30)) return fail(CL_EINVAL, "%s: room must be in 0..2^30 (got %d)", who, room);
+    const size_t row = static_cast<size_t>(width) * 4;
+    if (overlap(table, row * num_seqs, new_table, row * num_new) ||
+        overlap(kv_len, static_cast<size_t>(num_seqs) * 4, new_kv_len, static_cast<size_t>(num_new) * 4))
+        return fail(CL_EINVAL, "%s: the new rows overlap the old ones", who);
+    st = check_room(ws, ws_bytes, cl::pages_workspace_bytes(p.num_pages, num_new), who);
+    if (st) return st;
+    const cl::PageTable from{const_cast<int32_t*>(table), const_cast<int32_t*>(kv_len), num_seqs, width, prefix_len, p.page_shift};
+    const cl::PageTable to{new_table, new_kv_len, num_new, width, prefix_len, p.page_shift};
+    return hip_status(cl::launch_kv_fork(p, from, parents, to, room, ws, static_cast<hipStream_t>(stream)), who);
+}
+
+cl_status cl_kv_reserve(const cl_page_pool* pool, int32_t* table, const int32_t* kv_len, int32_t num_seqs,
+                        int32_t width, int32_t prefix_len, const int32_t* want, void* ws, size_t ws_bytes,
+                        void* stream) {
+    const char* who = "cl_kv_reserve";
+    cl::Pool p;
+    Buffers buffers;
+    cl_status st = check_pool(pool, &p, &buffers, who);
+    if (!st) st = check_table(table, kv_len, num_seqs, width, prefix_len, who);
+    if (st) return st;
+    if (!want || !aligned(want, 4)) return fail(CL_EINVAL, "%s: null or misaligned want", who);
+    st = check_room(ws, ws_bytes, cl::pages_workspace_bytes(p.num_pages, num_seqs), who);
+    if (st) return st;
+    const cl::PageTable t{table, const_cast<int32_t*>(kv_len), num_seqs, width, prefix_len, p.page_shift};
+    return hip_status(cl::launch_kv_reserve(p, t, want, ws, static_cast<hipStream_t>(stream)), who);
+}
+
+cl_status cl_kv_free(const cl_page_pool* pool, int32_t* table, int32_t* kv_len, int32_t num_seqs, int32_t width,
+                     const int32_t* rows, int32_t num_rows, void* stream) {
+    const char* who = "cl_kv_free";
+    cl::Pool p;
+    cl_status st = check_pool(pool, &p, nullptr, who);
+    if (!st) st = check_table(table, kv_len, num_seqs, width, 0, who);
+    if (st) return st;
+    if (!aligned(rows, 4)) return fail(CL_EINVAL, "%s: misaligned rows", who);
+    if (rows && (num_rows < 1 || num_rows > (1 << 20)))
+        return fail(CL_EINVAL, "%s: num_rows must be in 1..2^20 (got %d)", who, num_rows);
+    const cl::PageTable t{table, kv_len, num_seqs, width, 0, p.page_shift};
+    return hip_status(cl::launch_kv_free(p, t, rows, num_rows, static_cast<hipStream_t>(stream)), who);
+}
+
+cl_status cl_kv_compact(const cl_page_pool* pool, int32_t num_tables, int32_t* const* tables, const int64_t* sizes,
+                        void* ws, size_t ws_bytes, void* stream) {
+    const char* who = "cl_kv_compact";
+    cl::Pool p;
+    Buffers buffers;
+    cl_status st = check_pool(pool, &p, &buffers, who);
+    if (st) return st;
+    if (num_tables < 0 || num_tables > cl::kMaxTables || (num_tables > 0 && (!tables || !sizes)))
+        return fail(CL_EINVAL, "%s: num_tables must be in 0..%d, with their arrays", who, cl::kMaxTables);
+    for (int n = 0; n < num_tables; ++n)
+        if (!tables[n] || !aligned(tables[n], 4) || sizes[n] < 1)
+            return fail(CL_EINVAL, "%s: table %d is null, misaligned or empty", who, n);
+    st = check_room(ws, ws_bytes, cl::pages_workspace_bytes(p.num_pages, 1), who);
+    if (st) return st;
+    return hip_status(cl::launch_kv_compact(p, num_tables, tables, sizes, ws, static_cast<hipStream_t>(stream)), who);
+}
+
+cl_status cl_copy_pages(const cl_page_pool* pool, const int32_t* from, const int32_t* to, int32_t n, void* stream) {
+    const char* who = "cl_copy_pages";
+    cl::Pool p;
+    Buffers buffers;
+    const cl_status st = check_pool(pool, &p, &buffers, who);
+    if (st) return st;
+    if (n < 1) return fail(CL_EINVAL, "%s: n must be positive (got %d)", who, n);
+    if (!from || !to || !aligned(from, 4) || !aligned(to, 4)) return fail(CL_EINVAL, "%s: null or misaligned from or to", who);
+    cl::CopyArgs a{};
+    a.from = from;
+    a.to = to;
+    a.n = n;
+    a.from_rows = a.to_rows = p.num_pages;
+    return hip_status(cl::launch_copy_rows(a, p.buffers, p.num_buffers, static_cast<hipStream_t>(stream)), who);
+}
+
+cl_status cl_gather_rows(int32_t num_arrays, const cl_row_array* arrays, int32_t src_rows, const int32_t* index,
+                         int32_t n, void* stream) {
+    const char* who = "cl_gather_rows";
+    if (num_arrays < 1 || num_arrays > kMaxBuffers || !arrays)
+        return fail(CL_EINVAL, "%s: num_arrays must be in 1..%d, with their list", who, kMaxBuffers);
+    if (src_rows < 1 || n < 1) return fail(CL_EINVAL, "%s: src_rows and n must be positive (got %d, %d)", who, src_rows, n);
+    if (!index || !aligned(index, 4)) return fail(CL_EINVAL, "%s: null or misaligned index", who);
+    Buffers buffers;
+    cl::CopyBuffer* b = buffers.get(num_arrays);
+    if (!b) return fail(CL_EINVAL, "%s: no memory for the list of %d arrays", who, num_arrays);
+    for (int i = 0; i < num_arrays; ++i) {
+        const cl_row_array& x = arrays[i];
+        if (!x.src || !x.dst || x.row_bytes < 1 || x.row_bytes > 0x7fffffffll)
+            return fail(CL_EINVAL, "%s: array %d: null src or dst, or row_bytes not in 1..2^31 - 1", who, i);
+        if (overlap(x.src, static_cast<size_t>(x.row_bytes) * src_rows, x.dst, static_cast<size_t>(x.row_bytes) * n))
+            return fail(CL_EINVAL, "%s: array %d: src and dst overlap", who, i);
+        b[i] = {static_cast<const char*>(x.src), static_cast<char*>(x.dst), x.row_bytes, 0};
+    }
+    cl::CopyArgs a{};
+    a.from = index;
+    a.n = n;
+    a.from_rows = src_rows;
+    a.to_rows = n;
+    return hip_status(cl::launch_copy_rows(a, b, num_arrays, static_cast<hipStream_t>(stream)), who);
+}
+
+size_t cl_beam_workspace(const cl_beams* beams, int32_t groups, int32_t vocab) {
+    char saved[sizeof(g_err)];
+    memcpy(saved, g_err, sizeof(g_err));
+    cl::BeamArgs a{};
+    const size_t bytes = check_beams(beams, groups, vocab, &a, "") == CL_OK ? cl::beam_workspace_bytes(a) : 0;
+    memcpy(g_err, saved, sizeof(g_err));
+    return bytes;
+}
+
+cl_status cl_beam_select(const cl_beams* beams, const void* logits, int32_t logits_dtype, int64_t logits_stride,
+                         int32_t groups, int32_t vocab, const float* scores, const int32_t* lengths,
+                         const int32_t* finished, float* out_scores, int32_t* tokens, int32_t* parents,
+                         int32_t* out_lengths, int32_t* out_finished, void* ws, size_t ws_bytes, void* stream) {
+    const char* who = "cl_beam_select";
+    cl::BeamArgs a{};
+    cl_status st = check_beams(beams, groups, vocab, &a, who);
+    if (st) return st;
+    if (!out_type(logits_dtype)) return fail(CL_EINVAL, "%s: logits_dtype must be CL_FP16, CL_BF16 or CL_FP32", who);
+    if (!logits || !scores || !out_scores || !tokens || !parents)
+        return fail(CL_EINVAL, "%s: null logits, scores, out_scores, tokens or parents", who);
+    if (!aligned(logits, type_size(logits_dtype)) || !aligned(scores, 4) || !aligned(lengths, 4) || !aligned(finished, 4) ||
+        !aligned(out_scores, 4) || !aligned(tokens, 4) || !aligned(parents, 4) || !aligned(out_lengths, 4) ||
+        !aligned(out_finished, 4))
+        return fail(CL_EINVAL, "%s: an array is not aligned to its elements", who);
+    if (logits_stride < vocab) return fail(CL_EINVAL, "%s: logits_stride is shorter than a row", who);
+    if (!lengths && (a.alpha != 0.0 || out_lengths)) return fail(CL_EINVAL, "%s: alpha and out_lengths need lengths", who);
+    if (finished && a.eos < 0) return fail(CL_EINVAL, "%s: finished beams need an eos", who);
+    st = check_room(ws, ws_bytes, cl::beam_workspace_bytes(a), who);
+    if (st) return st;
+    a.logits = logits;
+    a.dtype = logits_dtype;
+    a.stride = logits_stride;
+    a.scores = scores;
+    a.lengths = lengths;
+    a.finished = finished;
+    a.out_scores = out_scores;
+    a.tokens = tokens;
+    a.parents = parents;
+    a.out_lengths = out_lengths;
+    a.out_finished = out_finished;
+    return hip_status(cl::launch_beam_select(a, ws, static_cast<hipStream_t>(stream)), who);
 }
 
 }  // extern "C"

@@ -182,6 +182,85 @@ struct RouteArgs {
 };
 hipError_t launch_moe_route(RouteArgs a, hipStream_t st);
 
+// Pages and their holders (pages.hip).
+struct CopyBuffer {                // rows of `bytes`, at src and dst
+    const char* src;
+    char* dst;
+    long long bytes;
+    int align;                     // 16, 4 or 1: of both and of the rows' length
+};
+constexpr int kMaxCopyBuffers = 96;            // of a launch: its arguments stay within 4 KB
+struct CopyArgs {
+    const int32_t *from, *to, *count;          // rows; null: their number, n of them
+    int n, from_rows, to_rows;
+    int buffers, chunks;
+    CopyBuffer buffer[kMaxCopyBuffers];
+};
+hipError_t launch_copy_rows(CopyArgs a, const CopyBuffer* buffers, int n, hipStream_t st);
+
+struct Pool {                      // validated
+    int32_t* refs;                 // [num_pages]
+    int32_t* missing;              // may be null
+    const CopyBuffer* buffers;
+    int num_buffers, num_pages, page_shift;
+};
+struct PageTable {
+    int32_t* pages;                // [rows][width]
+    int32_t* kv_len;               // [rows]
+    int rows, width, prefix_len, page_shift;
+};
+struct ForkArgs {
+    PageTable from, to;
+    const int32_t* parents;
+    int32_t *refs, *keep;          // keep: holders of a row's last page if it is the row's alone, else 0; -1: no row
+    int num_pages;
+};
+struct GiveArgs {
+    PageTable table;
+    int32_t *refs, *missing;
+    const int32_t *want, *keep;    // want null: room keys behind every row's; keep null: 1
+    int32_t *count, *copy_from, *copy_to, *free;
+    int num_pages, room;
+};
+struct FreeArgs {
+    PageTable table;
+    int32_t* refs;
+    const int32_t* rows;
+    int num_pages;
+};
+constexpr int kMaxTables = 16;
+struct CompactArgs {
+    int32_t *refs, *head, *from, *to, *rank;   // head: moves, pages in use
+    int num_pages, tables;
+    int32_t* table[kMaxTables];
+    long long size[kMaxTables];
+};
+size_t pages_workspace_bytes(int num_pages, int rows);
+hipError_t launch_kv_fork(const Pool& pool, const PageTable& from, const int32_t* parents, const PageTable& to, int room,
+                          void* ws, hipStream_t st);
+hipError_t launch_kv_reserve(const Pool& pool, const PageTable& table, const int32_t* want, void* ws, hipStream_t st);
+hipError_t launch_kv_free(const Pool& pool, const PageTable& table, const int32_t* rows, int n, hipStream_t st);
+hipError_t launch_kv_compact(const Pool& pool, int tables, int32_t* const* table, const int64_t* size, void* ws, hipStream_t st);
+
+// A beam search's step (beam.hip).
+struct BeamArgs {
+    const void* logits;
+    long long stride;              // elements from row to row
+    const float* scores;
+    const int32_t *lengths, *finished;         // may be null
+    float* out_scores;
+    int32_t *tokens, *parents, *out_lengths, *out_finished;
+    double alpha;
+    int groups, beams, picks, vocab, eos, dtype;
+    int chunk, splits;             // of a row's logits
+    unsigned long long* best;      // [rows][splits][picks], descending
+    double* sum;                   // [rows][splits]: of e^(l - most)
+    float* most;
+};
+bool beam_fits(const BeamArgs& a);
+size_t beam_workspace_bytes(BeamArgs a);
+hipError_t launch_beam_select(BeamArgs a, void* ws, hipStream_t st);
+
 // Rank allocation (host code, ranks.hip): salient-set size and salience
 // ratio of one descending spectrum; ranks of one compensation window (cont,
 // if not null, receives the continuous ranks before alignment); layer scores

@@ -1,0 +1,241 @@
+"""Forks, reservations, frees, compactions and copies of pages against plain loops: tables, counts, contents.  Everything is
+whole numbers or copies, so everything is equal."""
+
+import random
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import pages
+from paper_2605_05819_amd import cl
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16 = torch.float16, torch.bfloat16
+
+
+def i32(x, *shape):
+    t = torch.tensor(x, dtype=torch.int32, device="cuda")
+    return t.view(*shape) if shape else t
+
+
+class World:
+    """A pool of pages with several buffers on the device, and the oracle's lists of the same."""
+
+    def __init__(self, num, size, rows, width, layers=2, heads=2, dim=64, eight=False, prefix=0, seed=0):
+        g = torch.Generator().manual_seed(seed)
+        rnd = lambda *s: torch.randint(0, 256, s, generator=g, dtype=torch.int32).to(torch.uint8)  # noqa: E731
+        self.caches = []
+        for i in range(layers):
+            if eight:
+                block = min(size, 4)
+                self.caches.append(cl.KvCache8(*[x.cuda() for x in (rnd(num, heads, size, dim), rnd(num, heads, size, dim),
+                                                                    rnd(num, heads, size // block), rnd(num, heads, size // block))], F16))
+            else:
+                k, v = (rnd(num, heads, size, 2 * dim).view(F16).view(num, heads, size, dim).cuda() for _ in range(2))
+                self.caches.append(cl.KvCache(k, v))
+        self.missing = i32([0])
+        self.pool = cl.PagePool.of(self.caches, self.missing)
+        self.table, self.len = i32([-1] * (rows * width), rows, width), i32([0] * rows)
+        self.num, self.size, self.prefix, self.short = num, size, prefix, 0
+        self.refs, self.t, self.n = [0] * num, [[-1] * width for _ in range(rows)], [0] * rows
+        self.want = [x.cpu().clone() for x in self.buffers()]
+
+    def buffers(self):
+        return [x.view(torch.uint8).view(self.num, -1) for c in self.caches for x in
+                ((c.k, c.v, c.k_scale, c.v_scale) if isinstance(c, cl.KvCache8) else (c.k, c.v))]
+
+    def copied(self, copies):
+        for x in self.want:
+            old = x.clone()
+            for f, t in copies:
+                x[t] = old[f]
+
+    def set(self, n):
+        self.n = list(n)
+        self.len.copy_(i32(self.n))
+
+    def reserve(self, want):
+        cl.kv_reserve(self.pool, self.table, self.len, i32(want), prefix_len=self.prefix)
+        copies, m = pages.reserve(self.refs, self.t, self.n, want, self.size, self.prefix)
+        self.copied(copies)
+        self.short += m
+        return copies
+
+    def fork(self, parents, room):
+        self.table, self.len = cl.kv_fork(self.pool, self.table, self.len, i32(parents), room=room, prefix_len=self.prefix)
+        self.t, self.n, copies, m = pages.fork(self.refs, self.t, self.n, parents, self.size, room, self.prefix)
+        self.copied(copies)
+        self.short += m
+        return copies
+
+    def free(self, rows):
+        cl.kv_free(self.pool, self.table, self.len, rows=None if rows is None else i32(rows))
+        pages.free(self.refs, self.t, self.n, range(len(self.t)) if rows is None else rows)
+
+    def compact(self, *more):
+        cl.kv_compact(self.pool, [self.table] + [m[0] for m in more])
+        w = len(self.t[0])
+        flat = [p for t in self.t for p in t]
+        copies = pages.compact(self.refs, [flat] + [m[1] for m in more])
+        self.t = [flat[i:i + w] for i in range(0, len(flat), w)]
+        self.copied(copies)
+        return copies
+
+    def check(self):
+        torch.cuda.synchronize()
+        assert self.pool.refs.tolist() == self.refs
+        assert self.table.tolist() == self.t and self.len.tolist() == self.n
+        assert int(self.missing) == self.short
+        for got, want in zip(self.buffers(), self.want):
+            assert torch.equal(got.cpu(), want)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_calls_in_any_order(seed):
+    g = random.Random(seed)
+    size = g.choice((1, 4, 16, 64))
+    prefix = g.choice((0, 0, 10))
+    w = World(g.randint(8, 300), size, g.randint(1, 9), g.randint(2, 90), layers=g.randint(1, 3), eight=seed % 2 == 1, prefix=prefix,
+              seed=seed)
+    for _ in range(14):
+        what = g.choice(("reserve", "reserve", "fork", "fork", "free", "compact"))
+        rows, width = len(w.t), len(w.t[0])
+        if what == "reserve":
+            want = [x + g.choice((0, 1, g.randint(0, 3 * size), -1, g.randint(0, width * size + 2))) for x in w.n]
+            w.reserve(want)
+            w.set([max(x, min(y, prefix + width * size)) for x, y in zip(w.n, want)])
+        elif what == "fork":
+            w.fork([g.randint(-1, rows) for _ in range(g.randint(1, 12))], g.choice((0, 1, 1, 1, 2 * size + 1)))
+        elif what == "free":
+            w.free([g.randint(-1, rows) for _ in range(g.randint(1, 4))] if g.random() < 0.9 else None)
+        else:
+            w.compact()
+        w.check()
+
+
+def test_large_tables_and_pools():
+    """More rows than the scanning workgroup has threads, more pages than a pass of its, more buffers than a launch takes."""
+    g = random.Random(3)
+    w = World(9000, 4, 1500, 40, layers=55, heads=1, dim=64, seed=1)
+    w.reserve([g.choice((0, 1, 4, 9, 17)) for _ in range(1500)])
+    w.set([g.choice((0, 1, 2, 3, 4)) if t[0] >= 0 else 0 for t in w.t])
+    w.check()
+    w.fork([g.randint(0, 1499) for _ in range(1300)], 1)
+    w.check()
+    w.free([g.randint(0, 1299) for _ in range(700)])
+    assert len(w.compact()) > 100
+    w.check()
+
+
+def test_shortage_is_counted_and_leaves_the_rest_whole():
+    w = World(5, 4, 3, 4)
+    w.reserve([8, 8, 8])                      # six pages of five
+    assert w.short == 1
+    w.check()
+    w.set([7, 7, 3])
+    w.fork([0, 0, 1, 1], 1)                   # copies that find one free page (row 2's)
+    w.check()
+    assert w.short > 1
+
+
+def test_compact_renames_every_table_given():
+    w = World(40, 8, 4, 6)
+    w.reserve([40, 30, 20, 10])
+    prefix = [w.t[3][0], w.t[3][1], -1, 99]
+    dev = i32(prefix)
+    w.free([1])
+    assert w.compact((dev, prefix))
+    w.check()
+    assert dev.tolist() == prefix
+    assert not w.compact((dev, prefix))       # nothing left to move
+    w.check()
+
+
+def test_rows_named_twice_and_empty_calls():
+    w = World(20, 4, 3, 4)
+    w.reserve([16, 9, 3])
+    w.fork([0, 0, 1], 0)
+    w.free([1, 1, 1, 7, -2])
+    w.check()
+    assert w.refs == [1] * 7 + [0] * 13
+    cl.kv_free(w.pool, w.table, w.len, rows=i32([]))
+    cl.kv_compact(w.pool, [])
+    cl.copy_pages(w.pool, i32([]), i32([]))
+    w.check()
+
+
+def test_copy_pages_and_gather_rows():
+    w = World(12, 4, 1, 1, eight=True)
+    cl.copy_pages(w.pool, i32([3, 5, -1, 40, 2]), i32([0, 11, 1, 2, 12]))
+    w.copied([(3, 0), (5, 11)])
+    w.check()
+    g = torch.Generator().manual_seed(0)
+    rows = [torch.randint(0, 100, (7, 33), generator=g, dtype=torch.int32), torch.randn((7, 3, 5), generator=g).half(),
+            torch.randint(0, 2, (7,), generator=g).to(torch.uint8), torch.randn((7, 9001), generator=g, dtype=torch.float64)]
+    dev = [r.cuda() for r in rows]
+    index = [6, 0, 0, 3, -1, 7, 2]
+    outs = [torch.full_like(r, 5) for r in dev]
+    assert cl.gather_rows(dev, i32(index), outs) == outs
+    fresh = cl.gather_rows(dev, i32([1, 1, 4]))
+    torch.cuda.synchronize()
+    for r, o, f in zip(rows, outs, fresh):
+        for i, j in enumerate(index):
+            assert torch.equal(o[i].cpu(), r[j] if 0 <= j < 7 else torch.full_like(r[0], 5))
+        assert torch.equal(f.cpu(), r[[1, 1, 4]])
+
+
+def test_pools_past_2_31_bytes():
+    """Pages whose offsets pass 32 bits move and are found again."""
+    size, heads, dim = 64, 8, 128
+    num = (1 << 32) // (size * heads * dim * 2) + 5
+    k = torch.empty((num, heads, size, dim), dtype=F16, device="cuda")
+    v = torch.empty_like(k)
+    pool = cl.PagePool.of([cl.KvCache(k, v)])
+    table = torch.tensor([[num - 1, num - 2, -1]], dtype=torch.int32, device="cuda")
+    pool.refs[num - 2:] = 1
+    k[num - 2:] = torch.randn((2, heads, size, dim), device="cuda").half()
+    v[num - 2:] = torch.randn((2, heads, size, dim), device="cuda").half()
+    want = k[num - 1].clone(), v[num - 2].clone()
+    cl.kv_compact(pool, [table])
+    torch.cuda.synchronize()
+    assert table.tolist() == [[1, 0, -1]] and torch.equal(k[1], want[0]) and torch.equal(v[0], want[1])
+    cl.copy_pages(pool, i32([1, 0]), i32([num - 1, num - 3]))
+    torch.cuda.synchronize()
+    assert torch.equal(k[num - 1], want[0]) and torch.equal(v[num - 3], want[1])
+
+
+def test_captured_steps_replay_like_eager_ones():
+    """Two graphs of a fork there and back, each with its own workspace, replayed in turn with eager work between."""
+    def world():
+        w = World(200, 8, 4, 12, eight=True, seed=5)
+        w.reserve([50, 41, 33, 10])
+        w.set([50, 41, 33, 10])
+        return w
+
+    a, b = world(), world()
+    parents = i32([0, 0, 2, 1])
+    spare = [(torch.empty_like(w.table), torch.empty_like(w.len)) for w in (a, b)]
+
+    def step(w, s):
+        cl.kv_fork(w.pool, w.table, w.len, parents, room=1, table_out=s[0], kv_len_out=s[1])
+        cl.kv_fork(w.pool, s[0], s[1], parents, room=9, table_out=w.table, kv_len_out=w.len)
+        cl.kv_compact(w.pool, [w.table])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(a, spare[0])
+        step(b, spare[1])
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(a, spare[0])
+    for i in range(5):
+        parents.copy_(i32([[0, 0, 2, 1], [3, 1, 1, 1], [0, 1, 2, 3], [2, 2, 3, 3], [1, 0, 1, 0]][i]))
+        graph.replay()
+        step(b, spare[1])
+        torch.cuda.synchronize()
+        for x, y in zip([a.table, a.len, a.pool.refs] + a.buffers(), [b.table, b.len, b.pool.refs] + b.buffers()):
+            assert torch.equal(x, y)
