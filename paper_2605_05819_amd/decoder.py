@@ -8,14 +8,20 @@
     y       = down_e(SiLU(gate_e n) * up_e n)  cl.moe_route, cl.moe_linear_decode_*      (experts)
     h, n    = h + y (or its weighted slots), the next layer's norm
 
+Behind the layers :func:`beam_search` goes on with several hypotheses of each prompt:
+
+    pages     for the prompt and the next token     cl.kv_reserve, cl.kv_fork
+    tokens    the best of beams and vocabulary      cl.beam_select
+    rows      tables, pages, histories in order     cl.kv_fork, cl.gather_rows
+
 ``h`` is the residual stream and ``n`` its normalised value, both [tokens][hidden];
 a step takes the pair and returns the next layer's.  Up to 64 tokens go through
 the decode calls, more (dense layers only) through the prefill ones.
 
     python -m paper_2605_05819_amd.decoder
 
-runs a few layers of random weights over a prompt and some decode steps, and
-prints the times.
+runs a few layers of random weights over a prompt and some decode steps, then a
+beam search over a cache of 8 bits, and prints the times.
 """
 
 import time
@@ -137,6 +143,77 @@ def run(layers, caches, batch, x, norms, last_norm, eps=1e-6):
     return h, n
 
 
+@dataclass
+class Hypotheses:
+    """The rows of a beam search, ``beams`` for each prompt, best first."""
+    tokens: torch.Tensor                # int32 [rows][steps]: what was chosen so far
+    scores: torch.Tensor                # float32 [rows]: sums of log probabilities
+    lengths: torch.Tensor               # int32 [rows]: tokens of a hypothesis, its eos among them
+    finished: torch.Tensor              # int32 [rows]
+
+
+def beam_search(layers, caches, pool, norms, last_norm, embed, head, prompts, rule, steps, eps=1e-6):
+    """The best hypotheses of ``steps`` tokens behind each of ``prompts`` (int32
+    tensors) by ``rule`` (a cl.Beams whose picks are its beams).  embed and head
+    [vocab][hidden] in the activations' dtype; logits are fp32.  ``caches`` (16 or 8
+    bits, one a layer) hold the pages of ``pool``, which are given back at the end.
+    A full pool is an error."""
+    if rule.picks != rule.beams:
+        raise ValueError("a beam search goes on with as many picks as it has beams")
+    dev, n = embed.device, rule.beams
+    counts = [len(p) for p in prompts]
+    rows, size = n * len(prompts), pool.page_size
+    if rows > DECODE_TOKENS:
+        raise ValueError("a beam search takes at most %d rows" % DECODE_TOKENS)
+    missing = pool.missing
+    if missing is None:
+        raise ValueError("the pool of a beam search needs its count of missing pages")
+    missing.zero_()
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=dev)  # noqa: E731
+    width = -(-(max(counts) + steps) // size)
+
+    def logits(n_):
+        return torch.mm(n_, head.t(), out_dtype=torch.float32)
+
+    # the prompts, a row each
+    kv_len = i32([0] * len(prompts))
+    table = torch.full((len(prompts), width), -1, dtype=torch.int32, device=dev)
+    cl.kv_reserve(pool, table, kv_len, i32(counts))
+    kv_len.copy_(i32(counts))
+    ends = torch.tensor(counts, device=dev).cumsum(0)
+    start = torch.cat([ends.new_zeros(1), ends]).to(torch.int32)
+    batch = cl.KvBatch(kv_len, table, sum(counts), q_len=max(counts), q_start=start, max_kv_len=max(counts))
+    _, y = run(layers, caches, batch, embed[torch.cat(list(prompts)).long()], norms, last_norm, eps)
+    # every hypothesis but a prompt's first begins with a score of -inf: the first choice is among the first's tokens
+    old = cl.kv_fork(pool, table, kv_len, i32([g for g in range(len(prompts)) for _ in range(n)]))
+    new = tuple(torch.empty_like(t) for t in old)
+    x = logits(y[ends - 1]).repeat_interleave(n, 0)
+    s = Hypotheses(torch.zeros((rows, steps), dtype=torch.int32, device=dev),
+                   torch.where(torch.arange(rows, device=dev) % n == 0, 0.0, float("-inf")),
+                   torch.zeros(rows, dtype=torch.int32, device=dev), torch.zeros(rows, dtype=torch.int32, device=dev))
+    spare = torch.empty_like(s.tokens)
+    finished = s.finished if rule.eos >= 0 else None
+    for step in range(steps):
+        scores, tokens, parents, lengths, done = cl.beam_select(rule, x, s.scores, s.lengths, finished)
+        cl.gather_rows([s.tokens], parents, [spare])
+        spare, s.tokens = s.tokens, spare
+        s.tokens[:, step] = tokens.view(-1)
+        s.scores, s.lengths, s.finished = scores.view(-1), lengths.view(-1), done.view(-1)
+        finished = s.finished if rule.eos >= 0 else None
+        if step + 1 == steps:
+            break
+        table, kv_len = cl.kv_fork(pool, *old, parents.view(-1), room=1, table_out=new[0], kv_len_out=new[1])
+        old, new = new, old
+        kv_len.add_(1)
+        batch = cl.KvBatch(kv_len, table, rows, max_kv_len=max(counts) + step + 1)
+        _, y = run(layers, caches, batch, embed[tokens.view(-1).long()], norms, last_norm, eps)
+        x = logits(y)
+    cl.kv_free(pool, *old)
+    if int(missing):
+        raise RuntimeError("the pool had %d pages too few" % int(missing))
+    return s
+
+
 # ------------------------------------------------------------------ the example
 
 def _random_linear(g, d_out, d_in, rank=32, dev="cuda"):
@@ -192,6 +269,20 @@ def main(layers=4, seqs=8, prompt=256, steps=16, page=64):
         graph.replay()
     torch.cuda.synchronize()
     print("decode: %d sequences, %.1f us a layer and token" % (seqs, (time.perf_counter() - t) / (steps - 1) / layers * 1e6))
+    # four hypotheses of each of four prompts, over a cache of 8 bits
+    vocab, beams, groups = 32000, 4, 4
+    embed = torch.randn((vocab, hidden), generator=g, device=dev).to(dt)
+    head = embed * 0.02
+    caches = [cl.KvCache8.empty(2 * groups * width, page, kv_heads, head_dim, 16, dt, dev) for _ in stack]
+    pool = cl.PagePool.of(caches, torch.zeros(1, dtype=torch.int32, device=dev))
+    prompts = [torch.randint(0, vocab, (prompt - 7 * i,), generator=g, device=dev, dtype=torch.int32) for i in range(groups)]
+    for _ in range(2):
+        torch.cuda.synchronize()
+        t = time.perf_counter()
+        found = beam_search(stack, caches, pool, norms[:-1], norms[-1], embed, head, prompts, cl.Beams(beams), steps)
+        torch.cuda.synchronize()
+    print("beam search: %d x %d hypotheses of %d tokens, %.1f ms; best scores %s"
+          % (groups, beams, steps, (time.perf_counter() - t) * 1e3, [round(x, 2) for x in found.scores[::beams].tolist()]))
 
 
 if __name__ == "__main__":
