@@ -1247,15 +1247,19 @@ def beam_select(rule, logits, scores, lengths=None, finished=None, out=None, ws=
             _need(t.numel() == rows, "%s must have %d values" % (name, rows))
     shape, dts = (groups, rule.picks), (torch.float32,) + (torch.int32,) * 4
     if out is None:
-        out = tuple(None if i == 3 and lengths is None else _empty(shape, dt, logits.device, stream)
-                    for i, dt in enumerate(dts))
+        s, *rest = _empty((5,) + shape, torch.int32, logits.device, stream).unbind(0)      # one allocation
+        out = [s.view(torch.float32), *rest]
+        if lengths is None:
+            out[3] = None
     else:
         _need(len(out) == 5, "out must be (scores, tokens, parents, lengths, finished)")
         for t, dt, name in zip(out, dts, ("scores", "tokens", "parents", "lengths", "finished")):
             if t is not None or name in ("scores", "tokens", "parents"):
                 _dev_tensor(t, "out " + name, (dt,), shape)
-    need = beam_workspace(rule, groups, vocab)
-    ws = _room(max(need, 1), ws, logits.device, stream)
+    if ws is None:
+        ws = _empty((max(beam_workspace(rule, groups, vocab), 1),), torch.uint8, logits.device, stream)
+    else:
+        _dev_tensor(ws, "ws", (torch.uint8,))
     _check(_call("cl_beam_select")(rule._bytes, logits.data_ptr(), _DTYPE_CODE[logits.dtype], a if rows > 1 else vocab,
                                    groups, vocab, scores.data_ptr(), _opt_ptr(lengths), _opt_ptr(finished),
                                    *[_opt_ptr(t) for t in out], ws.data_ptr(), ws.numel(), _raw_stream(stream)))

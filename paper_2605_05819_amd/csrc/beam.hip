@@ -7,16 +7,16 @@
 // needs the sum.  Two launches:
 //
 //  * beam_scan: a workgroup takes a chunk of a row into registers, once: its sum of
-//    exponentials and its k best logits.  The k-th largest of a wave's lane
-//    maxima bounds the k-th best from below; what reaches the largest such bound
-//    of the workgroup (little more than k values) goes to a list in LDS, where each
-//    counts how many stand ahead of it.  Where ties fill the list, the k best are
-//    taken one after another instead.
+//    exponentials and its k best logits.  Where each of the four waves has k / 4
+//    lanes whose maxima reach a bound, k values do; what reaches the least of the
+//    waves' k / 4-th largest lane maxima (two or three times k values as a rule) goes to
+//    a list in LDS, where each counts how many stand ahead of it.  Where ties fill
+//    the list, the k best are taken one after another instead.
 //  * beam_pick: a workgroup a group: sums joined per beam in fp64, a beam's k best
 //    from its chunks' (a lane walks a chunk's list), then the ranks in fp64, each
 //    candidate counting those ahead of it.
 //
-// The sums are the only rounding that can change an order: an exponential is off
+// The sums (and a length's power, off by some 2^-51) are the only rounding that can change an order: an exponential is off
 // by 2^-23 of itself, differently for each value, terms are added in fp32 within a
 // lane and in fp64 beyond, so a row's logarithm is off by some 2^-24 / sqrt(lanes).
 // Bound by the read of the logits and by the issue of about ten instructions a
@@ -85,13 +85,13 @@ struct Wide {
 // A lane holds EPT values: VEC neighbours (16 bytes) a load, the wave's loads side
 // by side, so token(j) rises with j and with the lane inside a load.
 template <int DT, int EPT>
-__global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
+__global__ __launch_bounds__(256, 8) void beam_scan_kernel(BeamArgs a) {
     constexpr int VEC = DT == DT_FP32 ? 4 : 8, LOADS = EPT / VEC;
     __shared__ u64 list[kList];
     __shared__ int filled;
     __shared__ float tops[4];
     __shared__ uint32_t bounds[4];
-    __shared__ double sums[4];
+    __shared__ float sums[256];
     __shared__ u64 best[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
@@ -101,47 +101,65 @@ __global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
     const char* const from = static_cast<const char*>(a.logits) + static_cast<size_t>(row) * a.stride * size;
     const auto token = [&](int j) { return base + (j / VEC) * 64 * VEC + lane * VEC + j % VEC; };
 
+    const bool full = split * a.chunk + a.chunk <= a.vocab;
     float x[EPT], group[LOADS];
     Wide raw[LOADS];
+    const auto value = [&](const Wide& w, int j) {
+        if constexpr (DT == DT_FP32) return __builtin_bit_cast(float, w.w[j]);
+        else return act_to_f32(static_cast<uint16_t>(j & 1 ? w.w[j / 2] >> 16 : w.w[j / 2]), DT);
+    };
+    if (full) {
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i)
-        if (token(i * VEC) + VEC <= a.vocab) raw[i] = *reinterpret_cast<const Wide*>(from + static_cast<size_t>(token(i * VEC)) * size);
+        for (int i = 0; i < LOADS; ++i) raw[i] = *reinterpret_cast<const Wide*>(from + static_cast<size_t>(token(i * VEC)) * size);
+    } else {
+        // whole pieces, then the row's last values one by one into theirs
+        const uint32_t none = DT == DT_FP32 ? 0xff800000u : DT == DT_BF16 ? 0xff80ff80u : 0xfc00fc00u;      // -inf
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-        if (token(i * VEC) + VEC <= a.vocab) {
+        for (int i = 0; i < LOADS; ++i) {
+            raw[i] = Wide{{none, none, none, none}};
+            if (token(i * VEC) + VEC <= a.vocab)
+                raw[i] = *reinterpret_cast<const Wide*>(from + static_cast<size_t>(token(i * VEC)) * size);
+        }
+#pragma unroll 1
+        for (int i = 0; i < LOADS; ++i) {
+            const int t = token(i * VEC);
+            if (t >= a.vocab || t + VEC <= a.vocab) continue;
+            Wide w = {{none, none, none, none}};
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                if constexpr (DT == DT_FP32) {
-                    x[i * VEC + j] = __builtin_bit_cast(float, raw[i].w[j]);
-                } else {
-                    const uint32_t w = raw[i].w[j / 2];
-                    x[i * VEC + j] = act_to_f32(static_cast<uint16_t>(j & 1 ? w >> 16 : w), DT);
+            for (int j = 0; j < VEC; ++j)
+                if (t + j < a.vocab) {
+                    if constexpr (DT == DT_FP32) {
+                        w.w[j] = reinterpret_cast<const uint32_t*>(from)[t + j];
+                    } else {
+                        const uint32_t h = reinterpret_cast<const uint16_t*>(from)[t + j];
+                        w.w[j / 2] = j & 1 ? (w.w[j / 2] & 0xffffu) | h << 16 : (w.w[j / 2] & 0xffff0000u) | h;
+                    }
                 }
-            }
-        } else {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const int t = token(i * VEC + j);
-                x[i * VEC + j] = -INFINITY;
-                if (t < a.vocab) {
-                    if constexpr (DT == DT_FP32) x[i * VEC + j] = reinterpret_cast<const float*>(from)[t];
-                    else x[i * VEC + j] = act_to_f32(reinterpret_cast<const uint16_t*>(from)[t], DT);
-                }
-            }
+            for (int n = 0; n < LOADS; ++n)
+                if (n == i) raw[n] = w;
         }
     }
-    float mine = -INFINITY;                  // NaN is passed over: it makes the sum NaN, and the row has no list then
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[i * VEC + j] = value(raw[i], j);
+    // (a NaN makes the sum NaN, and the row has no list then; the maxima only have
+    // to take it without more instructions)
+    float mine = -INFINITY;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
         group[i] = x[i * VEC];
 #pragma unroll
-        for (int j = 1; j < VEC; ++j) group[i] = fmaxf(group[i], x[i * VEC + j]);
-        mine = fmaxf(mine, group[i]);
+        for (int j = 1; j < VEC; ++j) group[i] = __builtin_elementwise_maximum(group[i], x[i * VEC + j]);
+        mine = __builtin_elementwise_maximum(mine, group[i]);
     }
-    // the k-th largest of the lanes' maxima
-    const uint32_t own = token(0) < a.vocab ? order_key(mine != mine ? -INFINITY : mine) : 0u;
-    uint32_t key = own, kth = 0;
-    for (int j = 0; j < a.picks; ++j) {
+    // lane maxima one after another: k / 4 of each wave, and the least of the
+    // waves' last ones; in a row's last chunk, where waves may be empty, k of each,
+    // and the largest
+    const int each = full ? (a.picks + 3) / 4 : a.picks;
+    uint32_t key = token(0) < a.vocab ? order_key(mine != mine ? -INFINITY : mine) : 0u, kth = 0;
+    for (int j = 0; j < each; ++j) {
         kth = wave_max_u32(key);
         if (j == 0 && lane == 0) tops[wave] = kth ? from_key(kth) : -INFINITY;
         const uint64_t has = __ballot(key == kth);
@@ -153,16 +171,16 @@ __global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
     const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
     uint32_t bound = bounds[0];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) bound = bound > bounds[w] ? bound : bounds[w];
+    for (int w = 1; w < 4; ++w) bound = full ? min(bound, bounds[w]) : max(bound, bounds[w]);
     const float least = bound ? from_key(bound) : -INFINITY;
 
-    // e^(x - top), the difference first: what rounding adds is then different for each value
-    const float zero = top == -INFINITY ? 0.f : top;
+    // 2^(x log2 e - zero): what rounding adds is different for each value, as long as
+    // the reference is `zero` itself and not the maximum that it was rounded from
+    const float zero = top == -INFINITY ? 0.f : top * kLog2e;
     float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < EPT; ++j) s += __builtin_amdgcn_exp2f((x[j] - zero) * kLog2e);
-    const double total = wave_sum(static_cast<double>(s));
-    if (lane == 0) sums[wave] = total;
+    for (int j = 0; j < EPT; ++j) s += __builtin_amdgcn_exp2f(fmaf(x[j], kLog2e, -zero));
+    sums[tid] = s;
 
 #pragma unroll
     for (int i = 0; i < LOADS; ++i)
@@ -177,9 +195,12 @@ __global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
     __syncthreads();
     const size_t slot = static_cast<size_t>(row) * a.splits + split;
     u64* const out = a.best + slot * a.picks;
-    if (tid == 0) {
-        a.sum[slot] = sums[0] + sums[1] + sums[2] + sums[3];
-        a.most[slot] = zero;
+    if (wave == 3) {
+        const double total = wave_sum(static_cast<double>(sums[lane]) + sums[lane + 64] + sums[lane + 128] + sums[lane + 192]);
+        if (lane == 0) {
+            a.sum[slot] = total;
+            a.most[slot] = zero;
+        }
     }
     const int n = filled;
     if (n <= kList) {
@@ -239,20 +260,26 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a, int waves)
             const int row = g * a.beams + b;
             const bool done = a.finished && a.finished[row];
             const int len = (a.lengths ? a.lengths[row] : 0) + (done ? 0 : 1);
-            const double by = a.alpha != 0.0 ? pow(static_cast<double>(len > 1 ? len : 1), a.alpha) : 1.0;
+            // the lists' loads go ahead of the sums' chain
+            u64* const mine = lists + static_cast<size_t>(wave) * a.splits * a.picks;
+            const u64* const from = a.best + static_cast<size_t>(row) * a.splits * a.picks;
+            if (!done)
+                for (int i = lane; i < a.splits * a.picks; i += 64) mine[i] = from[i];
+            const double by = a.alpha != 0.0 && len > 1 ? exp(a.alpha * log(static_cast<double>(len))) : 1.0;
             const double before = static_cast<double>(a.scores[row]);
             // all candidates of one score: a finished beam's -inf, a beam of -inf, NaN
             double same = -INFINITY, lse = 0.0;
             bool plain = done;
             if (!done) {
                 const size_t at = static_cast<size_t>(row) * a.splits + lane;
-                const float m = lane < a.splits ? a.most[at] : -INFINITY;
+                const float m = lane < a.splits ? a.most[at] : -INFINITY;      // in units of log2 e, as the kernel above has it
                 const double s = lane < a.splits ? a.sum[at] : 0.0;
                 float top = m;
 #pragma unroll
                 for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-                const double sum = wave_sum(s == 0.0 ? 0.0 : s * exp(static_cast<double>(m) - static_cast<double>(top)));
-                lse = static_cast<double>(top) + log(sum);
+                const double unit = 1.0 / static_cast<double>(kLog2e);
+                const double sum = wave_sum(s == 0.0 ? 0.0 : s * exp((static_cast<double>(m) - static_cast<double>(top)) * unit));
+                lse = static_cast<double>(top) * unit + log(sum);
                 if (sum == 0.0) plain = true;                          // no logit above -inf
                 if (!(fabs(sum) <= 1.7976931348623157e308) || !(before <= 3.4028234663852886e38)) plain = true, same = NAN;
                 else if (before == -INFINITY) plain = true;
@@ -272,9 +299,6 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a, int waves)
                 }
                 continue;
             }
-            u64* const mine = lists + static_cast<size_t>(wave) * a.splits * a.picks;
-            const u64* const from = a.best + static_cast<size_t>(row) * a.splits * a.picks;
-            for (int i = lane; i < a.splits * a.picks; i += 64) mine[i] = from[i];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             int next = 0;
