@@ -875,7 +875,10 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
 
     // Q8: the same rows as codes in registers, 16 a lane and piece, loaded a step
     // ahead in place of the copies and written to LDS as 16-bit values when their
-    // buffer is free
+    // buffer is free, at the head of a step.  (32 conversions a wave and tile beside
+    // 64 MFMAs: ragged prompts 927 us, 862 from 16 bits.  The codes copied to LDS
+    // first and converted between the MFMAs took 972; held in registers until then,
+    // they spill.)
     constexpr int CQ = WR * D / 1024, QC = D / 16;    // pieces of a lane, pieces of a row
     struct Codes {
         u32x4 c[CQ > 0 ? CQ : 1];

@@ -105,15 +105,54 @@ __global__ __launch_bounds__(256) void fork_rows_kernel(ForkArgs a) {
     }
 }
 
+// The same by one wave, for few small rows.
+__device__ __forceinline__ void fork_row(const ForkArgs& a, int i) {
+    const int lane = threadIdx.x & 63, width = a.from.width;
+    const int p = i < a.to.rows ? a.parents[i] : -1;
+    const bool valid = p >= 0 && p < a.from.rows;
+    int earlier = 0, mine = 0, siblings = 0;
+    for (int base = 0; base < a.to.rows; base += 64) {
+        const int j = base + lane, q = j < a.to.rows ? a.parents[j] : -1;
+        earlier += __popcll(__ballot(j < i && q == p));
+        mine += __popcll(__ballot(j < a.to.rows && q == i));
+        siblings += __popcll(__ballot(j < a.to.rows && q == p));
+    }
+    if (i < a.to.rows) {
+        const int len = valid ? max(a.from.kv_len[p], 0) : 0;
+        const int used = entries_of(a.from, own_keys(a.from, len));
+        for (int e = lane; e < width; e += 64) {
+            const int page = valid && (e < used || earlier == 0) ? a.from.pages[static_cast<size_t>(p) * width + e] : -1;
+            a.to.pages[static_cast<size_t>(i) * width + e] = in_pool(page, a.num_pages) ? page : -1;
+        }
+        if (lane == 0) {
+            a.to.kv_len[i] = len;
+            a.keep[i] = !valid ? -1 : earlier == 0 ? siblings : 0;
+        }
+    }
+    if (i < a.from.rows) {
+        const int used = entries_of(a.from, own_keys(a.from, a.from.kv_len[i]));
+        for (int e = lane; e < width; e += 64) {
+            const int page = a.from.pages[static_cast<size_t>(i) * width + e], more = e < used ? mine - 1 : mine > 0 ? 0 : -1;
+            if (more != 0 && in_pool(page, a.num_pages)) atomicAdd(a.refs + page, more);
+        }
+    }
+}
+
 // ------------------------------------------------------------- giving pages
 
 // One workgroup: rows that are to grow ask for a page of their own in place of a
 // last one that others hold too (a copy), then for the entries they lack; the
 // lowest free pages go to them in row order.  What is free is scanned before any
-// count changes here, so no page is both copied from and given away.
-__global__ __launch_bounds__(kScan) void give_pages_kernel(GiveArgs a) {
+// count changes here, so no page is both copied from and given away.  LANES work
+// on a row: a wave where rows ask for many entries, one where they ask for a few (64
+// rows of one entry 5.7 us, 12 by waves).
+template <int LANES>
+__device__ __forceinline__ void give_pages(const GiveArgs& a) {
     __shared__ int waves[kScan / 64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid % LANES, team = tid / LANES;
+    constexpr int TEAMS = kScan / LANES;
+    // the lanes of a row that hold true, as bits from the row's first lane
+    const auto votes = [&](bool v) { return LANES == 64 ? static_cast<uint64_t>(__ballot(v)) : static_cast<uint64_t>(v); };
     const PageTable& t = a.table;
     int over = 0;                                  // entries past the table's width
 
@@ -145,11 +184,11 @@ __global__ __launch_bounds__(kScan) void give_pages_kernel(GiveArgs a) {
         return r;
     };
 
-    for (int i = wave; i < t.rows; i += kScan / 64) {
+    for (int i = team; i < t.rows; i += TEAMS) {
         const Ask r = ask_of(i);
         int n = r.page >= 0 ? 1 : 0;
-        for (int e = r.used; e < r.need; e += 64)
-            n += __popcll(__ballot(e + lane < r.need && !in_pool(t.pages[static_cast<size_t>(i) * t.width + e + lane], a.num_pages)));
+        for (int e = r.used; e < r.need; e += LANES)
+            n += __popcll(votes(e + lane < r.need && !in_pool(t.pages[static_cast<size_t>(i) * t.width + e + lane], a.num_pages)));
         if (lane == 0) {
             a.count[i] = n;
             a.copy_from[i] = r.page;
@@ -186,7 +225,7 @@ __global__ __launch_bounds__(kScan) void give_pages_kernel(GiveArgs a) {
     }
     __syncthreads();
     const int have = min(found, asked);
-    for (int i = wave; i < t.rows; i += kScan / 64) {
+    for (int i = team; i < t.rows; i += TEAMS) {
         int32_t* const row = t.pages + static_cast<size_t>(i) * t.width;
         const int old = a.copy_from[i];
         int at = a.count[i];
@@ -208,9 +247,9 @@ __global__ __launch_bounds__(kScan) void give_pages_kernel(GiveArgs a) {
             }
         }
         if (lane == 0) a.copy_to[i] = to;
-        for (int e = used; e < need; e += 64) {
+        for (int e = used; e < need; e += LANES) {
             const bool lacks = e + lane < need && !in_pool(row[e + lane], a.num_pages);
-            const uint64_t who = __ballot(lacks);
+            const uint64_t who = votes(lacks);
             if (lacks) {
                 const int k = at + __popcll(who & ((1ull << lane) - 1));
                 const int page = k < have ? a.free[k] : -1;
@@ -224,6 +263,21 @@ __global__ __launch_bounds__(kScan) void give_pages_kernel(GiveArgs a) {
         if (over) atomicAdd(a.missing, over);
         if (tid == 0 && asked > have) atomicAdd(a.missing, asked - have);
     }
+}
+
+template <int LANES>
+__global__ __launch_bounds__(kScan) void give_pages_kernel(GiveArgs a) {
+    give_pages<LANES>(a);
+}
+
+// A small fork whole: its rows, then their pages.  The counts that the first part
+// changes by atomics are read only in the second.
+__global__ __launch_bounds__(kScan) void fork_and_give_kernel(ForkArgs f, GiveArgs a) {
+    const int rows = max(f.from.rows, f.to.rows);
+    for (int i = threadIdx.x / 64; i < rows; i += kScan / 64) fork_row(f, i);
+    __threadfence();
+    __syncthreads();
+    give_pages<1>(a);
 }
 
 // ------------------------------------------------------------------ freeing
@@ -284,12 +338,12 @@ __global__ __launch_bounds__(kScan) void plan_moves_kernel(CompactArgs a) {
     if (tid == 0) a.head[0] = movers, a.head[1] = L;
 }
 
-__global__ __launch_bounds__(256) void rename_pages_kernel(CompactArgs a) {
+// Table entries by their pages' new numbers, by workgroup `block` of `blocks`.
+__device__ __forceinline__ void rename_pages(const CompactArgs& a, unsigned block, unsigned blocks) {
     const int L = a.head[1];
     for (int n = 0; n < a.tables; ++n) {
         int32_t* const table = a.table[n];
-        for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < a.size[n];
-             i += static_cast<long long>(gridDim.x) * 256) {
+        for (long long i = static_cast<long long>(block) * 256 + threadIdx.x; i < a.size[n]; i += static_cast<long long>(blocks) * 256) {
             const int page = table[i];
             if (page < L || page >= a.num_pages) continue;
             const int k = a.rank[page];
@@ -318,10 +372,10 @@ __device__ __forceinline__ void copy_chunk(const char* from, char* to, int bytes
 // Row from[i] of every buffer's source to row to[i] of its destination (i where
 // there is no such array), i < n.  A workgroup takes turns of 16 KB; rows out of
 // range, and rows that go nowhere (-1), are passed over.
-__global__ __launch_bounds__(256) void copy_rows_kernel(CopyArgs a) {
+__device__ __forceinline__ void copy_rows(const CopyArgs& a, unsigned block, unsigned blocks) {
     const int n = a.count ? min(*a.count, a.n) : a.n;
     const long long turns = static_cast<long long>(n) * a.buffers * a.chunks;
-    for (long long turn = blockIdx.x; turn < turns; turn += gridDim.x) {
+    for (long long turn = block; turn < turns; turn += blocks) {
         const int c = static_cast<int>(turn % a.chunks);
         const long long rest = turn / a.chunks;
         const int b = static_cast<int>(rest % a.buffers), i = static_cast<int>(rest / a.buffers);
@@ -339,6 +393,15 @@ __global__ __launch_bounds__(256) void copy_rows_kernel(CopyArgs a) {
     }
 }
 
+__global__ __launch_bounds__(256) void copy_rows_kernel(CopyArgs a) { copy_rows(a, blockIdx.x, gridDim.x); }
+
+// A compaction's moves and new names, which need nothing of each other: `renaming`
+// workgroups, the first ones, see to the tables.
+__global__ __launch_bounds__(256) void move_pages_kernel(CopyArgs c, CompactArgs a, unsigned renaming) {
+    if (blockIdx.x < renaming) rename_pages(a, blockIdx.x, renaming);
+    else copy_rows(c, blockIdx.x - renaming, gridDim.x - renaming);
+}
+
 size_t up256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 
 // Parts of a workspace.
@@ -353,21 +416,27 @@ struct Room {
 
 }  // namespace
 
+// The buffers from number `first` on into a launch's arguments, as many as it takes;
+// its workgroups.
+static unsigned fill(CopyArgs& a, const CopyBuffer* buffers, int first, int n) {
+    a.buffers = n - first < kMaxCopyBuffers ? n - first : kMaxCopyBuffers;
+    long long most = 1;
+    for (int b = 0; b < a.buffers; ++b) {
+        a.buffer[b] = buffers[first + b];
+        CopyBuffer& buf = a.buffer[b];
+        const uintptr_t bits = reinterpret_cast<uintptr_t>(buf.src) | reinterpret_cast<uintptr_t>(buf.dst) |
+                               static_cast<uintptr_t>(buf.bytes);
+        buf.align = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 1;
+        if (buf.bytes > most) most = buf.bytes;
+    }
+    a.chunks = static_cast<int>((most + kChunk - 1) / kChunk);
+    const long long turns = static_cast<long long>(a.n) * a.buffers * a.chunks;
+    return static_cast<unsigned>(turns < 8192 ? turns : 8192);
+}
+
 hipError_t launch_copy_rows(CopyArgs a, const CopyBuffer* buffers, int n, hipStream_t st) {
     for (int first = 0; first < n; first += kMaxCopyBuffers) {
-        a.buffers = n - first < kMaxCopyBuffers ? n - first : kMaxCopyBuffers;
-        long long most = 1;
-        for (int b = 0; b < a.buffers; ++b) {
-            a.buffer[b] = buffers[first + b];
-            CopyBuffer& buf = a.buffer[b];
-            const uintptr_t bits = reinterpret_cast<uintptr_t>(buf.src) | reinterpret_cast<uintptr_t>(buf.dst) |
-                                   static_cast<uintptr_t>(buf.bytes);
-            buf.align = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 1;
-            if (buf.bytes > most) most = buf.bytes;
-        }
-        a.chunks = static_cast<int>((most + kChunk - 1) / kChunk);
-        const long long turns = static_cast<long long>(a.n) * a.buffers * a.chunks;
-        const unsigned grid = static_cast<unsigned>(turns < 8192 ? turns : 8192);
+        const unsigned grid = fill(a, buffers, first, n);
         hipLaunchKernelGGL(copy_rows_kernel, dim3(grid), dim3(256), 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -384,8 +453,12 @@ size_t pages_workspace_bytes(int num_pages, int rows) {
 
 namespace {
 
-hipError_t give(const Pool& pool, const PageTable& table, const int32_t* want, int room, const int32_t* keep, Room ws,
+// f: a fork whose rows come first, in the same launch if each has a wave of its own
+// (4 rows of 20 entries 13.2 us with their copies, 16.5 in two launches; 64 rows of 64
+// would take 27 for 18).
+hipError_t give(const Pool& pool, const PageTable& table, const int32_t* want, int room, const ForkArgs* f, Room ws,
                 hipStream_t st) {
+    const int32_t* const keep = f ? f->keep : nullptr;
     GiveArgs g{};
     g.table = table;
     g.refs = pool.refs;
@@ -398,7 +471,17 @@ hipError_t give(const Pool& pool, const PageTable& table, const int32_t* want, i
     g.copy_from = ws.ints(table.rows);
     g.copy_to = ws.ints(table.rows);
     g.free = ws.ints(pool.num_pages);
-    hipLaunchKernelGGL(give_pages_kernel, dim3(1), dim3(kScan), 0, st, g);
+    const int rows = f && f->from.rows > table.rows ? f->from.rows : table.rows;
+    const bool little = f && rows <= kScan / 64 && table.width <= 256 && room <= 4 << table.page_shift;
+    if (little) {
+        hipLaunchKernelGGL(fork_and_give_kernel, dim3(1), dim3(kScan), 0, st, *f, g);
+    } else if (f) {
+        hipLaunchKernelGGL(fork_rows_kernel, dim3(rows), dim3(256), 0, st, *f);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (!little && f && room <= 4 << table.page_shift) hipLaunchKernelGGL(give_pages_kernel<1>, dim3(1), dim3(kScan), 0, st, g);
+    else if (!little) hipLaunchKernelGGL(give_pages_kernel<64>, dim3(1), dim3(kScan), 0, st, g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || pool.num_buffers == 0) return e;
     CopyArgs c{};
@@ -421,10 +504,9 @@ hipError_t launch_kv_fork(const Pool& pool, const PageTable& from, const int32_t
     f.refs = pool.refs;
     f.num_pages = pool.num_pages;
     f.keep = r.ints(to.rows);
+    if (room > 0) return give(pool, to, nullptr, room, &f, r, st);
     hipLaunchKernelGGL(fork_rows_kernel, dim3(from.rows > to.rows ? from.rows : to.rows), dim3(256), 0, st, f);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || room == 0) return e;
-    return give(pool, to, nullptr, room, f.keep, r, st);
+    return hipGetLastError();
 }
 
 hipError_t launch_kv_reserve(const Pool& pool, const PageTable& table, const int32_t* want, void* ws, hipStream_t st) {
@@ -456,20 +538,21 @@ hipError_t launch_kv_compact(const Pool& pool, int tables, int32_t* const* table
     hipLaunchKernelGGL(plan_moves_kernel, dim3(1), dim3(kScan), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (pool.num_buffers) {
-        CopyArgs c{};
-        c.from = a.from;
-        c.to = a.to;
-        c.count = a.head;
-        c.n = pool.num_pages;
-        c.from_rows = c.to_rows = pool.num_pages;
-        e = launch_copy_rows(c, pool.buffers, pool.num_buffers, st);
-        if (e != hipSuccess) return e;
-    }
-    if (tables == 0) return hipSuccess;
-    const int64_t blocks = (most + 255) / 256;
-    hipLaunchKernelGGL(rename_pages_kernel, dim3(static_cast<unsigned>(blocks < 1024 ? blocks : 1024)), dim3(256), 0, st, a);
-    return hipGetLastError();
+    CopyArgs c{};
+    c.from = a.from;
+    c.to = a.to;
+    c.count = a.head;
+    c.n = pool.num_pages;
+    c.from_rows = c.to_rows = pool.num_pages;
+    unsigned grid = fill(c, pool.buffers, 0, pool.num_buffers);
+    if (pool.num_buffers == 0) grid = 0;
+    const int64_t blocks = tables ? (most + 255) / 256 : 0;
+    const unsigned renaming = static_cast<unsigned>(blocks < 1024 ? blocks : 1024);
+    if (grid + renaming == 0) return hipSuccess;
+    hipLaunchKernelGGL(move_pages_kernel, dim3(grid + renaming), dim3(256), 0, st, c, a, renaming);
+    e = hipGetLastError();
+    if (e != hipSuccess || pool.num_buffers <= kMaxCopyBuffers) return e;
+    return launch_copy_rows(c, pool.buffers + kMaxCopyBuffers, pool.num_buffers - kMaxCopyBuffers, st);
 }
 
 }  // namespace cl
