@@ -157,3 +157,28 @@ def test_outputs_in_place_of_new_ones_repeat_bit_for_bit_and_replay():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_the_largest_lists():
+    """64 beams and picks over 2^19 tokens: a group's candidates and two waves' lists fill the LDS; with ties in every chunk."""
+    g = torch.Generator().manual_seed(11)
+    x = torch.randn((64, 1 << 19), generator=g).to(F16)
+    x[5] = 1.0
+    x[9, 100000:] = -float("inf")
+    check(x, (-3 * torch.rand(64, generator=g)).tolist(), 64, 64, lengths=[7] * 64, finished=[int(i == 3) for i in range(64)], eos=12345)
+
+
+def test_more_groups_than_a_grid_of_small_ones():
+    """30000 groups of 2 beams: a workgroup each, equal inputs in every thousandth."""
+    g = torch.Generator(device="cuda").manual_seed(12)
+    x = torch.randn((60000, 70), device="cuda", generator=g)
+    x[2000:4000] = x[:2000]
+    scores = -torch.rand(60000, device="cuda", generator=g)
+    scores[2000:4000] = scores[:2000]
+    s, t, p, n, f = cl.beam_select(cl.Beams(2, picks=3), x, scores)
+    torch.cuda.synchronize()
+    assert n is None and torch.equal(s[:1000], s[1000:2000]) and torch.equal(t[:1000], t[1000:2000])
+    assert torch.equal(p[:1000] + 2000, p[1000:2000]) and not f.any()
+    total = (scores[:, None].double() + torch.log_softmax(x.double(), 1)).view(30000, 140)
+    want = total.sort(dim=1, descending=True).values[:, :3]
+    assert (s.double() - want).abs().max() <= 2.0 ** -20

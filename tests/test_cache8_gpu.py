@@ -307,6 +307,53 @@ def test_append_against_oracle(D, page, block, inter, norm, dtype):
             at += a
 
 
+@pytest.mark.parametrize("D,page,block,inter,norm,prefix", [(128, 64, 16, False, True, 0), (128, 32, 32, True, False, 7), (128, 64, 64, False, False, 0),
+                                                            (128, 128, 128, False, True, 100), (64, 64, 64, True, True, 0), (64, 16, 1, False, False, 0),
+                                                            (256, 32, 16, False, True, 0), (256, 64, 32, True, False, 0), (64, 1024, 512, False, True, 0)])
+def test_append_of_prompts(D, page, block, inter, norm, prefix):
+    """Several hundred tokens at once, long and short sequences side by side, empty ones, blocks begun before and rows of no
+    sequence on both sides: every block size a wave holds, and those it does not."""
+    g = np.random.default_rng(D + block)
+    dtype = BF16 if inter else F16
+    Hkv = 3
+    p = Pool([700, 40, 400, 33, 20, 1, 130], Hkv, D, page, block, dtype, prefix=prefix, seed=block)
+    freq = cl.rope_frequencies(D, 10000.0)[0]
+    w = torch.from_numpy(1 + 0.2 * g.standard_normal(D)).to(dtype)
+    rope = cl.Rope(freq.cuda(), interleaved=inter)
+    lens = np.zeros(7, np.int64)
+    for counts in ([333, 0, 300, 5, 1, 0, 77], [350, 33, 1, 20, 3, 0, 40], [1, 1, 90, 0, 16, 1, 0]):
+        lens += counts
+        N, ahead = sum(counts), 5
+        start = torch.tensor(np.concatenate([[0], np.cumsum(counts)]) + ahead, dtype=torch.int32).cuda()
+        pre = torch.zeros(-(-prefix // page), dtype=torch.int32).cuda() if prefix else None
+        batch = cl.KvBatch(torch.tensor(lens, dtype=torch.int32).cuda(), p.table.cuda(), N + 9, q_len=max(counts), q_start=start,
+                           max_kv_len=int(max(lens)), prefix_table=pre, prefix_len=prefix)
+        q, k, v = (torch.from_numpy(g.standard_normal((N + 9, h, D)) * 2.0 ** g.integers(-4, 5, (N + 9, 1, 1))).to(dtype) for h in (5, Hkv, Hkv))
+        out = torch.full_like(q, 7.0).cuda()
+        cl.kv_append(p.cache, batch, k.cuda(), v.cuda(), q=q.cuda(), rope=rope, q_norm=w.cuda() if norm else None,
+                     k_norm=w.cuda() if norm else None, q_out=out)
+        torch.cuda.synchronize()
+        wd, mine = (w.double().numpy() if norm else None), slice(ahead, ahead + N)
+        p.check(lens, counts, turned(k[mine].double().numpy(), lens, counts, freq.double().numpy(), inter, wd), v[mine].double().numpy())
+        ref = turned(q[mine].double().numpy(), lens, counts, freq.double().numpy(), inter, wd)
+        far = np.abs(ref).max(axis=-1, keepdims=True)
+        u = 2.0 ** (-11 if dtype == F16 else -8)
+        assert (np.abs(out[mine].double().cpu().numpy() - ref) <= u * np.abs(ref) * 1.01 + 2.0 ** -20 * far + 2.0 ** -25).all()
+        assert (out[:ahead] == 7).all() and (out[ahead + N:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["fp16", "bf16"])
+def test_append_without_rotation_or_queries(dtype):
+    """V's path for K too: codes equal the oracle's bit for bit, in prompts and in single tokens."""
+    g = torch.Generator().manual_seed(9)
+    for counts in ([600, 100], [1, 1]):
+        p = Pool([700, 300], 2, 128, 32, 32, dtype)
+        k, v = (torch.randn((sum(counts), 2, 128), generator=g).to(dtype) for _ in range(2))
+        assert cl.kv_append(p.cache, p.batch([690, 111], counts), k.cuda(), v.cuda()) is None
+        torch.cuda.synchronize()
+        p.check([690, 111], counts, k.double().numpy(), v.double().numpy(), rel=0.0)
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16], ids=["fp16", "bf16"])
 def test_append_ends_of_the_range(dtype):
     """Zeros, the type's largest and smallest values, infinities, NaN, and blocks that grow from one end to the other."""
@@ -395,6 +442,27 @@ def test_read_of_a_16_bit_cache():
                                           prefix_table=c.batch.prefix_table, prefix_len=10))
     k = k.double().cpu().numpy()
     assert (k[:5] == 0).all() and np.array_equal(k[5:31], c.ks[0][:, :26].transpose(1, 0, 2)) and np.isnan(k[31:45]).all()
+
+
+def test_a_stream_of_its_own_beside_a_busy_one():
+    """Calls on another stream take their workspaces and results there: memory that queued work still reads is not theirs."""
+    c = Case8([1, 2, 1], [5000, 3000, 4000], 8, 2, 128, 16, F16)
+    q = c.q.cuda()
+    want = cl.attention(c.cache, c.batch, q, out_dtype=F32)
+    kept = cl.kv_read(c.cache, c.batch)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    big = torch.ones((4096, 4096), device="cuda")
+    for _ in range(4):
+        x = torch.full((cl.attention_workspace(c.cache, c.batch, 8) // 4,), 3.0, device="cuda")
+        for _ in range(20):
+            big = (big @ big).clamp_(max=1.0)
+        keep = x * 2
+        del x
+        got = cl.attention(c.cache, c.batch, q, out_dtype=F32, stream=side)
+        read = cl.kv_read(c.cache, c.batch, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and bool((keep == 6.0).all()) and all(torch.equal(a, b) for a, b in zip(read, kept))
 
 
 def test_results_repeat_on_other_streams_and_in_graphs():

@@ -115,6 +115,45 @@ def test_calls_in_any_order(seed):
         w.check()
 
 
+@pytest.mark.parametrize("rows,width,room", [(17, 30, 1), (40, 300, 1), (12, 300, 2), (16, 256, 40), (5, 20, 200), (33, 64, 500), (64, 3, 0)])
+def test_forks_of_every_size(rows, width, room):
+    """One launch and two, a lane and a wave a row, at their borders; and back from many rows to few."""
+    g = random.Random(rows)
+    w = World(900, 8, rows, width, layers=1, seed=rows)
+    w.reserve([g.randint(0, min(8 * width, 90)) for _ in range(rows)])
+    w.set([min(8 * sum(p >= 0 for p in t), g.randint(0, 90)) for t in w.t])
+    for n in (rows, rows + 1, max(1, rows - 3), 2):
+        w.fork([g.randint(0, len(w.t) - 1) for _ in range(n)], room)
+        w.check()
+
+
+def test_a_stream_of_its_own_beside_a_busy_one():
+    """Forks and gathers on another stream take their workspaces and results there."""
+    w = World(300, 8, 20, 12, seed=2)
+    w.reserve([50 + i for i in range(20)])
+    w.set([50 + i for i in range(20)])
+    side = torch.cuda.Stream()
+    big = torch.ones((4096, 4096), device="cuda")
+    x = torch.arange(200, dtype=torch.int32, device="cuda").view(20, 10)
+    for i in range(4):
+        parents = [(3 * j + i) % 20 for j in range(20)]
+        dev = i32(parents)
+        torch.cuda.synchronize()
+        held = torch.full((cl.pages_workspace(w.pool, 20) // 4,), 3.0, device="cuda")
+        for _ in range(20):
+            big = (big @ big).clamp_(max=1.0)
+        keep = held * 2
+        del held
+        w.table, w.len = cl.kv_fork(w.pool, w.table, w.len, dev, room=1, stream=side)
+        rows, = cl.gather_rows([x], dev, stream=side)
+        torch.cuda.synchronize()
+        w.t, w.n, copies, m = pages.fork(w.refs, w.t, w.n, parents, w.size, 1)
+        w.copied(copies)
+        w.short += m
+        w.check()
+        assert torch.equal(rows, x[dev.long()]) and bool((keep == 6.0).all())
+
+
 def test_large_tables_and_pools():
     """More rows than the scanning workgroup has threads, more pages than a pass of its, more buffers than a launch takes."""
     g = random.Random(3)
