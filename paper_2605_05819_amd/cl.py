@@ -1223,6 +1223,15 @@ class Beams:
         return self._bytes
 
 
+def _values(t, name, dtype, n):
+    """The address of a contiguous tensor of n values."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.is_contiguous() and t.numel() == n:
+        return t.data_ptr()
+    _dev_tensor(t, name, (dtype,))
+    _need(t.numel() == n, "%s must have %d values" % (name, n))
+    return t.data_ptr()
+
+
 def beam_workspace(rule, groups, vocab):
     return _call("cl_beam_workspace")(rule._bytes, groups, vocab)
 
@@ -1232,37 +1241,42 @@ def beam_select(rule, logits, scores, lengths=None, finished=None, out=None, ws=
     scores float32 and lengths, finished int32 of groups * beams -> (scores
     float32, tokens, parents, lengths, finished int32), each [groups][picks]
     (lengths None without lengths).  out: such a tuple to be filled."""
-    _need(isinstance(logits, torch.Tensor) and logits.dtype in _OUT, "logits must be an fp16, bf16 or fp32 tensor")
-    _need(logits.dim() == 2 and logits.shape[0] > 0 and logits.shape[0] % max(1, rule.beams) == 0,
-          "logits must be [groups * beams][vocab]")
+    if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dtype in _OUT and logits.dim() == 2):
+        _need(isinstance(logits, torch.Tensor) and logits.dtype in _OUT, "logits must be an fp16, bf16 or fp32 tensor")
+        _need(logits.dim() == 2, "logits must be [groups * beams][vocab]")
+        _need(logits.shape[0] % max(1, rule.beams) == 0, "logits must be [groups * beams][vocab]")
+        _need(logits.stride(1) == 1 or logits.shape[1] == 1, "a row of logits must be contiguous")
+        _need(logits.is_cuda, "logits must be on the GPU (got %s)" % logits.device)
     rows, vocab = logits.shape
-    a, b = logits.stride()
-    _need((b == 1 or vocab == 1) and (a >= vocab or rows == 1), "a row of logits must be contiguous")
-    _need(logits.is_cuda, "logits must be on the GPU (got %s)" % logits.device)
-    groups = rows // rule.beams
-    for t, name, dt in ((scores, "scores", torch.float32), (lengths, "lengths", torch.int32),
-                        (finished, "finished", torch.int32)):
-        if t is not None or name == "scores":
-            _dev_tensor(t, name, (dt,))
-            _need(t.numel() == rows, "%s must have %d values" % (name, rows))
-    shape, dts = (groups, rule.picks), (torch.float32,) + (torch.int32,) * 4
+    _need(rows > 0 and rows % max(1, rule.beams) == 0, "logits must be [groups * beams][vocab]")
+    step = vocab
+    if not logits.is_contiguous():
+        a, b = logits.stride()
+        _need((b == 1 or vocab == 1) and (a >= vocab or rows == 1), "a row of logits must be contiguous")
+        step = a if rows > 1 else vocab
+    groups, picks = rows // rule.beams, rule.picks
+    f32, i32 = torch.float32, torch.int32
+    ins = (_values(scores, "scores", f32, rows), 0 if lengths is None else _values(lengths, "lengths", i32, rows),
+           0 if finished is None else _values(finished, "finished", i32, rows))
     if out is None:
-        s, *rest = _empty((5,) + shape, torch.int32, logits.device, stream).unbind(0)      # one allocation
-        out = [s.view(torch.float32), *rest]
-        if lengths is None:
-            out[3] = None
+        s, *rest = _empty((5, groups, picks), i32, logits.device, stream).unbind(0)      # one allocation
+        out = (s.view(f32), rest[0], rest[1], None if lengths is None else rest[2], rest[3])
+        at, each = s.data_ptr(), 4 * groups * picks
+        outs = (at, at + each, at + 2 * each, 0 if lengths is None else at + 3 * each, at + 4 * each)
     else:
         _need(len(out) == 5, "out must be (scores, tokens, parents, lengths, finished)")
-        for t, dt, name in zip(out, dts, ("scores", "tokens", "parents", "lengths", "finished")):
+        for t, name in zip(out, ("scores", "tokens", "parents", "lengths", "finished")):
             if t is not None or name in ("scores", "tokens", "parents"):
-                _dev_tensor(t, "out " + name, (dt,), shape)
+                _dev_tensor(t, "out " + name, (f32 if name == "scores" else i32,), (groups, picks))
+        outs = [_opt_ptr(t) for t in out]
     if ws is None:
         ws = _empty((max(beam_workspace(rule, groups, vocab), 1),), torch.uint8, logits.device, stream)
     else:
         _dev_tensor(ws, "ws", (torch.uint8,))
-    _check(_call("cl_beam_select")(rule._bytes, logits.data_ptr(), _DTYPE_CODE[logits.dtype], a if rows > 1 else vocab,
-                                   groups, vocab, scores.data_ptr(), _opt_ptr(lengths), _opt_ptr(finished),
-                                   *[_opt_ptr(t) for t in out], ws.data_ptr(), ws.numel(), _raw_stream(stream)))
+    st = _call("cl_beam_select")(rule._bytes, logits.data_ptr(), _DTYPE_CODE[logits.dtype], step, groups, vocab, *ins, *outs,
+                                 ws.data_ptr(), ws.numel(), _raw_stream(stream))
+    if st:
+        _check(st)
     return tuple(out)
 
 

@@ -1040,7 +1040,7 @@ cl_status cl_copy_pages(const cl_page_pool* pool, const int32_t* from, const int
     if (st) return st;
     if (n < 1) return fail(CL_EINVAL, "%s: n must be positive (got %d)", who, n);
     if (!from || !to || !aligned(from, 4) || !aligned(to, 4)) return fail(CL_EINVAL, "%s: null or misaligned from or to", who);
-    cl::CopyArgs a{};
+    cl::CopyRows a{};
     a.from = from;
     a.to = to;
     a.n = n;
@@ -1066,7 +1066,7 @@ cl_status cl_gather_rows(int32_t num_arrays, const cl_row_array* arrays, int32_t
             return fail(CL_EINVAL, "%s: array %d: src and dst overlap", who, i);
         b[i] = {static_cast<const char*>(x.src), static_cast<char*>(x.dst), x.row_bytes, 0};
     }
-    cl::CopyArgs a{};
+    cl::CopyRows a{};
     a.from = index;
     a.n = n;
     a.from_rows = src_rows;

@@ -372,7 +372,8 @@ __device__ __forceinline__ void copy_chunk(const char* from, char* to, int bytes
 // Row from[i] of every buffer's source to row to[i] of its destination (i where
 // there is no such array), i < n.  A workgroup takes turns of 16 KB; rows out of
 // range, and rows that go nowhere (-1), are passed over.
-__device__ __forceinline__ void copy_rows(const CopyArgs& a, unsigned block, unsigned blocks) {
+template <int N>
+__device__ __forceinline__ void copy_rows(const CopyList<N>& a, unsigned block, unsigned blocks) {
     const int n = a.count ? min(*a.count, a.n) : a.n;
     const long long turns = static_cast<long long>(n) * a.buffers * a.chunks;
     for (long long turn = block; turn < turns; turn += blocks) {
@@ -393,11 +394,15 @@ __device__ __forceinline__ void copy_rows(const CopyArgs& a, unsigned block, uns
     }
 }
 
-__global__ __launch_bounds__(256) void copy_rows_kernel(CopyArgs a) { copy_rows(a, blockIdx.x, gridDim.x); }
+template <int N>
+__global__ __launch_bounds__(256) void copy_rows_kernel(CopyList<N> a) {
+    copy_rows(a, blockIdx.x, gridDim.x);
+}
 
 // A compaction's moves and new names, which need nothing of each other: `renaming`
 // workgroups, the first ones, see to the tables.
-__global__ __launch_bounds__(256) void move_pages_kernel(CopyArgs c, CompactArgs a, unsigned renaming) {
+template <int N>
+__global__ __launch_bounds__(256) void move_pages_kernel(CopyList<N> c, CompactArgs a, unsigned renaming) {
     if (blockIdx.x < renaming) rename_pages(a, blockIdx.x, renaming);
     else copy_rows(c, blockIdx.x - renaming, gridDim.x - renaming);
 }
@@ -418,8 +423,9 @@ struct Room {
 
 // The buffers from number `first` on into a launch's arguments, as many as it takes;
 // its workgroups.
-static unsigned fill(CopyArgs& a, const CopyBuffer* buffers, int first, int n) {
-    a.buffers = n - first < kMaxCopyBuffers ? n - first : kMaxCopyBuffers;
+template <int N>
+static unsigned fill(CopyList<N>& a, const CopyBuffer* buffers, int first, int n) {
+    a.buffers = n - first < N ? n - first : N;
     long long most = 1;
     for (int b = 0; b < a.buffers; ++b) {
         a.buffer[b] = buffers[first + b];
@@ -434,14 +440,22 @@ static unsigned fill(CopyArgs& a, const CopyBuffer* buffers, int first, int n) {
     return static_cast<unsigned>(turns < 8192 ? turns : 8192);
 }
 
-hipError_t launch_copy_rows(CopyArgs a, const CopyBuffer* buffers, int n, hipStream_t st) {
-    for (int first = 0; first < n; first += kMaxCopyBuffers) {
+template <int N>
+static hipError_t copy_in_turn(const CopyRows& rows, const CopyBuffer* buffers, int n, hipStream_t st) {
+    CopyList<N> a;
+    static_cast<CopyRows&>(a) = rows;
+    for (int first = 0; first < n; first += N) {
         const unsigned grid = fill(a, buffers, first, n);
-        hipLaunchKernelGGL(copy_rows_kernel, dim3(grid), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(copy_rows_kernel<N>, dim3(grid), dim3(256), 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+
+hipError_t launch_copy_rows(const CopyRows& rows, const CopyBuffer* buffers, int n, hipStream_t st) {
+    return n <= kFewCopyBuffers ? copy_in_turn<kFewCopyBuffers>(rows, buffers, n, st)
+                                : copy_in_turn<kMaxCopyBuffers>(rows, buffers, n, st);
 }
 
 // Row lists and free pages of kv_fork and kv_reserve; lists of kv_compact.
@@ -484,7 +498,7 @@ hipError_t give(const Pool& pool, const PageTable& table, const int32_t* want, i
     else if (!little) hipLaunchKernelGGL(give_pages_kernel<64>, dim3(1), dim3(kScan), 0, st, g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || pool.num_buffers == 0) return e;
-    CopyArgs c{};
+    CopyRows c{};
     c.from = g.copy_from;
     c.to = g.copy_to;
     c.n = table.rows;
@@ -519,6 +533,18 @@ hipError_t launch_kv_free(const Pool& pool, const PageTable& table, const int32_
     return hipGetLastError();
 }
 
+template <int N>
+static hipError_t move(const Pool& pool, const CopyRows& rows, const CompactArgs& a, unsigned renaming, hipStream_t st) {
+    CopyList<N> c;
+    static_cast<CopyRows&>(c) = rows;
+    const unsigned grid = (pool.num_buffers ? fill(c, pool.buffers, 0, pool.num_buffers) : 0) + renaming;
+    if (grid == 0) return hipSuccess;
+    hipLaunchKernelGGL(move_pages_kernel<N>, dim3(grid), dim3(256), 0, st, c, a, renaming);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || pool.num_buffers <= N) return e;
+    return launch_copy_rows(rows, pool.buffers + N, pool.num_buffers - N, st);
+}
+
 hipError_t launch_kv_compact(const Pool& pool, int tables, int32_t* const* table, const int64_t* size, void* ws, hipStream_t st) {
     Room r{static_cast<char*>(ws)};
     CompactArgs a{};
@@ -538,21 +564,16 @@ hipError_t launch_kv_compact(const Pool& pool, int tables, int32_t* const* table
     hipLaunchKernelGGL(plan_moves_kernel, dim3(1), dim3(kScan), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    CopyArgs c{};
+    CopyRows c{};
     c.from = a.from;
     c.to = a.to;
     c.count = a.head;
     c.n = pool.num_pages;
     c.from_rows = c.to_rows = pool.num_pages;
-    unsigned grid = fill(c, pool.buffers, 0, pool.num_buffers);
-    if (pool.num_buffers == 0) grid = 0;
     const int64_t blocks = tables ? (most + 255) / 256 : 0;
     const unsigned renaming = static_cast<unsigned>(blocks < 1024 ? blocks : 1024);
-    if (grid + renaming == 0) return hipSuccess;
-    hipLaunchKernelGGL(move_pages_kernel, dim3(grid + renaming), dim3(256), 0, st, c, a, renaming);
-    e = hipGetLastError();
-    if (e != hipSuccess || pool.num_buffers <= kMaxCopyBuffers) return e;
-    return launch_copy_rows(c, pool.buffers + kMaxCopyBuffers, pool.num_buffers - kMaxCopyBuffers, st);
+    if (pool.num_buffers <= kFewCopyBuffers) return move<kFewCopyBuffers>(pool, c, a, renaming, st);
+    return move<kMaxCopyBuffers>(pool, c, a, renaming, st);
 }
 
 }  // namespace cl
