@@ -687,8 +687,8 @@ typedef struct cl_kv_cache8 {
  * cl_kv_append8 -- cl_kv_append into a cache of 8 bits.  The new rows of a block
  * are rounded to e4m3 (to nearest, ties to even) under 2^e, e the smallest with
  * max |x| <= 448 2^e over them, within -15..8 (CL_FP16) or -117..120 (CL_BF16), and
- * at least the exponent of the rows that stood in the block ahead of them; where
- * that is the smaller one, those rows are rescaled (exactly, but for codes that
+ * at least the block's so far where rows stand in it ahead of them (tokens that
+ * were taken back count on); where that is the smaller one, those rows are rescaled (exactly, but for codes that
  * come to stand below 2^-6, which are rounded again).  What stood behind the new
  * rows of a block counts as gone.  Computed in float32 and rounded once.  Magnitudes above
  * 1.875 2^15 (CL_FP16) or 1.875 2^127 are held as that; infinities and NaN as NaN,
@@ -734,9 +734,9 @@ cl_status cl_kv_read8(const cl_kv_cache8* cache, const cl_kv_batch* batch, void*
  *  buffers     host array: what moves with a page (k and v of every layer, the
  *              scales of a cache of 8 bits), page p at base + p page_bytes; NULL
  *              with num_buffers 0
- *  num_buffers 0..4096;  num_pages >= 1;  page_size as the caches'
- * Tables: device int32 [rows][width], entries outside 0..num_pages - 1 hold no
- * page (write -1; the calls do).  Row b holds kv_len[b] keys, prefix_len of them in
+ *  num_buffers 0..4096;  num_pages 1..2^30;  page_size as the caches'
+ * Tables: device int32 [rows][width] (up to 2^20 and 2^26), entries outside
+ * 0..num_pages - 1 hold no page (write -1; the calls do).  Row b holds kv_len[b] keys, prefix_len of them in
  * a shared prefix outside of the table, the others in its first entries;
  * pages behind those are held ahead of their keys.
  * All choices go by number (the lowest free page to the first entry in row
@@ -777,8 +777,8 @@ size_t cl_pages_workspace(const cl_page_pool* pool, int32_t rows);
  *  room                   0..2^30
  *  ws                     device workspace, 256-byte aligned
  * An entry that got no page is -1 (attention over it gives NaN, appends do not
- * store) and counted in pool->missing, as are keys past the width.
- * Errors: CL_EINVAL, CL_EWORKSPACE, CL_EHIP.
+ * store) and counted in pool->missing, as are entries past the width.
+ * Errors: CL_EINVAL, CL_EUNSUPPORTED, CL_EWORKSPACE, CL_EHIP (all five calls).
  */
 cl_status cl_kv_fork(const cl_page_pool* pool, const int32_t* table, const int32_t* kv_len, int32_t num_seqs,
                      int32_t width, int32_t prefix_len, const int32_t* parents, int32_t num_new, int32_t room,
@@ -800,7 +800,6 @@ cl_status cl_kv_reserve(const cl_page_pool* pool, int32_t* table, const int32_t*
  * cl_kv_free -- rows give all their pages back: entries -1, kv_len 0.
  *  rows  device int32 [num_rows] (others than 0..num_seqs - 1 are passed over; one
  *        named twice is freed once), or NULL: every row
- * Errors: CL_EINVAL, CL_EHIP.
  */
 cl_status cl_kv_free(const cl_page_pool* pool, int32_t* table, int32_t* kv_len, int32_t num_seqs, int32_t width,
                      const int32_t* rows, int32_t num_rows, void* stream);
@@ -812,7 +811,6 @@ cl_status cl_kv_free(const cl_page_pool* pool, int32_t* table, int32_t* kv_len, 
  *          holds pages of the pool (prefix tables too); sizes: host [num_tables],
  *          their entries
  *  ws      device workspace, 256-byte aligned
- * Errors: CL_EINVAL, CL_EWORKSPACE, CL_EHIP.
  */
 cl_status cl_kv_compact(const cl_page_pool* pool, int32_t num_tables, int32_t* const* tables, const int64_t* sizes,
                         void* ws, size_t ws_bytes, void* stream);
@@ -822,7 +820,6 @@ cl_status cl_kv_compact(const cl_page_pool* pool, int32_t num_tables, int32_t* c
  * stand in `to` twice, or in both lists; pairs outside the pool are passed over.
  * Counts and tables stay.
  *  from, to  device int32 [n]
- * Errors: CL_EINVAL, CL_EHIP.
  */
 cl_status cl_copy_pages(const cl_page_pool* pool, const int32_t* from, const int32_t* to, int32_t n, void* stream);
 

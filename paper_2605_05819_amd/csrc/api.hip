@@ -873,6 +873,8 @@ cl_status cl_residual_norm(const cl_norm* norm, const void* y, int32_t y_dtype, 
 namespace {
 
 constexpr int kMaxBuffers = 4096;
+// Page, row and entry numbers stay clear of 2^31 with a scan's step added.
+constexpr int kMaxPages = 1 << 30, kMaxTableRows = 1 << 20, kMaxTableWidth = 1 << 26;
 
 // The buffers of a pool, or none where memory for their list is out.
 struct Buffers {
@@ -891,6 +893,7 @@ cl_status check_pool(const cl_page_pool* p, cl::Pool* out, Buffers* buffers, con
     if (!p->refs || !aligned(p->refs, 4) || !aligned(p->missing, 4))
         return fail(CL_EINVAL, "%s: null refs, or refs or missing misaligned", who);
     if (p->num_pages < 1) return fail(CL_EINVAL, "%s: num_pages must be positive", who);
+    if (p->num_pages > kMaxPages) return fail(CL_EUNSUPPORTED, "%s: num_pages must be at most 2^30 (got %d)", who, p->num_pages);
     if (p->page_size < 1 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)))
         return fail(CL_EINVAL, "%s: page_size must be a power of two in 1..1024 (got %d)", who, p->page_size);
     if (p->num_buffers < 0 || p->num_buffers > kMaxBuffers || (p->num_buffers > 0 && !p->buffers))
@@ -914,7 +917,8 @@ cl_status check_pool(const cl_page_pool* p, cl::Pool* out, Buffers* buffers, con
 
 cl_status check_table(const void* table, const void* kv_len, int rows, int width, int prefix_len, const char* who) {
     if (rows < 1 || width < 1) return fail(CL_EINVAL, "%s: rows and width must be positive (got %d, %d)", who, rows, width);
-    if (rows > (1 << 20)) return fail(CL_EINVAL, "%s: at most 2^20 rows (got %d)", who, rows);
+    if (rows > kMaxTableRows || width > kMaxTableWidth)
+        return fail(CL_EUNSUPPORTED, "%s: at most 2^20 rows of 2^26 entries (got %d, %d)", who, rows, width);
     if (prefix_len < 0) return fail(CL_EINVAL, "%s: prefix_len must not be negative", who);
     if (!table || !kv_len || !aligned(table, 4) || !aligned(kv_len, 4))
         return fail(CL_EINVAL, "%s: null or misaligned table or kv_len", who);
@@ -958,7 +962,7 @@ cl_status check_beams(const cl_beams* r, int groups, int vocab, cl::BeamArgs* a,
 extern "C" {
 
 size_t cl_pages_workspace(const cl_page_pool* pool, int32_t rows) {
-    if (!pool || pool->num_pages < 1 || rows < 1 || rows > (1 << 20)) return 0;
+    if (!pool || pool->num_pages < 1 || pool->num_pages > kMaxPages || rows < 1 || rows > kMaxTableRows) return 0;
     return cl::pages_workspace_bytes(pool->num_pages, rows);
 }
 
@@ -1009,7 +1013,7 @@ cl_status cl_kv_free(const cl_page_pool* pool, int32_t* table, int32_t* kv_len, 
     if (!st) st = check_table(table, kv_len, num_seqs, width, 0, who);
     if (st) return st;
     if (!aligned(rows, 4)) return fail(CL_EINVAL, "%s: misaligned rows", who);
-    if (rows && (num_rows < 1 || num_rows > (1 << 20)))
+    if (rows && (num_rows < 1 || num_rows > kMaxTableRows))
         return fail(CL_EINVAL, "%s: num_rows must be in 1..2^20 (got %d)", who, num_rows);
     const cl::PageTable t{table, kv_len, num_seqs, width, 0, p.page_shift};
     return hip_status(cl::launch_kv_free(p, t, rows, num_rows, static_cast<hipStream_t>(stream)), who);

@@ -65,7 +65,8 @@ def test_pools(kw, needle):
 
 @pytest.mark.parametrize("kw,status,needle", [
     (dict(table=0), cl.CL_EINVAL, "table"), (dict(kv_len=FAKE + 2), cl.CL_EINVAL, "kv_len"), (dict(rows=0), cl.CL_EINVAL, "positive"),
-    (dict(width=0), cl.CL_EINVAL, "positive"), (dict(rows=(1 << 20) + 1), cl.CL_EINVAL, "2^20"),
+    (dict(width=0), cl.CL_EINVAL, "positive"), (dict(rows=(1 << 20) + 1), cl.CL_EUNSUPPORTED, "2^20"),
+    (dict(width=(1 << 26) + 1), cl.CL_EUNSUPPORTED, "2^26"),
     (dict(prefix=-1), cl.CL_EINVAL, "prefix_len"), (dict(ws=0), cl.CL_EWORKSPACE, "workspace"),
     (dict(bytes=100), cl.CL_EWORKSPACE, "workspace"), (dict(ws=FAKE + 16), cl.CL_EINVAL, "256-byte")])
 def test_fork_and_reserve(kw, status, needle):
@@ -96,9 +97,11 @@ def test_reserve_free_compact_copy():
 
 
 def test_workspaces_cover_their_lists():
-    for pages, rows in ((1, 1), (100, 5), (1 << 20, 1 << 20), (7, 100000), (0x7fffffff, 1)):
+    for pages, rows in ((1, 1), (100, 5), (1 << 20, 1 << 20), (7, 100000), (1 << 30, 1)):
         need = cl.lib().cl_pages_workspace(ctypes.byref(_pool(num_pages=pages)), rows)
         assert need >= 4 * (4 * rows + pages) and need >= 12 * pages
+    assert cl.lib().cl_pages_workspace(ctypes.byref(_pool(num_pages=(1 << 30) + 1)), 1) == 0
+    _refused(_compact(_pool(num_pages=(1 << 30) + 1)), cl.CL_EUNSUPPORTED, "2^30")
     assert cl.lib().cl_pages_workspace(None, 1) == 0 and cl.lib().cl_pages_workspace(ctypes.byref(_pool()), 0) == 0
 
 
