@@ -21,7 +21,7 @@
 // workgroups a CU, and by memory for the queries: 8593 tokens of 32 + 8 + 8 heads of
 // 128 with per-head norms, 194 MB, 52 us, 3.7 TB/s (130 registers and more leave three
 // workgroups a CU: 79 us); 64 single tokens 4.7 us.  Reading rows back: 8676 tokens' of 8 heads,
-// 53 MB, in 16.6 us.
+// 53 MB, in 15.8 us.
 
 #include <math.h>
 
@@ -441,49 +441,64 @@ bool wide(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 // ------------------------------------------------------------- reading back
 
-// A workgroup a token, 8 values a lane.
-template <bool CODES>
+// A workgroup for TOKENS neighbours, 8 values a lane: their chains (starts -> length
+// -> page -> values) run side by side.
+template <bool CODES, int TOKENS>
 __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a) {
-    const int t = static_cast<int>(a.first + blockIdx.x);
-    const int s = seq_of(a.batch, t);
-    if (s < 0) return;
-    const Seq q = load_seq(a.batch, s);
-    if (t >= q.start + q.count) return;
-    const int pos = q.keys - q.count + (t - q.start);
     const int P = a.batch.prefix_len, D = a.cache.dim, Hk = a.cache.heads;
-    int page = -1, row = 0;
-    if (pos >= 0) {
+    const long long t0 = static_cast<long long>(a.first + blockIdx.x) * TOKENS;
+    int first[TOKENS];                                 // pool row of head 0; -1: outside, -2: before position 0, -3: no token
+#pragma unroll
+    for (int n = 0; n < TOKENS; ++n) {
+        first[n] = -3;
+        if (t0 + n >= a.batch.tokens) continue;
+        const int t = static_cast<int>(t0 + n), s = seq_of(a.batch, t);
+        if (s < 0) continue;
+        const Seq q = load_seq(a.batch, s);
+        if (t >= q.start + q.count) continue;
+        const int pos = q.keys - q.count + (t - q.start);
+        first[n] = -2;
+        if (pos < 0) continue;
         const int32_t* table = pos < P ? a.batch.prefix_table : a.batch.page_table + static_cast<size_t>(s) * a.batch.table_width;
-        const int i = pos < P ? pos : pos - P;
-        page = table[i >> a.cache.page_shift];
-        row = i & ((1 << a.cache.page_shift) - 1);
+        const int i = pos < P ? pos : pos - P, page = table[i >> a.cache.page_shift];
+        first[n] = page >= 0 && page < a.cache.num_pages
+                       ? (page * Hk << a.cache.page_shift) + (i & ((1 << a.cache.page_shift) - 1)) : -1;
     }
-    const bool there = page >= 0 && page < a.cache.num_pages;
-    const uint32_t fill = pos < 0 ? 0u : 0xffffffffu;          // NaN in fp16 and bf16
     const int each = Hk * D / 8;
     for (int i = threadIdx.x; i < 2 * each; i += 256) {
         const bool is_v = i >= each;
         const int at = 8 * (is_v ? i - each : i), head = at / D;
-        u32x4 x = {fill, fill, fill, fill};
-        if (there) {
-            const int r = ((page * Hk + head) << a.cache.page_shift) + row;
+        u32x4 x[TOKENS];
+        u32x2 c[TOKENS];
+        uint32_t scale[TOKENS];
+#pragma unroll
+        for (int n = 0; n < TOKENS; ++n) {
+            const int r = max(first[n], 0) + (head << a.cache.page_shift);
             const size_t from = static_cast<size_t>(r) * D + at % D;
             if constexpr (CODES) {
-                const uint32_t b = (is_v ? a.cache.v_scale : a.cache.k_scale)[static_cast<unsigned>(r) >> a.cache.block_shift];
-                const float scale = __builtin_bit_cast(float, b << 23);
-                const u32x2 c = *reinterpret_cast<const u32x2*>(reinterpret_cast<const uint8_t*>(is_v ? a.cache.v : a.cache.k) + from);
-                const f32x2 v[4] = {__builtin_amdgcn_cvt_pk_f32_fp8(c[0], false), __builtin_amdgcn_cvt_pk_f32_fp8(c[0], true),
-                                    __builtin_amdgcn_cvt_pk_f32_fp8(c[1], false), __builtin_amdgcn_cvt_pk_f32_fp8(c[1], true)};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const Quad two{{v[j][0] * scale, v[j][1] * scale, 0.f, 0.f}};
-                    x[j] = narrow(two, a.cache.dtype).a;
-                }
+                c[n] = *reinterpret_cast<const u32x2*>(reinterpret_cast<const uint8_t*>(is_v ? a.cache.v : a.cache.k) + from);
+                scale[n] = (is_v ? a.cache.v_scale : a.cache.k_scale)[static_cast<unsigned>(r) >> a.cache.block_shift];
             } else {
-                x = *reinterpret_cast<const u32x4*>((is_v ? a.cache.v : a.cache.k) + from);
+                x[n] = *reinterpret_cast<const u32x4*>((is_v ? a.cache.v : a.cache.k) + from);
             }
         }
-        *reinterpret_cast<u32x4*>((is_v ? a.v : a.k) + static_cast<size_t>(t) * Hk * D + at) = x;
+#pragma unroll
+        for (int n = 0; n < TOKENS; ++n) {
+            if (first[n] == -3) continue;
+            if constexpr (CODES) {
+                const float f = __builtin_bit_cast(float, scale[n] << 23);
+                const f32x2 v[4] = {__builtin_amdgcn_cvt_pk_f32_fp8(c[n][0], false), __builtin_amdgcn_cvt_pk_f32_fp8(c[n][0], true),
+                                    __builtin_amdgcn_cvt_pk_f32_fp8(c[n][1], false), __builtin_amdgcn_cvt_pk_f32_fp8(c[n][1], true)};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    x[n][j] = a.cache.dtype == DT_BF16 ? narrow2<true>(v[j][0] * f, v[j][1] * f) : narrow2<false>(v[j][0] * f, v[j][1] * f);
+            }
+            if (first[n] < 0) {
+                const uint32_t fill = first[n] == -2 ? 0u : 0xffffffffu;         // NaN in fp16 and bf16
+                x[n] = u32x4{fill, fill, fill, fill};
+            }
+            *reinterpret_cast<u32x4*>((is_v ? a.v : a.k) + static_cast<size_t>(t0 + n) * Hk * D + at) = x[n];
+        }
     }
 }
 
@@ -497,10 +512,14 @@ hipError_t launch_kv_append8(const AppendArgs& a, hipStream_t st) {
 
 hipError_t launch_kv_read(const ReadArgs& args, bool codes, hipStream_t st) {
     ReadArgs a = args;
-    return launch_all(a.batch.tokens, [&](unsigned first, unsigned count) {
+    const bool many = a.batch.tokens >= 2048;          // four tokens a workgroup (8676 tokens 16.7 -> 15.8 us)
+    return launch_all((a.batch.tokens + (many ? 3ll : 0ll)) / (many ? 4 : 1), [&](unsigned first, unsigned count) {
         a.first = first;
-        if (codes) hipLaunchKernelGGL((kv_read_kernel<true>), dim3(count), dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((kv_read_kernel<false>), dim3(count), dim3(256), 0, st, a);
+        const dim3 grid(count), block(256);
+        if (codes && many) hipLaunchKernelGGL((kv_read_kernel<true, 4>), grid, block, 0, st, a);
+        else if (codes) hipLaunchKernelGGL((kv_read_kernel<true, 1>), grid, block, 0, st, a);
+        else if (many) hipLaunchKernelGGL((kv_read_kernel<false, 4>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((kv_read_kernel<false, 1>), grid, block, 0, st, a);
     });
 }
 

@@ -426,6 +426,43 @@ def test_rows_of_no_sequence_are_left_alone():
     assert torch.equal(q[1:6], x[1:6]) and ((v[1:6] - x[1:6]).abs() <= 2.0 ** -4 * x[1:6].abs() + 2.0 ** -9).all()
 
 
+@pytest.mark.parametrize("eight", [False, True], ids=["16bit", "8bit"])
+@pytest.mark.parametrize("D,Hkv", [(128, 3), (64, 1), (256, 2)])
+def test_read_of_whole_sequences(D, Hkv, eight):
+    """More rows than a call takes a workgroup each: sequences from their first key on, one asked for more rows than it has
+    keys, pages outside the pool, rows of no sequence on both sides."""
+    lens, page, ahead = [1500, 700, 30, 1], 16, 3
+    p = Pool(lens, Hkv, D, page, 8, BF16)
+    if eight:
+        cache, val = p.cache, [decoded(p.t[i], p.t[2 + i], 8, BF16) for i in (0, 1)]
+    else:
+        val = [torch.randn(p.t[0].shape).to(BF16) for _ in range(2)]
+        cache = cl.KvCache(*[v.cuda() for v in val])
+    p.table[1, 2] = len(p.t[0])
+    counts = [1500, 700, 35, 1]
+    start = torch.tensor(np.concatenate([[0], np.cumsum(counts)]) + ahead, dtype=torch.int32).cuda()
+    N = sum(counts) + 2 * ahead + 1
+    batch = cl.KvBatch(torch.tensor(lens, dtype=torch.int32).cuda(), p.table.cuda(), N, q_len=1500, q_start=start, max_kv_len=1500)
+    out = [torch.full((N, Hkv, D), 7.0, device="cuda").to(BF16) for _ in range(2)]
+    cl.kv_read(cache, batch, *out)
+    torch.cuda.synchronize()
+    for got, v in zip(out, val):
+        got = got.cpu()
+        assert (got[:ahead] == 7).all() and (got[N - ahead - 1:] == 7).all()
+        at = ahead
+        for b, (n, a) in enumerate(zip(lens, counts)):
+            for i in range(a):
+                j = n - a + i
+                row = got[at + i]
+                if j < 0:
+                    assert (row == 0).all()
+                elif b == 1 and j // page == 2:
+                    assert row.isnan().all()
+                else:
+                    assert torch.equal(row, v[int(p.table[b, j // page]), :, j % page])
+            at += a
+
+
 def test_read_of_a_16_bit_cache():
     c = Case([3, 2], [40, 30], 4, 2, 64, 16, BF16, prefix=10)
     k, v = cl.kv_read(c.cache, c.batch)
