@@ -40,6 +40,13 @@
 //    keys: 844 to 862 us, 1.0 PFLOP/s (one slower card: 932; a library product of
 //    8192^3 runs at 1.20 to 1.22).
 //
+// Codes (Q8) become values of the 16-bit type on their way to the operands: K in
+// registers where keys stream (a lane's 16 codes of a key are two MFMAs' operands,
+// the queries laid out to match), V and both in tiles ahead of LDS, one conversion a
+// pair with the block's power of two in it.  Streams read half the bytes: the four long
+// sequences 189 to 196 us, 5.0 TB/s; one of 2049 keys 9.4 us (16 bits: 10.0).  Tiles spend
+// 76 more instructions a wave and tile (347, of which 32 convert): 927 us.
+//
 // Rounding: probabilities enter the second product as the cache's type, to
 // nearest (off by 2^-8 of each at most in bf16, 2^-11 in fp16, and there by 2^-37
 // of the row's largest where that is more; see kLift), beside the output's own
@@ -327,6 +334,22 @@ __device__ __forceinline__ int swz(int row, int chunk) {
     return row * (D / 8) + (chunk ^ (row & kMask));
 }
 
+// Codes come 16 to a lane and go out as two chunks of 8 values.  Neighbouring lanes
+// of a row would write every second chunk and meet on half the banks, so lanes in
+// fours change between two rows, whose swizzles differ in the lowest bit (conflicts
+// of the ragged prompts 1.06e8 -> 5.3e7, those of the reads; their time is bound
+// elsewhere): which of every 64 / (D / 16) rows a lane has, and its piece of the row.
+template <int D>
+__device__ __forceinline__ int code_row(int lane) {
+    constexpr int QC = D / 16;
+    return 2 * (lane / (2 * QC)) + (lane >> 2 & 1);
+}
+template <int D>
+__device__ __forceinline__ int code_piece(int lane) {
+    constexpr int QC = D / 16;
+    return 4 * (lane % (2 * QC) >> 3) + (lane & 3);
+}
+
 // Operand of V^T: 16 dims (block d) x 32 keys (rows 32 kk ..) of a tile in LDS.
 template <int D>
 __device__ __forceinline__ u32x4 load_vt(const uint16_t* v, int kk, int d) {
@@ -536,10 +559,9 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
             }
 #pragma unroll
             for (int i = 0; i < VR; ++i) {
-                const int c = lane + 64 * i;
-                const int r = __shfl(where, c / VC, 64);
+                const int r = __shfl(where, code_row<D>(lane) + 64 / VC * i, 64);
                 vr[i] = kZeros;
-                if (r >= 0) vr[i] = *reinterpret_cast<const u32x4*>(v8 + static_cast<size_t>(r) * D + 16 * (c % VC));
+                if (r >= 0) vr[i] = *reinterpret_cast<const u32x4*>(v8 + static_cast<size_t>(r) * D + 16 * code_piece<D>(lane));
             }
             return;
         }
@@ -589,10 +611,10 @@ __device__ __forceinline__ void attn_stream(const AttnArgs& a, const Plan& pl, i
                 }
 #pragma unroll
                 for (int i = 0; i < VR; ++i) {
-                    const int c = lane + 64 * i;
-                    const float sv = scale_of(__shfl(vs, c / VC, 64));
-                    *reinterpret_cast<u32x4*>(vl + 8 * swz<D>(c / VC, 2 * (c % VC))) = decode8<BF>(vr[i][0], vr[i][1], sv);
-                    *reinterpret_cast<u32x4*>(vl + 8 * swz<D>(c / VC, 2 * (c % VC) + 1)) = decode8<BF>(vr[i][2], vr[i][3], sv);
+                    const int r = code_row<D>(lane) + 64 / VC * i, c = 2 * code_piece<D>(lane);
+                    const float sv = scale_of(__shfl(vs, r, 64));
+                    *reinterpret_cast<u32x4*>(vl + 8 * swz<D>(r, c)) = decode8<BF>(vr[i][0], vr[i][1], sv);
+                    *reinterpret_cast<u32x4*>(vl + 8 * swz<D>(r, c + 1)) = decode8<BF>(vr[i][2], vr[i][3], sv);
                 }
             } else {
 #pragma unroll
@@ -893,19 +915,19 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
             const uint8_t* const src = codes + static_cast<size_t>(first) * D;
 #pragma unroll
             for (int i = 0; i < CQ; ++i) {
-                const int c = 64 * i + lane;
-                to.c[i] = *reinterpret_cast<const u32x4*>(src + 16 * c);
-                to.scale[i] = scale_byte(scales, a, first + c / QC);
+                const int r = code_row<D>(lane) + 64 / QC * i;
+                to.c[i] = *reinterpret_cast<const u32x4*>(src + r * D + 16 * code_piece<D>(lane));
+                to.scale[i] = scale_byte(scales, a, first + r);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < CQ; ++i) {
-                const int c = 64 * i + lane, key = at + WR * wave + c / QC;
+                const int key = at + WR * wave + code_row<D>(lane) + 64 / QC * i;
                 const int r = key < seg.keys ? pool_row(a, seg, head, key) : -2;
                 to.c[i] = r == -1 ? kNaNs : kZeros;
                 to.scale[i] = 0;
                 if (r >= 0) {
-                    to.c[i] = *reinterpret_cast<const u32x4*>(codes + static_cast<size_t>(r) * D + 16 * (c % QC));
+                    to.c[i] = *reinterpret_cast<const u32x4*>(codes + static_cast<size_t>(r) * D + 16 * code_piece<D>(lane));
                     to.scale[i] = scale_byte(scales, a, r);
                 }
             }
@@ -914,10 +936,10 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
     const auto put = [&](const Codes& from8, uint32_t to) {
 #pragma unroll
         for (int i = 0; i < CQ; ++i) {
-            const int c = 64 * i + lane, r = WR * wave + c / QC;
+            const int r = WR * wave + code_row<D>(lane) + 64 / QC * i, c = 2 * code_piece<D>(lane);
             const float sc8 = scale_of(from8.scale[i]);
-            *(lds_u32x4*)(uintptr_t)(to + 16 * swz<D>(r, 2 * (c % QC))) = decode8<BF>(from8.c[i][0], from8.c[i][1], sc8);
-            *(lds_u32x4*)(uintptr_t)(to + 16 * swz<D>(r, 2 * (c % QC) + 1)) = decode8<BF>(from8.c[i][2], from8.c[i][3], sc8);
+            *(lds_u32x4*)(uintptr_t)(to + 16 * swz<D>(r, c)) = decode8<BF>(from8.c[i][0], from8.c[i][1], sc8);
+            *(lds_u32x4*)(uintptr_t)(to + 16 * swz<D>(r, c + 1)) = decode8<BF>(from8.c[i][2], from8.c[i][3], sc8);
         }
     };
 
