@@ -31,6 +31,9 @@ linear  -- the compensated forward (decode and prefill compute the same thing)
 moe     -- expert-gathered compensated forward
 ranks   -- rank allocation from the residual spectra (Section 4.3, Appendix B.1)
 layer   -- between the linears of a layer: attention, rotary positions, routing, norms
+cache8  -- e4m3 codes and the blocks of an 8-bit cache
+pages   -- pages of a cache and their holders
+beam    -- one step of a beam search
 """
 
-from . import quant, comp, layer, linear, moe, ranks  # noqa: F401
+from . import beam, cache8, comp, layer, linear, moe, pages, quant, ranks  # noqa: F401
