@@ -710,6 +710,9 @@ cl_status cl_kv_append8(const cl_kv_cache8* cache, const cl_kv_batch* batch, con
 cl_status cl_attention8(const cl_kv_cache8* cache, const cl_kv_batch* batch, const void* q, int64_t q_stride,
                         int32_t q_heads, float scale, int32_t causal, int32_t window, void* out, int32_t out_dtype,
                         float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes for cl_attention8, as cl_attention_workspace; for prompts of
+ * many tokens with room for their keys and values in 16 bits, up to 2 GiB. */
 size_t cl_attention8_workspace(const cl_kv_cache8* cache, const cl_kv_batch* batch, int32_t q_heads);
 
 /*

@@ -622,7 +622,8 @@ cl_status attention_checked(cl::AttnArgs& a, bool codes, const void* q, int64_t 
     if (window < 0) return fail(CL_EINVAL, "%s: window must not be negative", who);
     if (!out_type(out_dtype)) return fail(CL_EINVAL, "%s: out_dtype must be CL_FP16, CL_BF16 or CL_FP32", who);
     if (lse && !aligned(lse, 4)) return fail(CL_EINVAL, "%s: misaligned lse", who);
-    const size_t need = cl::attention_workspace_bytes(a.cache, a.batch, q_heads);
+    const size_t need = codes ? cl::attention8_workspace_bytes(a.cache, a.batch, q_heads)
+                              : cl::attention_workspace_bytes(a.cache, a.batch, q_heads);
     if (need > 0) {
         if (!ws || ws_bytes < need)
             return fail(CL_EWORKSPACE, "%s: workspace of %zu bytes needed (got %zu)", who, need, ws ? ws_bytes : 0);
@@ -642,9 +643,9 @@ cl_status attention_checked(cl::AttnArgs& a, bool codes, const void* q, int64_t 
 }
 
 // Of checked descriptors; 0 for rejected ones.
-size_t attention_bytes(cl_status st, const cl::KvCache& c, const cl::KvBatch& b, int q_heads) {
+size_t attention_bytes(cl_status st, bool codes, const cl::KvCache& c, const cl::KvBatch& b, int q_heads) {
     if (st != CL_OK || q_heads < c.heads || q_heads % c.heads || !cl::attention_size_ok(c, b, q_heads)) return 0;
-    return cl::attention_workspace_bytes(c, b, q_heads);
+    return codes ? cl::attention8_workspace_bytes(c, b, q_heads) : cl::attention_workspace_bytes(c, b, q_heads);
 }
 
 cl_status read_checked(const cl::ReadArgs& a, bool codes, const void* k, const void* v, void* stream, const char* who) {
@@ -701,7 +702,7 @@ size_t cl_attention_workspace(const cl_kv_cache* cache, const cl_kv_batch* batch
     memcpy(saved, g_err, sizeof(g_err));
     cl::KvCache c;
     cl::KvBatch b;
-    const size_t bytes = attention_bytes(check_kv(cache, batch, &c, &b, ""), c, b, q_heads);
+    const size_t bytes = attention_bytes(check_kv(cache, batch, &c, &b, ""), false, c, b, q_heads);
     memcpy(g_err, saved, sizeof(g_err));
     return bytes;
 }
@@ -722,7 +723,7 @@ size_t cl_attention8_workspace(const cl_kv_cache8* cache, const cl_kv_batch* bat
     memcpy(saved, g_err, sizeof(g_err));
     cl::KvCache c;
     cl::KvBatch b;
-    const size_t bytes = attention_bytes(check_kv8(cache, batch, &c, &b, ""), c, b, q_heads);
+    const size_t bytes = attention_bytes(check_kv8(cache, batch, &c, &b, ""), true, c, b, q_heads);
     memcpy(g_err, saved, sizeof(g_err));
     return bytes;
 }

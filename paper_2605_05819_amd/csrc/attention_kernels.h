@@ -43,7 +43,8 @@
 // Codes (Q8) become values of the 16-bit type on their way to the operands: K in
 // registers where keys stream (a lane's 16 codes of a key are two MFMAs' operands,
 // the queries laid out to match), V and both in tiles ahead of LDS, one conversion a
-// pair with the block's power of two in it.  Streams read half the bytes: the four long
+// pair with the block's power of two in it (long prompts convert ahead of all, see
+// attention8.hip).  Streams read half the bytes: the four long
 // sequences 189 to 196 us, 5.0 TB/s; one of 2049 keys 9.4 us (16 bits: 10.0).  Tiles spend
 // 76 more instructions a wave and tile (347, of which 32 convert): 927 us.
 //

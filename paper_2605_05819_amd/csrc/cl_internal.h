@@ -146,11 +146,13 @@ struct AttnArgs {
     float scale;
     void* out;
     float* lse;                    // may be null
+    unsigned first;                // a conversion's first workgroup of a launch
 };
 bool attention_dim_ok(int dim);
 bool attention_size_ok(const KvCache& c, const KvBatch& b, int q_heads);   // every number of the launch fits
 size_t attention_workspace_bytes(const KvCache& c, const KvBatch& b, int q_heads);
 hipError_t launch_attention(const AttnArgs& a, void* ws, hipStream_t st);
+size_t attention8_workspace_bytes(const KvCache& c, const KvBatch& b, int q_heads);
 hipError_t launch_attention8(const AttnArgs& a, void* ws, hipStream_t st);      // of a cache of 8 bits
 
 // Residual add, gate, combination of slots and norms of one row (norm.hip).

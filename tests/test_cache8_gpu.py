@@ -94,6 +94,52 @@ def test_attention_blocks_and_scales(block):
     check(c, scale=0.0)
 
 
+LONG = [                                          # prompts whose keys are converted ahead: 16 row blocks and more, 256 in all
+    ([600, 17, 300, 1], [600, 400, 333, 9], 16, 4, 128, 16, 8),
+    ([530, 3, 0, 520], [900, 3, 20, 520], 16, 4, 64, 64, 64),
+    ([300, 290, 1, 40], [300, 512, 70, 41], 16, 4, 256, 32, 1),
+    ([700, 650], [1300, 650], 24, 8, 128, 256, 32),
+    ([129, 128, 1, 1], [129, 200, 1, 0], 64, 4, 64, 1, 1),
+]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["fp16", "bf16"])
+@pytest.mark.parametrize("shape", range(len(LONG)))
+def test_long_prompts(shape, dtype):
+    q, kv, Hq, Hkv, D, page, block = LONG[shape]
+    c = Case8(q, kv, Hq, Hkv, D, page, dtype, block=block, seed=shape)
+    assert cl.attention_workspace(c.cache, c.batch, Hq) >= sum(kv) * 4 * Hkv * D
+    check(c)
+    check(c, causal=False, window=(0, 70, 1, 130, 33)[shape], out_dtype=F32)
+
+
+@pytest.mark.parametrize("shape", [0, 2])
+def test_long_prompts_with_nan_codes_and_bad_pages(shape):
+    q, kv, Hq, Hkv, D, page, block = LONG[shape]
+    c = Case8(q, kv, Hq, Hkv, D, page, BF16, block=block, seed=shape)
+    for window in (0, 40):
+        c = Case8(q, kv, Hq, Hkv, D, page, BF16, block=block, seed=shape)
+        x = c.q.cuda()
+        ws = torch.full((cl.attention_workspace(c.cache, c.batch, Hq),), 255, dtype=torch.uint8, device="cuda")
+        clean = cl.attention(c.cache, c.batch, x, window=window, out_dtype=F32, ws=ws)
+        g, j = Hq // Hkv, kv[0] - 150                  # a value of the second key head in the middle of the first prompt
+        c.cache.v[c.table[0, j // page].long(), 1, j % page, 5] = 0x7f
+        out = cl.attention(c.cache, c.batch, x, window=window, out_dtype=F32, ws=ws.fill_(255))
+        torch.cuda.synchronize()
+        pos = torch.arange(kv[0] - q[0], kv[0], device="cuda")
+        sees = (pos >= j) & ((pos < j + window) if window else True)
+        touched = torch.zeros_like(out, dtype=torch.bool)
+        touched[:q[0], g:2 * g, 5] = sees[:, None]
+        assert out[touched].isnan().all() and touched.any()
+        assert torch.allclose(out[~touched], clean[~touched], rtol=2.0 ** -20, atol=2.0 ** -20)
+    c = Case8(q, kv, Hq, Hkv, D, page, BF16, block=block, seed=shape)
+    for bad in (-1, c.cache.num_pages, 1 << 30):
+        c.table[0, 3] = bad
+        out = cl.attention(c.cache, c.batch, x, out_dtype=F32, causal=False)
+        torch.cuda.synchronize()
+        assert out[:q[0]].isnan().all() and out[q[0]:].isfinite().all()
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16], ids=["fp16", "bf16"])
 def test_every_code_and_exponent_decodes_exactly(dtype):
     """One key a query sees: the output is its value, for every code and the type's exponents."""
