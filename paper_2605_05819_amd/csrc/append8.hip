@@ -94,12 +94,14 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t c, float f) {
 }
 
 // Sine and cosine of pair j at a position, times the magnitude; the angle as
-// append.hip forms it.
+// append.hip forms it, and what its rounding to fp32 leaves out to first order.
 __device__ __forceinline__ float2 turn_of(const AppendArgs& a, int pos, int j) {
     const double turns = static_cast<double>(pos) * static_cast<double>(a.rope.inv_freq[j]) * 0.15915494309189533577;  // 1 / (2 pi)
+    const double part = turns - rint(turns);
+    const float near = static_cast<float>(part), rest = static_cast<float>(part - near) * 6.28318531f;
     float sn, cs;
-    sincospif(2.0f * static_cast<float>(turns - rint(turns)), &sn, &cs);
-    return float2{cs * a.rope.magnitude, sn * a.rope.magnitude};
+    sincospif(2.0f * near, &sn, &cs);
+    return float2{fmaf(-sn, rest, cs) * a.rope.magnitude, fmaf(cs, rest, sn) * a.rope.magnitude};
 }
 
 // A lane's four pairs turned: (u_i, v_i) in halves, or neighbours in u, then v.
@@ -187,7 +189,7 @@ __device__ __forceinline__ void queries(const AppendArgs& a, float2* turns, int 
             load8<VEC>(a.q_norm, lo, hi, half, rx, ry);
             const Quad wx = widen<BF>(rx), wy = widen<BF>(ry);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) u.v[i] *= r * wx.v[i], v.v[i] *= r * wy.v[i];
+            for (int i = 0; i < 4; ++i) u.v[i] = u.v[i] * wx.v[i] * r, v.v[i] = v.v[i] * wy.v[i] * r;
         }
         if (rotary) turn(u, v, sc, half);
         store8<VEC, (HP > 1)>(a.q_out + (static_cast<size_t>(t) * a.q_heads + h) * D, lo, hi, half, narrow<BF>(u), narrow<BF>(v));
@@ -195,6 +197,11 @@ __device__ __forceinline__ void queries(const AppendArgs& a, float2* turns, int 
 }
 
 // New rows of one head (of K or V, a wave's) into one block.
+// The norm and the turn are in fp32: the few values that stand within its errors,
+// 1e-7, of a code step's border get the neighbour's code (8 to 15 of 9 M values of
+// 8676 tokens of 8 heads; 15 to 18 before the angle kept its rest and the product
+// with the weight became exact).  A Newton step on the inverse root changed none of
+// it, K's part in fp64 took 97 us where this takes 65.
 // R > 0: the wave holds the rows, 64 / LG an iteration and R of them at most, as
 // they came, from one batch of loads.  R = 0: any number, loaded for each pass.
 template <int LG, bool VEC, bool BF, int R>
@@ -242,7 +249,7 @@ __device__ __forceinline__ void block_rows(const AppendArgs& a, const float2* tu
         if (w) {
             const float r = inverse_rms<LG>(u, v, D, a.eps);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) u.v[j] *= r * wx.v[j], v.v[j] *= r * wy.v[j];
+            for (int j = 0; j < 4; ++j) u.v[j] = u.v[j] * wx.v[j] * r, v.v[j] = v.v[j] * wy.v[j] * r;      // the first product is exact
         }
         if (turned) {
             float2 sc[4];
