@@ -26,7 +26,7 @@ def select(logits, scores, beams, picks, lengths=None, finished=None, eos=-1, al
             else:
                 with np.errstate(invalid="ignore", divide="ignore"):
                     m = x.max()
-                    s = s0 + (x - (m + np.log(np.exp(x - m).sum())))
+                    s = s0 + ((x - m) - np.log(np.exp(x - m).sum()))
                 if np.isnan(x).any() or (x == np.inf).any() or not s0 < np.inf:
                     s = np.full(V, np.nan)
                 elif s0 == -np.inf or m == -np.inf:

@@ -177,9 +177,15 @@ __global__ __launch_bounds__(256, 8) void beam_scan_kernel(BeamArgs a) {
     // 2^(x log2 e - zero): what rounding adds is different for each value, as long as
     // the reference is `zero` itself and not the maximum that it was rounded from
     const float zero = top == -INFINITY ? 0.f : top * kLog2e;
+    const bool far = fabsf(top) >= 16777216.0f && fabsf(top) <= 3.4028234663852886e38f;
     float s = 0.f;
+    if (!far) {
 #pragma unroll
-    for (int j = 0; j < EPT; ++j) s += __builtin_amdgcn_exp2f(fmaf(x[j], kLog2e, -zero));
+        for (int j = 0; j < EPT; ++j) s += __builtin_amdgcn_exp2f(fmaf(x[j], kLog2e, -zero));
+    } else {                                       // masks of a type's lowest value: `zero` is too far from top, x - top is exact
+#pragma unroll
+        for (int j = 0; j < EPT; ++j) s += __builtin_amdgcn_exp2f((x[j] - top) * kLog2e);
+    }
     sums[tid] = s;
 
 #pragma unroll
@@ -199,7 +205,7 @@ __global__ __launch_bounds__(256, 8) void beam_scan_kernel(BeamArgs a) {
         const double total = wave_sum(static_cast<double>(sums[lane]) + sums[lane + 64] + sums[lane + 128] + sums[lane + 192]);
         if (lane == 0) {
             a.sum[slot] = total;
-            a.most[slot] = zero;
+            a.most[slot] = top == -INFINITY || far ? static_cast<double>(top) : static_cast<double>(zero) / static_cast<double>(kLog2e);
         }
     }
     const int n = filled;
@@ -268,18 +274,17 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a, int waves)
             const double by = a.alpha != 0.0 && len > 1 ? exp(a.alpha * log(static_cast<double>(len))) : 1.0;
             const double before = static_cast<double>(a.scores[row]);
             // all candidates of one score: a finished beam's -inf, a beam of -inf, NaN
-            double same = -INFINITY, lse = 0.0;
+            double same = -INFINITY, top = 0.0, lse = 0.0;      // lse: beyond top
             bool plain = done;
             if (!done) {
                 const size_t at = static_cast<size_t>(row) * a.splits + lane;
-                const float m = lane < a.splits ? a.most[at] : -INFINITY;      // in units of log2 e, as the kernel above has it
+                const double m = lane < a.splits ? a.most[at] : -INFINITY;
                 const double s = lane < a.splits ? a.sum[at] : 0.0;
-                float top = m;
+                top = m;
 #pragma unroll
-                for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-                const double unit = 1.0 / static_cast<double>(kLog2e);
-                const double sum = wave_sum(s == 0.0 ? 0.0 : s * exp((static_cast<double>(m) - static_cast<double>(top)) * unit));
-                lse = static_cast<double>(top) * unit + log(sum);
+                for (int off = 32; off > 0; off >>= 1) top = fmax(top, __shfl_xor(top, off, 64));
+                const double sum = wave_sum(s == 0.0 ? 0.0 : s * exp(m - top));
+                lse = log(sum);
                 if (sum == 0.0) plain = true;                          // no logit above -inf
                 if (!(fabs(sum) <= 1.7976931348623157e308) || !(before <= 3.4028234663852886e38)) plain = true, same = NAN;
                 else if (before == -INFINITY) plain = true;
@@ -308,7 +313,7 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a, int waves)
                 if (head == c && c != 0) {
                     ++next;
                     head = next < a.picks ? mine[lane * a.picks + next] : 0;
-                    const double s = before + (static_cast<double>(from_key(static_cast<uint32_t>(c >> 32))) - lse);
+                    const double s = before + ((static_cast<double>(from_key(static_cast<uint32_t>(c >> 32))) - top) - lse);
                     rank[b * a.picks + j] = rank_key(s / by);
                     score[b * a.picks + j] = static_cast<float>(s);
                     token[b * a.picks + j] = static_cast<int>(~static_cast<uint32_t>(c));
@@ -377,7 +382,7 @@ bool beam_fits(const BeamArgs& args) {
 size_t beam_workspace_bytes(BeamArgs a) {
     cut(a);
     const size_t slots = static_cast<size_t>(a.groups) * a.beams * a.splits;
-    return up256(slots * a.picks * 8) + up256(slots * 8) + up256(slots * 4);
+    return up256(slots * a.picks * 8) + 2 * up256(slots * 8);
 }
 
 hipError_t launch_beam_select(BeamArgs a, void* ws, hipStream_t st) {
@@ -387,7 +392,7 @@ hipError_t launch_beam_select(BeamArgs a, void* ws, hipStream_t st) {
     a.best = reinterpret_cast<u64*>(at);
     at += up256(slots * a.picks * 8);
     a.sum = reinterpret_cast<double*>(at);
-    a.most = reinterpret_cast<float*>(at + up256(slots * 8));
+    a.most = reinterpret_cast<double*>(at + up256(slots * 8));
     if (a.dtype == DT_FP32) scan<DT_FP32>(a, st);
     else if (a.dtype == DT_BF16) scan<DT_BF16>(a, st);
     else scan<DT_FP16>(a, st);

@@ -33,7 +33,8 @@ def check(x, scores, beams, picks=None, lengths=None, finished=None, eos=-1, alp
     sure = gap > 2.0 ** -20 * scale
     assert (~sure).sum() <= most_left_out, gap.min()
     s = got[0].double().cpu().numpy()
-    same = (s == want[0]) | (np.isnan(s) & np.isnan(want[0]))
+    with np.errstate(over="ignore"):                 # a score past fp32's range (lowest less highest logit) is -inf
+        same = (s == want[0].astype(np.float32)) | (np.isnan(s) & np.isnan(want[0]))
     with np.errstate(invalid="ignore"):
         near = np.abs(s - want[0]) <= 2.0 ** -24 * np.abs(want[0]) * 1.01 + 2.0 ** -20
     assert (same | near)[sure].all()
@@ -86,6 +87,29 @@ def test_masked_vocabularies(V):
         x[r, at] = torch.randn(n, generator=g)
     check(x, [-1.0, -2.0, -0.5, -0.1, -3.0, -1.5, -2.5, -9.0], 4, 12)
     check(x, [-1.0, -2.0, -0.5, -0.1, -3.0, -1.5, -2.5, -9.0], 2, 5, lengths=[4, 5, 6, 7, 8, 9, 1, 2], alpha=1.0)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32], ids=["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("V", [100, 9000, 70000])
+def test_masks_of_the_lowest_value(V, dtype):
+    """Masks of the type's lowest value over all or nearly all of a row, of whole chunks beside others, its largest
+    value; and chunks of -inf beside logits far below zero, whose exponentials only their own maximum keeps."""
+    g = torch.Generator().manual_seed(7)
+    low, high = torch.finfo(dtype).min, torch.finfo(dtype).max
+    x = torch.randn((8, V), generator=g).to(dtype)
+    x[0] = low
+    x[1, 3:] = low
+    x[2, :V // 2] = low
+    x[3, V // 2:] = low
+    x[4], x[4, V // 3] = low, high / 2
+    x[5, V - 4:] = high
+    x[6, V // 2:] = -float("inf")
+    x[6, :V // 2] -= 20000 if dtype == F16 else 3.0e5
+    x[7] = high
+    scores = [-1.0, -2.0, -0.5, -0.25, -3.0, -1.5, -2.5, -6.0]
+    check(x, scores, 1, 3)
+    check(x[:4].contiguous(), scores[:4], 4, 6)
+    check(x[6:].contiguous(), scores[6:], 2, 6)
 
 
 def test_first_step_and_dead_beams():
