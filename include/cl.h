@@ -738,7 +738,7 @@ cl_status cl_kv_read8(const cl_kv_cache8* cache, const cl_kv_batch* batch, void*
  *              scales of a cache of 8 bits), page p at base + p page_bytes; NULL
  *              with num_buffers 0
  *  num_buffers 0..4096;  num_pages 1..2^30;  page_size as the caches'
- * Tables: device int32 [rows][width] (up to 2^20 and 2^26), entries outside
+ * Tables: device int32 [rows][width] (up to 2^20 and 2^26, 2^31 - 1 entries in all), entries outside
  * 0..num_pages - 1 hold no page (write -1; the calls do).  Row b holds kv_len[b] keys, prefix_len of them in
  * a shared prefix outside of the table, the others in its first entries;
  * pages behind those are held ahead of their keys.
@@ -780,7 +780,8 @@ size_t cl_pages_workspace(const cl_page_pool* pool, int32_t rows);
  *  room                   0..2^30
  *  ws                     device workspace, 256-byte aligned
  * An entry that got no page is -1 (attention over it gives NaN, appends do not
- * store) and counted in pool->missing, as are entries past the width.
+ * store) and counted in pool->missing, as are entries past the width (1024 of a row
+ * at most).
  * Errors: CL_EINVAL, CL_EUNSUPPORTED, CL_EWORKSPACE, CL_EHIP (all five calls).
  */
 cl_status cl_kv_fork(const cl_page_pool* pool, const int32_t* table, const int32_t* kv_len, int32_t num_seqs,

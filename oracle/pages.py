@@ -48,7 +48,7 @@ def _give(refs, table, kv_len, want, keep, size, prefix):
         if want[i] <= kv_len[i]:
             continue
         need = max(-(-max(want[i] - prefix, 0) // size), used)
-        missing += max(need - width, 0)
+        missing += min(max(need - width, 0), 1024)
         if own % size and _held(row[used - 1], refs) and not (keep[i] > 0 and refs[row[used - 1]] == keep[i]):
             asks.append((i, used - 1, row[used - 1]))
         asks += [(i, e, None) for e in range(used, min(need, width)) if not _held(row[e], refs)]

@@ -920,6 +920,8 @@ cl_status check_table(const void* table, const void* kv_len, int rows, int width
     if (rows < 1 || width < 1) return fail(CL_EINVAL, "%s: rows and width must be positive (got %d, %d)", who, rows, width);
     if (rows > kMaxTableRows || width > kMaxTableWidth)
         return fail(CL_EUNSUPPORTED, "%s: at most 2^20 rows of 2^26 entries (got %d, %d)", who, rows, width);
+    if (static_cast<long long>(rows) * width > 0x7fffffffll)
+        return fail(CL_EUNSUPPORTED, "%s: at most 2^31 - 1 entries (got %d rows of %d)", who, rows, width);
     if (prefix_len < 0) return fail(CL_EINVAL, "%s: prefix_len must not be negative", who);
     if (!table || !kv_len || !aligned(table, 4) || !aligned(kv_len, 4))
         return fail(CL_EINVAL, "%s: null or misaligned table or kv_len", who);

@@ -154,7 +154,7 @@ __device__ __forceinline__ void give_pages(const GiveArgs& a) {
     // the lanes of a row that hold true, as bits from the row's first lane
     const auto votes = [&](bool v) { return LANES == 64 ? static_cast<uint64_t>(__ballot(v)) : static_cast<uint64_t>(v); };
     const PageTable& t = a.table;
-    int over = 0;                                  // entries past the table's width
+    int over = 0;                                  // entries past the table's width, 2^10 a row at most (2^20 rows stay below 2^31)
 
     struct Ask {
         int used, need, page;                      // page: of the last entry in use, to be copied (-1: none)
@@ -174,7 +174,7 @@ __device__ __forceinline__ void give_pages(const GiveArgs& a) {
         if (want > len) {
             const long long need = want > t.prefix_len ? (want - t.prefix_len + (1 << t.page_shift) - 1) >> t.page_shift : 0;
             r.need = static_cast<int>(min(max(need, static_cast<long long>(r.used)), static_cast<long long>(t.width)));
-            if (lane == 0 && need > t.width) over += static_cast<int>(min(need - t.width, 1ll << 30));
+            if (lane == 0 && need > t.width) over += static_cast<int>(min(need - t.width, 1ll << 10));
             if (own & ((1 << t.page_shift) - 1)) {
                 const int page = t.pages[static_cast<size_t>(i) * t.width + r.used - 1];
                 const int keep = a.keep ? a.keep[i] : 1;

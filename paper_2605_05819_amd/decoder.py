@@ -163,6 +163,8 @@ def beam_search(layers, caches, pool, norms, last_norm, embed, head, prompts, ru
     dev, n = embed.device, rule.beams
     counts = [len(p) for p in prompts]
     rows, size = n * len(prompts), pool.page_size
+    if not counts or min(counts) < 1:
+        raise ValueError("a beam search needs prompts of at least one token")
     if rows > DECODE_TOKENS:
         raise ValueError("a beam search takes at most %d rows" % DECODE_TOKENS)
     missing = pool.missing

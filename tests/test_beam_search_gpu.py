@@ -95,6 +95,11 @@ def test_refusals():
         call(cl.Beams(33), n=2)
     with pytest.raises(ValueError, match="missing"):
         call(cl.Beams(2), cl.PagePool.of(caches))
+    with pytest.raises(ValueError, match="at least one token"):
+        call(cl.Beams(2), n=0)
+    with pytest.raises(ValueError, match="at least one token"):
+        decoder.beam_search(layers, caches, pool, norms[:-1], norms[-1], embed, head,
+                            [torch.zeros(n, dtype=torch.int32, device="cuda") for n in (3, 0)], cl.Beams(2), 1)
 
 
 def test_the_example_runs(capsys):

@@ -278,3 +278,11 @@ def test_captured_steps_replay_like_eager_ones():
         torch.cuda.synchronize()
         for x, y in zip([a.table, a.len, a.pool.refs] + a.buffers(), [b.table, b.len, b.pool.refs] + b.buffers()):
             assert torch.equal(x, y)
+
+
+def test_wants_beyond_any_table_are_counted():
+    """Four rows that lack 2^31 - 4 entries each: the sum of what is missing does not wrap to nothing."""
+    w = World(20, 1, 4, 3)
+    w.reserve([2**31 - 1] * 4)
+    w.check()
+    assert int(w.missing) == 4 * 1024

@@ -66,7 +66,7 @@ def test_pools(kw, needle):
 @pytest.mark.parametrize("kw,status,needle", [
     (dict(table=0), cl.CL_EINVAL, "table"), (dict(kv_len=FAKE + 2), cl.CL_EINVAL, "kv_len"), (dict(rows=0), cl.CL_EINVAL, "positive"),
     (dict(width=0), cl.CL_EINVAL, "positive"), (dict(rows=(1 << 20) + 1), cl.CL_EUNSUPPORTED, "2^20"),
-    (dict(width=(1 << 26) + 1), cl.CL_EUNSUPPORTED, "2^26"),
+    (dict(width=(1 << 26) + 1), cl.CL_EUNSUPPORTED, "2^26"), (dict(rows=1 << 10, width=1 << 21), cl.CL_EUNSUPPORTED, "entries"),
     (dict(prefix=-1), cl.CL_EINVAL, "prefix_len"), (dict(ws=0), cl.CL_EWORKSPACE, "workspace"),
     (dict(bytes=100), cl.CL_EWORKSPACE, "workspace"), (dict(ws=FAKE + 16), cl.CL_EINVAL, "256-byte")])
 def test_fork_and_reserve(kw, status, needle):
