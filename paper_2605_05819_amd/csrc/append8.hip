@@ -28,6 +28,7 @@
 #include <type_traits>
 
 #include "append_common.h"
+#include "append_units.h"
 #include "cl_device.h"
 #include "cl_internal.h"
 #include "kv_common.h"
@@ -204,24 +205,27 @@ __device__ __forceinline__ void queries(const AppendArgs& a, float2* turns, int 
 // it, K's part in fp64 took 97 us where this takes 65.
 // R > 0: the wave holds the rows, 64 / LG an iteration and R of them at most, as
 // they came, from one batch of loads.  R = 0: any number, loaded for each pass.
+// A wave without a head helps with the turns and reads nothing of k and v.
 template <int LG, bool VEC, bool BF, int R>
 __device__ __forceinline__ void block_rows(const AppendArgs& a, const float2* turns, int t, int pos, int rows, int before, int first,
-                                           bool is_v, int head, bool shared_turns) {
+                                           const KvUnit& unit, bool shared_turns) {
     constexpr int ROWS = 64 / LG, HOLD = R > 0 ? R : 1;
     const int lane = threadIdx.x % LG, at = 8 * lane, group = (threadIdx.x & 63) / LG;
     const int D = a.cache.dim;
+    const bool is_v = unit.is_v;
     const bool turned = a.rope.inv_freq && at < a.rope.rot_dim && !is_v;
     const bool half = turned && !a.rope.interleaved;
     const int lo = half ? 4 * lane : at, hi = half ? a.rope.rot_dim / 2 + 4 * lane : at + 4;
     const int pairs = a.rope.rot_dim / 2;
-    const uint16_t* const src = (is_v ? a.v : a.k) + static_cast<size_t>(head) * D;
+    const uint16_t* const src = is_v ? a.v : a.k;
     const long long stride = is_v ? a.v_stride : a.k_stride;
+    const int loaded = loaded_rows(unit, rows);
     const uint16_t* const w = is_v ? nullptr : a.k_norm;
 
     Raw x[HOLD], y[HOLD];
     const auto load = [&](int i, Raw& rx, Raw& ry) {              // the block's i-th new row
         rx = ry = Raw{0u, 0u};
-        if (i < rows) load8<VEC>(src + static_cast<long long>(t + i) * stride, lo, hi, half, rx, ry);
+        if (i < loaded) load8<VEC>(src + row_offset(unit, stride, D, t + i), lo, hi, half, rx, ry);
     };
 #pragma unroll
     for (int n = 0; n < R; ++n)
@@ -234,7 +238,7 @@ __device__ __forceinline__ void block_rows(const AppendArgs& a, const float2* tu
         }
         __syncthreads();
     }
-    if (head < 0) return;
+    if (!unit.live) return;
 
     Quad wx = {}, wy = {};
     if (w) {
@@ -370,9 +374,8 @@ __global__ __launch_bounds__(256, R <= 8 ? 4 : 2) void kv_append8_kernel(AppendA
         return;
     }
     const int Hk = a.cache.heads, block = 1 << a.cache.block_shift, fours = (2 * Hk + 3) / 4;
-    const int unit0 = 4 * static_cast<int>(id % fours), unit = unit0 + wave;
-    const bool is_v = unit >= Hk;
-    const int head = unit < 2 * Hk ? (is_v ? unit - Hk : unit) : -1;
+    const int unit0 = 4 * static_cast<int>(id % fours);
+    const KvUnit unit = kv_unit(unit0 + wave, Hk);
     const bool shared_turns = a.rope.inv_freq && unit0 < Hk;
     const long long from = id / fours * span;
     const int to = static_cast<int>(min(from + span, static_cast<long long>(a.batch.tokens)));
@@ -397,8 +400,8 @@ __global__ __launch_bounds__(256, R <= 8 ? 4 : 2) void kv_append8_kernel(AppendA
         const int rows = min(block - before, q.start + q.count - t);
         const int page = a.batch.page_table[static_cast<size_t>(s) * a.batch.table_width + (mine >> a.cache.page_shift)];
         if ((before == 0 || t == q.start) && page >= 0 && page < a.cache.num_pages) {
-            const int first = ((page * Hk + max(head, 0)) << a.cache.page_shift) + (mine & ((1 << a.cache.page_shift) - 1));
-            block_rows<LG, VEC, BF, R>(a, turns, t, mine + a.batch.prefix_len, rows, before, first, is_v, head, shared_turns);
+            const int first = ((page * Hk + unit.head) << a.cache.page_shift) + (mine & ((1 << a.cache.page_shift) - 1));
+            block_rows<LG, VEC, BF, R>(a, turns, t, mine + a.batch.prefix_len, rows, before, first, unit, shared_turns);
             if (R > 0 && shared_turns && t + rows < to) __syncthreads();      // before the turns are others
         }
         t += rows;
