@@ -779,9 +779,10 @@ size_t cl_pages_workspace(const cl_page_pool* pool, int32_t rows);
  *                         overlap the old ones)
  *  room                   0..2^30
  *  ws                     device workspace, 256-byte aligned
- * An entry that got no page is -1 (attention over it gives NaN, appends do not
- * store) and counted in pool->missing, as are entries past the width (1024 of a row
- * at most).
+ * Where pages run out no key is lost: an entry for keys to come that got no page is -1 (attention over it gives NaN, appends do not
+ * store), and a row that got none for its copy goes on sharing its last page.  It may append
+ * nothing then: its next key's place is that of the others that share the page.  Both are counted in pool->missing, as are entries past the
+ * width (1024 of a row at most); cl_kv_reserve for the same keys asks again.
  * Errors: CL_EINVAL, CL_EUNSUPPORTED, CL_EWORKSPACE, CL_EHIP (all five calls).
  */
 cl_status cl_kv_fork(const cl_page_pool* pool, const int32_t* table, const int32_t* kv_len, int32_t num_seqs,

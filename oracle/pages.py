@@ -57,13 +57,13 @@ def _give(refs, table, kv_len, want, keep, size, prefix):
     for k, (i, e, old) in enumerate(asks):
         page = free[k] if k < len(free) else -1
         missing += page < 0
-        table[i][e] = page
         if page >= 0:
             refs[page] = 1
-        if old is not None:
-            refs[old] -= 1
-            if page >= 0:
+            if old is not None:
+                refs[old] -= 1
                 copies.append((old, page))
+        if page >= 0 or old is None:
+            table[i][e] = page
     return copies, missing
 
 

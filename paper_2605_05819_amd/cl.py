@@ -1134,7 +1134,8 @@ def kv_fork(pool, table, kv_len, parents, room=0, prefix_len=0, table_out=None, 
 
 def kv_reserve(pool, table, kv_len, want, prefix_len=0, ws=None, stream=None):
     """``cl_kv_reserve``: rows with want[b] > kv_len[b] (int32 [rows]) get the
-    pages they lack for want[b] keys, in place."""
+    pages they lack for want[b] keys, in place.  A pool that runs out loses no key
+    (``missing`` counts what is lacking); the same call asks again."""
     _check_table(table, kv_len)
     _dev_tensor(want, "want", _I32, (table.shape[0],))
     ws = _room(pages_workspace(pool, table.shape[0]), ws, table.device, stream)

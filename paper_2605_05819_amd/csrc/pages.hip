@@ -142,8 +142,10 @@ __device__ __forceinline__ void fork_row(const ForkArgs& a, int i) {
 
 // One workgroup: rows that are to grow ask for a page of their own in place of a
 // last one that others hold too (a copy), then for the entries they lack; the
-// lowest free pages go to them in row order.  What is free is scanned before any
-// count changes here, so no page is both copied from and given away.  LANES work
+// lowest free pages go to them in row order.  Where pages run out a row keeps the page that
+// it holds, shared as it was: its keys are whole, and it can ask again.  What is free is
+// scanned before any count changes here, so no page is both copied from and given
+// away.  LANES work
 // on a row: a wave where rows ask for many entries, one where they ask for a few (64
 // rows of one entry 5.7 us, 12 by waves).
 template <int LANES>
@@ -240,10 +242,10 @@ __device__ __forceinline__ void give_pages(const GiveArgs& a) {
         if (old >= 0) {
             to = at < have ? a.free[at] : -1;
             ++at;
-            if (lane == 0) {
+            if (lane == 0 && to >= 0) {
                 row[used - 1] = to;
                 atomicAdd(a.refs + old, -1);
-                if (to >= 0) a.refs[to] = 1;
+                a.refs[to] = 1;
             }
         }
         if (lane == 0) a.copy_to[i] = to;
