@@ -769,9 +769,9 @@ size_t cl_pages_workspace(const cl_page_pool* pool, int32_t rows);
  * parents[i] (several of one: samples, beams that go on; none of a row: its pages
  * are given back; a parent outside 0..num_seqs - 1: an empty row, which gets none).  Used pages are
  * shared.  With room > 0 each row can take `room` more keys at once: a last page that is
- * partly used becomes the row's own (the first child keeps it where no other row
- * holds it, the others get copies), and pages are given for what is to come.  Pages
- * held ahead go to the first child.
+ * partly used becomes the row's own (the first row that holds it keeps it where all its
+ * holders are among the new ones, the others get copies), and pages are given for what is to
+ * come.  Pages held ahead go to the first child.
  *  table, kv_len          device [num_seqs][width], [num_seqs]: the old rows, unchanged,
  *                         whose holdings pass to the new ones
  *  parents                device int32 [num_new]
@@ -779,10 +779,12 @@ size_t cl_pages_workspace(const cl_page_pool* pool, int32_t rows);
  *                         overlap the old ones)
  *  room                   0..2^30
  *  ws                     device workspace, 256-byte aligned
- * Where pages run out no key is lost: an entry for keys to come that got no page is -1 (attention over it gives NaN, appends do not
- * store), and a row that got none for its copy goes on sharing its last page.  It may append
- * nothing then: its next key's place is that of the others that share the page.  Both are counted in pool->missing, as are entries past the
- * width (1024 of a row at most); cl_kv_reserve for the same keys asks again.
+ * Where pages run out no key is lost: an entry for keys to come that got no page is
+ * -1 (attention over it gives NaN, appends do not store), and a row that got none for
+ * its copy goes on sharing its last page.  It may append nothing then: its next key's
+ * place is that of the others that share the page.  Both are counted in
+ * pool->missing, as are entries past the width (1024 of a row at most);
+ * cl_kv_reserve for the same keys asks again.
  * Errors: CL_EINVAL, CL_EUNSUPPORTED, CL_EWORKSPACE, CL_EHIP (all five calls).
  */
 cl_status cl_kv_fork(const cl_page_pool* pool, const int32_t* table, const int32_t* kv_len, int32_t num_seqs,
@@ -791,8 +793,9 @@ cl_status cl_kv_fork(const cl_page_pool* pool, const int32_t* table, const int32
 
 /*
  * cl_kv_reserve -- pages for rows that are to grow: a row with want[b] > kv_len[b]
- * gets what it lacks for want[b] keys, and a partly used last page of its own, a
- * copy, if others hold it too.
+ * gets what it lacks for want[b] keys, and a partly used last page of its own: a
+ * copy if others hold it too, but for the first of its holders where all of them
+ * are to grow.
  *  table, kv_len  device [num_seqs][width] (in place), [num_seqs]
  *  want           device int32 [num_seqs]
  * The rest and errors: as cl_kv_fork.

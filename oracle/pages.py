@@ -20,28 +20,34 @@ def fork(refs, table, kv_len, parents, size, room=0, prefix=0):
         for e, p in enumerate(table[r]):
             if _held(p, refs):
                 refs[p] += len(children[r]) - 1 if e < used else 0 if children[r] else -1
-    new, lens, keep = [], [], []
+    new, lens = [], []
     for i, r in enumerate(parents):
         if not 0 <= r < n:
-            new.append([-1] * width), lens.append(0), keep.append(0)
+            new.append([-1] * width), lens.append(0)
             continue
         used = -(-_own(kv_len[r], prefix, width, size) // size)
         first = children[r][0] == i
         new.append([p if _held(p, refs) and (e < used or first) else -1 for e, p in enumerate(table[r])])
         lens.append(max(kv_len[r], 0))
-        keep.append(len(children[r]) if first else 0)
     want = [x + room if 0 <= r < n else 0 for x, r in zip(lens, parents)]
-    copies, missing = _give(refs, new, lens, want, keep, size, prefix) if room else ([], 0)
+    copies, missing = _give(refs, new, lens, want, size, prefix) if room else ([], 0)
     return new, lens, copies, missing
 
 
 def reserve(refs, table, kv_len, want, size, prefix=0):
-    return _give(refs, table, kv_len, want, [1] * len(table), size, prefix)
+    return _give(refs, table, kv_len, want, size, prefix)
 
 
-def _give(refs, table, kv_len, want, keep, size, prefix):
+def _give(refs, table, kv_len, want, size, prefix):
+    """A growing row copies a partly used last page that others hold too, but where all its holders grow the first
+    keeps it; then it gets what it lacks.  Where pages run out the row keeps the one it holds."""
     width = len(table[0])
     asks, missing = [], 0
+    growing = {}
+    for i, row in enumerate(table):
+        own = _own(kv_len[i], prefix, width, size)
+        if want[i] > kv_len[i] and own % size:
+            growing.setdefault(row[-(-own // size) - 1], []).append(i)
     for i, row in enumerate(table):
         own = _own(kv_len[i], prefix, width, size)
         used = -(-own // size)
@@ -49,8 +55,10 @@ def _give(refs, table, kv_len, want, keep, size, prefix):
             continue
         need = max(-(-max(want[i] - prefix, 0) // size), used)
         missing += min(max(need - width, 0), 1024)
-        if own % size and _held(row[used - 1], refs) and not (keep[i] > 0 and refs[row[used - 1]] == keep[i]):
-            asks.append((i, used - 1, row[used - 1]))
+        if own % size and _held(row[used - 1], refs):
+            who = growing[row[used - 1]]
+            if len(who) != refs[row[used - 1]] or who[0] != i:
+                asks.append((i, used - 1, row[used - 1]))
         asks += [(i, e, None) for e in range(used, min(need, width)) if not _held(row[e], refs)]
     free = [p for p, c in enumerate(refs) if c == 0]
     copies = []

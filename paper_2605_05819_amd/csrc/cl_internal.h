@@ -218,7 +218,7 @@ struct PageTable {
 struct ForkArgs {
     PageTable from, to;
     const int32_t* parents;
-    int32_t *refs, *keep;          // keep: holders of a row's last page if it is the row's alone, else 0; -1: no row
+    int32_t *refs, *keep;          // keep: the children of a row's parent, of the first of them; -1 less that of the others; -1: no row
     int num_pages;
 };
 struct GiveArgs {

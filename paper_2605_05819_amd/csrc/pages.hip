@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void fork_rows_kernel(ForkArgs a) {
         }
         if (tid == 0) {
             a.to.kv_len[i] = len;
-            a.keep[i] = !valid ? -1 : first ? sums[2] : 0;
+            a.keep[i] = !valid ? -1 : first ? sums[2] : -1 - sums[2];
         }
     }
     if (i < a.from.rows) {
@@ -126,7 +126,7 @@ __device__ __forceinline__ void fork_row(const ForkArgs& a, int i) {
         }
         if (lane == 0) {
             a.to.kv_len[i] = len;
-            a.keep[i] = !valid ? -1 : earlier == 0 ? siblings : 0;
+            a.keep[i] = !valid ? -1 : earlier == 0 ? siblings : -1 - siblings;
         }
     }
     if (i < a.from.rows) {
@@ -141,12 +141,12 @@ __device__ __forceinline__ void fork_row(const ForkArgs& a, int i) {
 // ------------------------------------------------------------- giving pages
 
 // One workgroup: rows that are to grow ask for a page of their own in place of a
-// last one that others hold too (a copy), then for the entries they lack; the
-// lowest free pages go to them in row order.  Where pages run out a row keeps the page that
+// partly used last one that others hold too (a copy), then for the entries they lack; the
+// lowest free pages go to them in row order.  A last page whose holders are all to
+// grow stays with the first of them.  Where pages run out a row keeps the page that
 // it holds, shared as it was: its keys are whole, and it can ask again.  What is free is
 // scanned before any count changes here, so no page is both copied from and given
-// away.  LANES work
-// on a row: a wave where rows ask for many entries, one where they ask for a few (64
+// away.  LANES work on a row: a wave where rows ask for many entries, one where they ask for a few (64
 // rows of one entry 5.7 us, 12 by waves).
 template <int LANES>
 __device__ __forceinline__ void give_pages(const GiveArgs& a) {
@@ -160,10 +160,11 @@ __device__ __forceinline__ void give_pages(const GiveArgs& a) {
 
     struct Ask {
         int used, need, page;                      // page: of the last entry in use, to be copied (-1: none)
+        bool open;                                 // others than the parent's children hold it too, who may all be growing
     };
     const auto want_of = [&](int i, int len) {         // a new row without a parent stays empty
         if (a.want) return static_cast<long long>(a.want[i]);
-        return a.keep[i] < 0 ? 0ll : static_cast<long long>(len) + a.room;
+        return a.keep[i] == -1 ? 0ll : static_cast<long long>(len) + a.room;
     };
     const auto ask_of = [&](int i) {
         const int len = max(t.kv_len[i], 0);
@@ -173,30 +174,63 @@ __device__ __forceinline__ void give_pages(const GiveArgs& a) {
         r.used = entries_of(t, own);
         r.need = r.used;
         r.page = -1;
+        r.open = false;
         if (want > len) {
             const long long need = want > t.prefix_len ? (want - t.prefix_len + (1 << t.page_shift) - 1) >> t.page_shift : 0;
             r.need = static_cast<int>(min(max(need, static_cast<long long>(r.used)), static_cast<long long>(t.width)));
             if (lane == 0 && need > t.width) over += static_cast<int>(min(need - t.width, 1ll << 10));
             if (own & ((1 << t.page_shift) - 1)) {
                 const int page = t.pages[static_cast<size_t>(i) * t.width + r.used - 1];
-                const int keep = a.keep ? a.keep[i] : 1;
-                if (in_pool(page, a.num_pages) && !(keep > 0 && a.refs[page] == keep)) r.page = page;
+                const int keep = a.keep ? a.keep[i] : 1, kin = keep > 0 ? keep : -1 - keep;
+                if (in_pool(page, a.num_pages)) {
+                    r.open = a.refs[page] != kin;
+                    if (r.open || keep < 0) r.page = page;
+                }
             }
         }
         return r;
     };
 
+    bool open = false;
     for (int i = team; i < t.rows; i += TEAMS) {
         const Ask r = ask_of(i);
+        open |= r.open;
         int n = r.page >= 0 ? 1 : 0;
         for (int e = r.used; e < r.need; e += LANES)
             n += __popcll(votes(e + lane < r.need && !in_pool(t.pages[static_cast<size_t>(i) * t.width + e + lane], a.num_pages)));
         if (lane == 0) {
             a.count[i] = n;
             a.copy_from[i] = r.page;
+            a.copy_to[i] = r.open ? r.page : -1;
         }
     }
-    __syncthreads();
+    if (__syncthreads_or(open)) {
+        // The holders that grow leave their pages; one that nobody holds then stays
+        // with the first of them (by number, through a.free's place for the page), and
+        // all counts are put back.  Other waves' values are read by atomics, past the L1.
+        const auto pages = [&](auto what) {
+            for (int i = tid; i < t.rows; i += kScan) {
+                const int page = a.copy_to[i];
+                if (page >= 0) what(i, page);
+            }
+            __threadfence();
+            __syncthreads();
+        };
+        pages([&](int, int page) {
+            atomicAdd(a.refs + page, -1);
+            atomicExch(a.free + page, 0x7fffffff);
+        });
+        pages([&](int i, int page) {
+            if (atomicAdd(a.refs + page, 0) == 0) atomicMin(a.free + page, i);
+        });
+        pages([&](int i, int page) {
+            if (atomicAdd(a.free + page, 0) == i) {
+                a.copy_from[i] = -1;
+                --a.count[i];
+            }
+        });
+        pages([&](int, int page) { atomicAdd(a.refs + page, 1); });
+    }
     int asked = 0;
     for (int base = 0; base < t.rows; base += kScan) {
         const int n = base + tid < t.rows ? a.count[base + tid] : 0;

@@ -1,4 +1,5 @@
-"""Pools that run out: no row loses keys that it held, and a call that is made again gets what was missing."""
+"""Pools that run out, and last pages whose holders all grow: no row loses keys that it held, a call that is made again
+gets what was missing, and a page stays with one of its holders where all of them would leave it."""
 
 import random
 
@@ -6,6 +7,17 @@ import pytest
 import torch
 
 from oracle import pages
+
+
+def test_all_holders_grow_and_the_first_keeps_the_page():
+    # rows 0 and 1 share page 1 (6 keys of pages of 4); one page is free
+    refs, table = [2, 2, 0], [[0, 1, -1], [0, 1, -1]]
+    copies, missing = pages.reserve(refs, table, [6, 6], [7, 7], 4)
+    assert copies == [(1, 2)] and missing == 0 and table == [[0, 1, -1], [0, 2, -1]] and refs == [2, 1, 1]
+    # a holder that does not grow keeps it: the other one copies
+    refs, table = [2, 2, 0], [[0, 1, -1], [0, 1, -1]]
+    copies, missing = pages.reserve(refs, table, [6, 6], [7, 6], 4)
+    assert copies == [(1, 2)] and missing == 0 and table == [[0, 2, -1], [0, 1, -1]] and refs == [2, 1, 1]
 
 
 def test_a_row_without_a_page_for_its_copy_keeps_the_shared_one():
@@ -17,6 +29,13 @@ def test_a_row_without_a_page_for_its_copy_keeps_the_shared_one():
     pages.free(refs, table, lens, [3])
     copies, missing = pages.reserve(refs, table, lens, [7, 7, 6, 0], 4)
     assert copies == [(1, 2)] and missing == 1 and table[:3] == [[0, 2, -1], [0, 1, -1], [0, 1, -1]] and refs == [3, 2, 1]
+
+
+def test_children_of_different_parents():
+    # rows 0 and 1 share page 0 and have two children and one
+    refs, table = [2, 0, 0], [[0, -1], [0, -1]]
+    new, n, copies, missing = pages.fork(refs, table, [3, 3], [1, 0, 0], 4, room=1)
+    assert new == [[0, -1], [1, -1], [2, -1]] and copies == [(0, 1), (0, 2)] and missing == 0 and refs == [1, 1, 1]
 
 
 def _rows(w):
@@ -70,3 +89,19 @@ def test_scarce_pools_lose_no_keys(seed):
             w.reserve([max(a, b) if b else 0 for a, b in zip(want, w.n)])
             w.check()
             assert _rows(w) == before
+
+
+@pytest.mark.gpu
+def test_many_rows_share_and_grow():
+    """More rows than the scanning workgroup has threads, groups of them over one last page each."""
+    from tests.test_pages_gpu import World
+    g = random.Random(5)
+    w = World(1600, 4, 300, 3, layers=1, heads=1, seed=1)
+    w.reserve([6] * 300)
+    w.set([6] * 300)
+    w.fork([g.randint(0, 299) for _ in range(1500)], 0)
+    w.check()
+    w.reserve([x + (g.random() < 0.9) for x in w.n])
+    w.check()
+    w.fork(list(range(1500)), 1)
+    w.check()
