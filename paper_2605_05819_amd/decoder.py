@@ -156,8 +156,8 @@ def beam_search(layers, caches, pool, norms, last_norm, embed, head, prompts, ru
     """The best hypotheses of ``steps`` tokens behind each of ``prompts`` (int32
     tensors) by ``rule`` (a cl.Beams whose picks are its beams).  embed and head
     [vocab][hidden] in the activations' dtype; logits are fp32.  ``caches`` (16 or 8
-    bits, one a layer) hold the pages of ``pool``, which are given back at the end.
-    A full pool is an error."""
+    bits, one a layer) hold the pages of ``pool``, which are given back at the end,
+    whatever ends the search.  A full pool is an error."""
     if rule.picks != rule.beams:
         raise ValueError("a beam search goes on with as many picks as it has beams")
     dev, n = embed.device, rule.beams
@@ -180,37 +180,40 @@ def beam_search(layers, caches, pool, norms, last_norm, embed, head, prompts, ru
     # the prompts, a row each
     kv_len = i32([0] * len(prompts))
     table = torch.full((len(prompts), width), -1, dtype=torch.int32, device=dev)
-    cl.kv_reserve(pool, table, kv_len, i32(counts))
-    kv_len.copy_(i32(counts))
-    ends = torch.tensor(counts, device=dev).cumsum(0)
-    start = torch.cat([ends.new_zeros(1), ends]).to(torch.int32)
-    batch = cl.KvBatch(kv_len, table, sum(counts), q_len=max(counts), q_start=start, max_kv_len=max(counts))
-    _, y = run(layers, caches, batch, embed[torch.cat(list(prompts)).long()], norms, last_norm, eps)
-    # every hypothesis but a prompt's first begins with a score of -inf: the first choice is among the first's tokens
-    old = cl.kv_fork(pool, table, kv_len, i32([g for g in range(len(prompts)) for _ in range(n)]))
-    new = tuple(torch.empty_like(t) for t in old)
-    x = logits(y[ends - 1]).repeat_interleave(n, 0)
-    s = Hypotheses(torch.zeros((rows, steps), dtype=torch.int32, device=dev),
-                   torch.where(torch.arange(rows, device=dev) % n == 0, 0.0, float("-inf")),
-                   torch.zeros(rows, dtype=torch.int32, device=dev), torch.zeros(rows, dtype=torch.int32, device=dev))
-    spare = torch.empty_like(s.tokens)
-    finished = s.finished if rule.eos >= 0 else None
-    for step in range(steps):
-        scores, tokens, parents, lengths, done = cl.beam_select(rule, x, s.scores, s.lengths, finished)
-        cl.gather_rows([s.tokens], parents, [spare])
-        spare, s.tokens = s.tokens, spare
-        s.tokens[:, step] = tokens.view(-1)
-        s.scores, s.lengths, s.finished = scores.view(-1), lengths.view(-1), done.view(-1)
+    held = table, kv_len                # the rows that hold the pages
+    try:
+        cl.kv_reserve(pool, table, kv_len, i32(counts))
+        kv_len.copy_(i32(counts))
+        ends = torch.tensor(counts, device=dev).cumsum(0)
+        start = torch.cat([ends.new_zeros(1), ends]).to(torch.int32)
+        batch = cl.KvBatch(kv_len, table, sum(counts), q_len=max(counts), q_start=start, max_kv_len=max(counts))
+        _, y = run(layers, caches, batch, embed[torch.cat(list(prompts)).long()], norms, last_norm, eps)
+        # every hypothesis but a prompt's first begins with a score of -inf: the first choice is among the first's tokens
+        old = held = cl.kv_fork(pool, table, kv_len, i32([g for g in range(len(prompts)) for _ in range(n)]))
+        new = tuple(torch.empty_like(t) for t in old)
+        x = logits(y[ends - 1]).repeat_interleave(n, 0)
+        s = Hypotheses(torch.zeros((rows, steps), dtype=torch.int32, device=dev),
+                       torch.where(torch.arange(rows, device=dev) % n == 0, 0.0, float("-inf")),
+                       torch.zeros(rows, dtype=torch.int32, device=dev), torch.zeros(rows, dtype=torch.int32, device=dev))
+        spare = torch.empty_like(s.tokens)
         finished = s.finished if rule.eos >= 0 else None
-        if step + 1 == steps:
-            break
-        table, kv_len = cl.kv_fork(pool, *old, parents.view(-1), room=1, table_out=new[0], kv_len_out=new[1])
-        old, new = new, old
-        kv_len.add_(1)
-        batch = cl.KvBatch(kv_len, table, rows, max_kv_len=max(counts) + step + 1)
-        _, y = run(layers, caches, batch, embed[tokens.view(-1).long()], norms, last_norm, eps)
-        x = logits(y)
-    cl.kv_free(pool, *old)
+        for step in range(steps):
+            scores, tokens, parents, lengths, done = cl.beam_select(rule, x, s.scores, s.lengths, finished)
+            cl.gather_rows([s.tokens], parents, [spare])
+            spare, s.tokens = s.tokens, spare
+            s.tokens[:, step] = tokens.view(-1)
+            s.scores, s.lengths, s.finished = scores.view(-1), lengths.view(-1), done.view(-1)
+            finished = s.finished if rule.eos >= 0 else None
+            if step + 1 == steps:
+                break
+            held = table, kv_len = cl.kv_fork(pool, *old, parents.view(-1), room=1, table_out=new[0], kv_len_out=new[1])
+            old, new = new, old
+            kv_len.add_(1)
+            batch = cl.KvBatch(kv_len, table, rows, max_kv_len=max(counts) + step + 1)
+            _, y = run(layers, caches, batch, embed[tokens.view(-1).long()], norms, last_norm, eps)
+            x = logits(y)
+    finally:
+        cl.kv_free(pool, *held)
     if int(missing):
         raise RuntimeError("the pool had %d pages too few" % int(missing))
     return s
