@@ -170,7 +170,7 @@ def beam_search(layers, caches, pool, norms, last_norm, embed, head, prompts, ru
     missing = pool.missing
     if missing is None:
         raise ValueError("the pool of a beam search needs its count of missing pages")
-    missing.zero_()
+    before = missing.clone()            # the pool's count goes on: what earlier calls lacked stays in it
     i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=dev)  # noqa: E731
     width = -(-(max(counts) + steps) // size)
 
@@ -214,8 +214,9 @@ def beam_search(layers, caches, pool, norms, last_norm, embed, head, prompts, ru
             x = logits(y)
     finally:
         cl.kv_free(pool, *held)
-    if int(missing):
-        raise RuntimeError("the pool had %d pages too few" % int(missing))
+    short = int(missing - before)
+    if short:
+        raise RuntimeError("the pool had %d pages too few" % short)
     return s
 
 

@@ -1,4 +1,4 @@
-"""How a beam search leaves its pool: every page given back, whatever ends it."""
+"""How a beam search leaves its pool: every page given back, whatever ends it, and its count of missing pages added to."""
 
 import pytest
 import torch
@@ -55,3 +55,19 @@ def test_prompts_too_long_for_experts():
         search(m, [list(range(40)), [5] * 25])
     assert held(pool) == 0
     assert search(m, [list(range(40)), [5] * 24]).tokens.shape == (6, 6) and held(pool) == 0
+
+
+def test_the_count_of_missing_pages_goes_on():
+    """What earlier calls lacked is neither an error of this search nor lost; what this one lacks is added."""
+    m = model(False, 6)
+    pool = m[3]
+    table, n = torch.full((1, 9), -1, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    cl.kv_reserve(pool, table, n, torch.full_like(n, 9 * PAGE))       # 9 pages of 6
+    assert int(pool.missing) == 3
+    cl.kv_free(pool, table, n)
+    search(m, [[3, 1, 4]], beams=2, steps=3)
+    assert int(pool.missing) == 3 and held(pool) == 0
+    with pytest.raises(RuntimeError, match="pages too few") as e:
+        search(m, [list(range(30))], beams=4, steps=12)
+    assert int(pool.missing) == 3 + int(str(e.value).split("had ")[1].split()[0]) and held(pool) == 0
+    search(m, [[3, 1, 4]], beams=2, steps=3)
