@@ -712,7 +712,8 @@ cl_status cl_attention8(const cl_kv_cache8* cache, const cl_kv_batch* batch, con
                         float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /* Workspace bytes for cl_attention8, as cl_attention_workspace; for prompts of
- * many tokens with room for their keys and values in 16 bits, up to 2 GiB. */
+ * many tokens with room for the keys and values, in 16 bits, of as many sequences as
+ * can have such a prompt among the batch's tokens, up to 2 GiB. */
 size_t cl_attention8_workspace(const cl_kv_cache8* cache, const cl_kv_batch* batch, int32_t q_heads);
 
 /*

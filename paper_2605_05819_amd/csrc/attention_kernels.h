@@ -784,8 +784,25 @@ constexpr float kSlack = 3.f;
 // an engine idle (ragged prompts 858 -> 2122 us that way round).
 constexpr int tile_lds(int D) { return 4 * tile_keys(D) * D * 2; }
 
+// Workgroup `id`'s head, split, row block and sequence.
+struct TilePlace {
+    int head, split, block, seq;
+};
+
+template <bool PREFIX>
+__device__ __forceinline__ TilePlace tile_place(const AttnArgs& a, const Plan& pl, int id) {
+    const int head = id % a.cache.heads;
+    int rest = id / a.cache.heads;
+    const int splits = PREFIX ? pl.psplits : pl.splits;
+    const int split = rest % splits;
+    rest /= splits;
+    const int blocks = PREFIX ? pl.pblocks : pl.blocks, upper = (blocks + 1) / 2, nth = rest % blocks;
+    return TilePlace{head, split, pl.paired && nth >= upper ? nth - upper : blocks - 1 - nth, rest / blocks};
+}
+
 template <int D, bool BF, bool Q8, int NQ, bool PREFIX>
-__device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int id, unsigned char* lds) {
+__device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, const TilePlace& place, const Segment& seg,
+                                          unsigned char* lds) {
     constexpr int NS = D / 32, ND = D / 16, CH = D / 8, KT = tile_keys(D), KB = KT / 16;
     constexpr int RW = 64 * NQ;                       // rows of a workgroup
     constexpr int WR = KT / 4;                        // keys of a tile that a wave copies
@@ -795,14 +812,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs& a, const Plan& pl, int
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g4 = lane >> 4, col = lane & 15;
     const int Hk = a.cache.heads, group = a.q_heads / Hk;
-    const int head = id % Hk;
-    int rest = id / Hk;
-    const int splits = PREFIX ? pl.psplits : pl.splits, len = PREFIX ? pl.plen : pl.len;
-    const int split = rest % splits;
-    rest /= splits;
-    const int blocks = PREFIX ? pl.pblocks : pl.blocks, upper = (blocks + 1) / 2, nth = rest % blocks;
-    const int block = pl.paired && nth >= upper ? nth - upper : blocks - 1 - nth;
-    const Segment seg = PREFIX ? prefix_segment(a) : own_segment(a, rest / blocks);
+    const int head = place.head, split = place.split, block = place.block, len = PREFIX ? pl.plen : pl.len;
     const int nrows = (PREFIX ? a.batch.tokens : min(seg.seq.count, a.batch.q_len)) * group;
     if (block * RW >= nrows) return;
     const int begin = split * len, end = min(begin + len, seg.keys);
@@ -1240,13 +1250,16 @@ __global__ __launch_bounds__(256, (O <= S2 || O == S0) && D > 128 ? 1 : P == NON
     if constexpr (P != NONE) {
         if (id < pl.pgrid) {
             if constexpr (P <= S2) attn_stream<D, BF, Q8, P, true, false>(a, pl, id, lds);
-            else attn_tile<D, BF, Q8, P - S2, true>(a, pl, id, lds);
+            else attn_tile<D, BF, Q8, P - S2, true>(a, pl, tile_place<true>(a, pl, id), prefix_segment(a), lds);
             return;
         }
     }
     if constexpr (O == S0) attn_stream<D, BF, Q8, 1, false, true>(a, pl, id - pl.pgrid, lds);
     else if constexpr (O <= S2) attn_stream<D, BF, Q8, O, false, false>(a, pl, id - pl.pgrid, lds);
-    else attn_tile<D, BF, Q8, O - S2, false>(a, pl, id - pl.pgrid, lds);
+    else {
+        const TilePlace place = tile_place<false>(a, pl, id - pl.pgrid);
+        attn_tile<D, BF, Q8, O - S2, false>(a, pl, place, own_segment(a, place.seq), lds);
+    }
 }
 
 // ------------------------------------------------------------- joining splits
@@ -1407,6 +1420,23 @@ hipError_t launch(const AttnArgs& a, Plan p, hipStream_t st) {
     });
 }
 
+// The splits' results into the call's.
+template <int D>
+hipError_t join(const AttnArgs& a, Plan p, hipStream_t st) {
+    const size_t rows = static_cast<size_t>(a.batch.tokens) * a.q_heads;
+    if (p.psplits + p.splits <= kRowSplits && rows >= 4096) {
+        constexpr size_t at = 1024 / D;
+        return launch_all(static_cast<long long>((rows + at - 1) / at), [&](unsigned first, unsigned count) {
+            p.first = first;
+            hipLaunchKernelGGL((attn_join_rows_kernel<D>), dim3(count), dim3(256), 0, st, a, p);
+        });
+    }
+    return launch_all(static_cast<long long>(rows), [&](unsigned first, unsigned count) {
+        p.first = first;
+        hipLaunchKernelGGL((attn_join_kernel<D>), dim3(count), dim3(256), 0, st, a, p);
+    });
+}
+
 // The prefix's unit has at least as many rows as a sequence's, so these
 // combinations cover every call (a tiled prefix takes 128-row tiles, a streamed
 // one of 17 to 32 rows streams the sequences' likewise).
@@ -1442,30 +1472,22 @@ hipError_t run(const AttnArgs& a, Plan p, hipStream_t st) {
             : own == T1 ? launch<D, BF, Q8, T2, T1>(a, p, st)
                         : launch<D, BF, Q8, T2, T2>(a, p, st);
     }
-    if (e != hipSuccess || p.direct) return e;
-    const size_t rows = static_cast<size_t>(a.batch.tokens) * a.q_heads;
-    if (p.psplits + p.splits <= kRowSplits && rows >= 4096) {
-        constexpr size_t at = 1024 / D;
-        return launch_all(static_cast<long long>((rows + at - 1) / at), [&](unsigned first, unsigned count) {
-            p.first = first;
-            hipLaunchKernelGGL((attn_join_rows_kernel<D>), dim3(count), dim3(256), 0, st, a, p);
-        });
-    }
-    return launch_all(static_cast<long long>(rows), [&](unsigned first, unsigned count) {
-        p.first = first;
-        hipLaunchKernelGGL((attn_join_kernel<D>), dim3(count), dim3(256), 0, st, a, p);
-    });
+    return e != hipSuccess || p.direct ? e : join<D>(a, p, st);
 }
 
-// Splits' room in the workspace, and the kernels for the heads' width and type.
+// Splits' room in the workspace.
+void place_parts(const AttnArgs& a, void* ws, Plan& p) {
+    if (p.direct) return;
+    const size_t n = static_cast<size_t>(p.psplits + p.splits) * a.batch.tokens * a.q_heads;
+    p.part = static_cast<float*>(ws);
+    p.stat = reinterpret_cast<float2*>(static_cast<char*>(ws) + up256(n * a.cache.dim * sizeof(float)));
+}
+
+// The kernels for the heads' width and type.
 template <bool Q8>
 hipError_t launch_for(const AttnArgs& a, void* ws, hipStream_t st) {
     Plan p = make_plan(a.cache, a.batch, a.q_heads);
-    if (!p.direct) {
-        const size_t n = static_cast<size_t>(p.psplits + p.splits) * a.batch.tokens * a.q_heads;
-        p.part = static_cast<float*>(ws);
-        p.stat = reinterpret_cast<float2*>(static_cast<char*>(ws) + up256(n * a.cache.dim * sizeof(float)));
-    }
+    place_parts(a, ws, p);
     const bool bf = a.cache.dtype == DT_BF16;
     if (a.cache.dim == 64) return bf ? run<64, true, Q8>(a, p, st) : run<64, false, Q8>(a, p, st);
     if (a.cache.dim == 128) return bf ? run<128, true, Q8>(a, p, st) : run<128, false, Q8>(a, p, st);
