@@ -869,8 +869,9 @@ typedef struct cl_beams {
  * elsewhere.  Picks come by descending rank, ties by the lower beam, then by the
  * larger logit, then by the lower token.  A beam whose score or whose logits are all
  * -inf has candidates of -inf; a NaN among its logits, +inf there, or a score that is
- * NaN or +inf makes all of them NaN, which are picked last.  Ranks are fp64, of sums off by about
- * 2^-24; scores are rounded once to float32.
+ * NaN or +inf makes all of them NaN, which are picked last.  Ranks are fp64, of sums
+ * whose logarithms are off by 2^-21.8 at most (where many equal logits round alike;
+ * 2^-25 and less as a rule); scores are rounded once to float32.
  *  logits   device [groups * beams][vocab] of logits_dtype (CL_FP16, CL_BF16, CL_FP32),
  *           logits_stride elements from row to row (>= vocab), aligned to its elements
  *  vocab    1..2^19 (CL_EUNSUPPORTED beyond); picks <= beams * vocab

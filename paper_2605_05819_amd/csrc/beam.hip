@@ -10,17 +10,24 @@
 //    exponentials and its k best logits.  Where each of the four waves has k / 4
 //    lanes whose maxima reach a bound, k values do; what reaches the least of the
 //    waves' k / 4-th largest lane maxima (two or three times k values as a rule) goes to
-//    a list in LDS, where each counts how many stand ahead of it.  Where ties fill
-//    the list, the k best are taken one after another instead.
+//    a list in LDS, where each counts how many stand ahead of it.  Where ties with that
+//    bound fill the list (masked vocabularies: 27 us for 128 rows of 128000, 21 unmasked)
+//    it takes what is above the bound, and the lowest tokens at it.
 //  * beam_pick: a workgroup a group: sums joined per beam in fp64, a beam's k best
 //    from its chunks' (a lane walks a chunk's list), then the ranks in fp64, each
 //    candidate counting those ahead of it.
 //
-// The sums (and a length's power, off by some 2^-51) are the only rounding that can change an order: an exponential is off
-// by 2^-23 of itself, differently for each value, terms are added in fp32 within a
-// lane and in fp64 beyond, so a row's logarithm is off by some 2^-24 / sqrt(lanes).
-// Bound by the read of the logits and by the issue of about ten instructions a
-// value (the exponential counts four).
+// The sums (and a length's power, off by some 2^-51) are the only rounding that can change an order.  e^l is 2^(l log2 e)
+// with what the product's rounding leaves out, and what log2 e lacks in fp32, to first
+// order; nothing is taken from l ahead of it where no exponential can overflow or
+// vanish (a chunk's largest logit in -32..64), so that nothing else is rounded.  The instruction
+// is off by 2^-23.5 at most (measured over its range; -2^-28 on the mean), eight terms are
+// added in fp32 as a tree, the rest in fp64: a row's logarithm is off by 2^-21.8 at most, where all
+// terms round alike, and by 2^-25 (root mean square; sharp rows of 2000) to 2^-29 (flat ones of 128000)
+// where they do not.
+// Bound by the read of the logits and by the issue of about fourteen instructions a
+// value (the exponential counts four): 128 rows of 128000 in bf16 13.4 us (12.2 with a
+// plain 2^(l log2 e - top log2 e), off by 2^-21), in fp32 16.8.
 
 #include <math.h>
 
@@ -32,7 +39,8 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kLog2e = 1.4426950408889634, kLn2 = 0.69314718055994531;
+constexpr float kLog2eHi = static_cast<float>(kLog2e), kLog2eLo = static_cast<float>(kLog2e - kLog2eHi);
 constexpr int kList = 1024;                  // entries of a workgroup's list
 constexpr int kMaxSplits = 64;               // a lane each in beam_pick
 
@@ -91,7 +99,7 @@ __global__ __launch_bounds__(256, 8) void beam_scan_kernel(BeamArgs a) {
     __shared__ int filled;
     __shared__ float tops[4];
     __shared__ uint32_t bounds[4];
-    __shared__ float sums[256];
+    __shared__ double sums[256];
     __shared__ u64 best[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
@@ -174,41 +182,96 @@ __global__ __launch_bounds__(256, 8) void beam_scan_kernel(BeamArgs a) {
     for (int w = 1; w < 4; ++w) bound = full ? min(bound, bounds[w]) : max(bound, bounds[w]);
     const float least = bound ? from_key(bound) : -INFINITY;
 
-    // 2^(x log2 e - zero): what rounding adds is different for each value, as long as
-    // the reference is `zero` itself and not the maximum that it was rounded from
-    const float zero = top == -INFINITY ? 0.f : top * kLog2e;
-    const bool far = fabsf(top) >= 16777216.0f && fabsf(top) <= 3.4028234663852886e38f;
-    float s = 0.f;
-    if (!far) {
+    // the sum of e^(x - reference), as 2^p with what p lacks beside it; far below the
+    // reference (-inf too) is 0, and a NaN or an infinity makes the row's sum NaN
+    const bool near = top >= -32.0f && top <= 64.0f;      // reference 0
+    const double zero = near ? 0.0 : static_cast<double>(top);
+    double s = 0.0;
+    float more = 0.f;
+    const auto add = [&](int i, auto form) {
+        float e[VEC];
 #pragma unroll
-        for (int j = 0; j < EPT; ++j) s += __builtin_amdgcn_exp2f(fmaf(x[j], kLog2e, -zero));
-    } else {                                       // masks of a type's lowest value: `zero` is too far from top, x - top is exact
+        for (int j = 0; j < VEC; ++j) {
+            float p, rest;
+            form(x[i * VEC + j], p, rest);
+            e[j] = __builtin_amdgcn_exp2f(p);
+            more = fmaf(e[j], rest, more);
+        }
 #pragma unroll
-        for (int j = 0; j < EPT; ++j) s += __builtin_amdgcn_exp2f((x[j] - top) * kLog2e);
+        for (int w = VEC / 2; w > 0; w /= 2)
+#pragma unroll
+            for (int j = 0; j < w; ++j) e[j] += e[j + w];
+        s += static_cast<double>(e[0]);
+    };
+    if (near) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            add(i, [](float l, float& p, float& rest) {
+                l = fmaxf(l, -200.f);
+                p = l * kLog2eHi;
+                rest = fmaf(l, kLog2eLo, fmaf(l, kLog2eHi, -p));
+            });
+    } else {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            add(i, [zero](float l, float& p, float& rest) {
+                const double d = fmax(static_cast<double>(l) - zero, -200.0) * kLog2e;
+                p = static_cast<float>(d);
+                rest = static_cast<float>(d - static_cast<double>(p));
+            });
     }
+    s = mine != mine || top == INFINITY ? static_cast<double>(NAN) : s + static_cast<double>(more) * kLn2;
     sums[tid] = s;
 
+    // those that `fit` to the list, as far as it goes
+    const auto collect = [&](auto fit) {
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i)
-        if (__ballot(group[i] >= least)) {
+        for (int i = 0; i < LOADS; ++i)
+            if (__ballot(fit(group[i]))) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j)
-                if (x[i * VEC + j] >= least && token(i * VEC + j) < a.vocab) {
-                    const int at = atomicAdd(&filled, 1);
-                    if (at < kList) list[at] = candidate(x[i * VEC + j], token(i * VEC + j));
-                }
-        }
+                for (int j = 0; j < VEC; ++j)
+                    if (fit(x[i * VEC + j]) && token(i * VEC + j) < a.vocab) {
+                        const int at = atomicAdd(&filled, 1);
+                        if (at < kList) list[at] = candidate(x[i * VEC + j], token(i * VEC + j));
+                    }
+            }
+    };
+    collect([least](float v) { return v >= least; });
     __syncthreads();
     const size_t slot = static_cast<size_t>(row) * a.splits + split;
     u64* const out = a.best + slot * a.picks;
     if (wave == 3) {
-        const double total = wave_sum(static_cast<double>(sums[lane]) + sums[lane + 64] + sums[lane + 128] + sums[lane + 192]);
+        const double total = wave_sum(sums[lane] + sums[lane + 64] + sums[lane + 128] + sums[lane + 192]);
         if (lane == 0) {
             a.sum[slot] = total;
-            a.most[slot] = top == -INFINITY || far ? static_cast<double>(top) : static_cast<double>(zero) / static_cast<double>(kLog2e);
+            a.most[slot] = zero;
         }
     }
-    const int n = filled;
+    int n = filled;
+    if (n > kList) {
+        // ties with the least (masks, as a rule): those above it, then its lowest tokens one after another
+        uint32_t equal = 0;                            // of the lane's values
+#pragma unroll
+        for (int j = 0; j < EPT; ++j) equal |= x[j] == least && token(j) < a.vocab ? 1u << j : 0u;
+        __syncthreads();
+        if (tid == 0) filled = 0;
+        __syncthreads();
+        collect([least](float v) { return v > least; });
+        __syncthreads();
+        n = filled;
+        while (n < a.picks) {
+            const uint32_t key = equal ? ~static_cast<uint32_t>(token(__ffs(static_cast<int>(equal)) - 1)) : 0u;
+            const uint32_t most = wave_max_u32(key);
+            if (lane == 0) bounds[wave] = most;
+            __syncthreads();
+            const uint32_t c = max(max(bounds[0], bounds[1]), max(bounds[2], bounds[3]));
+            if (c == 0) break;                         // all values of a row's end
+            if (key == c) equal &= equal - 1;
+            if (tid == 0) list[n] = static_cast<u64>(order_key(least)) << 32 | c;
+            ++n;
+            __syncthreads();
+        }
+    }
     if (n <= kList) {
         for (int i = tid; i < n; i += 256) {
             const u64 c = list[i];
@@ -219,14 +282,28 @@ __global__ __launch_bounds__(256, 8) void beam_scan_kernel(BeamArgs a) {
         for (int i = n + tid; i < a.picks; i += 256) out[i] = 0;      // fewer values than picks
         return;
     }
-    // ties: each next best below the last one
+    // more than the list holds above the least lane's maximum: each next best below the last
+    // one, from memory again (values held for this would cost every chunk its registers)
     u64 last = ~0ull;
     for (int k = 0; k < a.picks; ++k) {
         u64 c = 0;
+#pragma unroll 1
+        for (int i = 0; i < LOADS; ++i) {
+            const int t = token(i * VEC);
+            const auto take = [&](float v, int at) {
+                const u64 o = candidate(v, at);
+                if (o < last && o > c) c = o;
+            };
+            if (t + VEC <= a.vocab) {
+                const Wide w = *reinterpret_cast<const Wide*>(from + static_cast<size_t>(t) * size);
 #pragma unroll
-        for (int j = 0; j < EPT; ++j) {
-            const u64 o = candidate(x[j], token(j));
-            if (token(j) < a.vocab && x[j] == x[j] && o < last && o > c) c = o;
+                for (int j = 0; j < VEC; ++j) take(value(w, j), t + j);
+            } else {
+                for (int j = t; j < a.vocab; ++j) {
+                    if constexpr (DT == DT_FP32) take(reinterpret_cast<const float*>(from)[j], j);
+                    else take(act_to_f32(reinterpret_cast<const uint16_t*>(from)[j], DT), j);
+                }
+            }
         }
         c = wave_max_u64(c);
         if (lane == 0) best[wave] = c;

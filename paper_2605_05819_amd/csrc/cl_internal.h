@@ -261,7 +261,7 @@ struct BeamArgs {
     int chunk, splits;             // of a row's logits
     unsigned long long* best;      // [rows][splits][picks], descending
     double* sum;                   // [rows][splits]: of e^(l - most)
-    double* most;                  // the sum's reference, the chunk's largest logit but for rounding; -inf: no logit above
+    double* most;                  // the sum's reference: 0, or the chunk's largest logit; -inf: no logit above
 };
 bool beam_fits(const BeamArgs& a);
 size_t beam_workspace_bytes(BeamArgs a);
