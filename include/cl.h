@@ -664,7 +664,11 @@ size_t cl_attention_workspace(const cl_kv_cache* cache, const cl_kv_batch* batch
  *  k, v       device [num_pages][kv_heads][page_size][head_dim] codes: sign, 4
  *             bits of exponent (bias 7), 3 of fraction; 0x7f and 0xff are NaN.
  *             16-byte aligned
- *  k_scale, v_scale  device uint8 [num_pages][kv_heads][page_size / block]
+ *  k_scale, v_scale  device uint8 [num_pages][kv_heads][page_size / block]; where rows
+ *             stand in a block, 112..135 (CL_FP16) or 10..247 (CL_BF16), and at the
+ *             largest of them codes of 240 at most, as cl_kv_append8 writes them: all
+ *             elements but NaN are then finite values of dtype.  What other bytes
+ *             stand for differs between the calls
  *  block      rows that share a scale: a power of two, 1..page_size
  *  dtype      CL_FP16 or CL_BF16: the type of queries and new tokens, in which
  *             every element that cl_kv_append8 writes is a value exactly

@@ -830,8 +830,8 @@ class KvCache:
 class KvCache8:
     """A pool of pages of 8-bit codes (cl_kv_cache8): k and v uint8
     [num_pages][kv_heads][page_size][head_dim], k_scale and v_scale uint8
-    [num_pages][kv_heads][page_size / block]; dtype (fp16 or bf16) is that of
-    queries and new tokens.  It goes wherever a KvCache does.  Checked once, when
+    [num_pages][kv_heads][page_size / block], 112..135 (fp16) or 10..247 (bf16)
+    where rows stand in a block; dtype (fp16 or bf16) is that of queries and new tokens.  It goes wherever a KvCache does.  Checked once, when
     it is made."""
 
     _append, _attention, _workspace, _read = "cl_kv_append8", "cl_attention8", "cl_attention8_workspace", "cl_kv_read8"
