@@ -1212,11 +1212,14 @@ def gather_rows(arrays, index, outs=None, stream=None):
 class Beams:
     """How a beam search goes on (cl_beams): ``beams`` rows a group, ``picks``
     continuations of them (default: as many), ranked by score / length^alpha;
-    eos: the token that finishes a hypothesis, or -1."""
+    eos: the token that finishes a hypothesis, or -1.  beams and picks are checked
+    when it is made, the rest by the calls."""
 
     def __init__(self, beams, picks=None, eos=-1, alpha=0.0):
         self.beams, self.picks = int(beams), int(beams if picks is None else picks)
         self.eos, self.alpha = int(eos), float(alpha)
+        _need(1 <= self.beams <= 64 and 1 <= self.picks <= 64,
+              "beams and picks must be in 1..64 (got %d, %d)" % (self.beams, self.picks))
         self._bytes = struct.pack("diii4x", self.alpha, self.beams, self.picks, self.eos)
 
     def packed(self):
