@@ -855,7 +855,8 @@ cl_status cl_gather_rows(int32_t num_arrays, const cl_row_array* arrays, int32_t
 
 /*
  * cl_beams -- how a beam search goes on.
- *  alpha  candidates are ranked by score / length^alpha (0: by score)
+ *  alpha  candidates are ranked by score / length^alpha (0: by score); -32..32, where
+ *         every length's power is a finite number
  *  beams  1..64 rows a group;  picks  1..64 continuations a group
  *  eos    the token that finishes a hypothesis, or -1: none
  */
@@ -880,7 +881,7 @@ typedef struct cl_beams {
  *           logits_stride elements from row to row (>= vocab), aligned to its elements
  *  vocab    1..2^19 (CL_EUNSUPPORTED beyond); picks <= beams * vocab
  *  scores   device float32 [groups * beams]
- *  lengths  device int32 [groups * beams], or NULL (alpha 0)
+ *  lengths  device int32 [groups * beams], below 2^31 - 1, or NULL (alpha 0)
  *  finished device int32 [groups * beams], not 0: finished; or NULL (needs eos)
  *  out_scores, tokens, parents  device [groups][picks] float32, int32, int32; a
  *           parent is a row of logits (cl_kv_fork and cl_gather_rows take them)

@@ -1211,7 +1211,7 @@ def gather_rows(arrays, index, outs=None, stream=None):
 
 class Beams:
     """How a beam search goes on (cl_beams): ``beams`` rows a group, ``picks``
-    continuations of them (default: as many), ranked by score / length^alpha;
+    continuations of them (default: as many), ranked by score / length^alpha (-32..32);
     eos: the token that finishes a hypothesis, or -1.  beams and picks are checked
     when it is made, the rest by the calls."""
 

@@ -941,7 +941,7 @@ bool overlap(const void* a, size_t an, const void* b, size_t bn) {
 
 cl_status check_beams(const cl_beams* r, int groups, int vocab, cl::BeamArgs* a, const char* who) {
     if (!r) return fail(CL_EINVAL, "%s: null beams", who);
-    if (!isfinite(r->alpha)) return fail(CL_EINVAL, "%s: alpha must be finite", who);
+    if (!(fabs(r->alpha) <= 32.0)) return fail(CL_EINVAL, "%s: alpha must be in -32..32", who);      // of a length below 2^31: 2^992 at most
     if (r->beams < 1 || r->beams > 64 || r->picks < 1 || r->picks > 64)
         return fail(CL_EINVAL, "%s: beams and picks must be in 1..64 (got %d, %d)", who, r->beams, r->picks);
     if (groups < 1 || vocab < 1) return fail(CL_EINVAL, "%s: groups and vocab must be positive (got %d, %d)", who, groups, vocab);
