@@ -80,3 +80,41 @@ def test_only_long_sequences_are_converted():
     want = cl.attention(c.twin, c.batch, x)
     torch.cuda.synchronize()
     assert torch.equal(out[:600], want[:600]) and torch.equal(out[602:912], want[602:912])
+
+
+@pytest.mark.gpu
+def test_a_graph_whose_sequences_change_places():
+    """One captured call, replayed while starts and lengths move: which sequences are long is the device's to see."""
+    from tests.test_cache8_gpu import Case8
+    Hq, Hkv, D, page = 16, 4, 128, 16
+    c = Case8([520, 1, 1, 300], [640, 640, 640, 640], Hq, Hkv, D, page, torch.float16, block=16, seed=2)
+    x, out = c.q.cuda(), torch.empty_like(c.q, device="cuda")
+    ws = torch.full((cl.attention_workspace(c.cache, c.batch, Hq),), 255, dtype=torch.uint8, device="cuda")
+    start, lens = c.batch.q_start, c.batch.kv_len
+    run = lambda: cl.attention(c.cache, c.batch, x, out=out, ws=ws)  # noqa: E731
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    for q, kv in (([520, 1, 1, 300], [640] * 4), ([1, 300, 520, 1], [640, 512, 600, 33]), ([2, 1, 1, 1], [640, 2, 1, 64]),
+                  ([0, 224, 225, 373], [5, 640, 640, 640]), ([520, 302, 0, 0], [640, 640, 640, 0])):
+        s = [0]
+        for n in q:
+            s.append(s[-1] + n)
+        start.copy_(i32(s)), lens.copy_(i32(kv))
+        want = cl.attention(c.twin, c.batch, x)                # of the 16-bit cache of the same values
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[s[-1]:], torch.full_like(out[s[-1]:], 7.0))
+        # two results' outputs and probabilities, each rounded by 2^-11 at most: 2^-9
+        off = (out[:s[-1]].float() - want[:s[-1]].float()).abs()
+        assert (off <= 2.0 ** -9 * want[:s[-1]].float().abs() + 2.0 ** -12).all()
+        eager = cl.attention(c.cache, c.batch, x)
+        torch.cuda.synchronize()
+        assert torch.equal(out[:s[-1]], eager[:s[-1]])
