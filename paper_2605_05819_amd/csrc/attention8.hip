@@ -134,8 +134,12 @@ __global__ __launch_bounds__(256) void convert_kernel(AttnArgs a, Ahead h, unsig
 // Those of 64-wide heads go 64 rows at a time: the 128-row tile of codes would take a third
 // workgroup's place on the CU (four prompts of 500 to 2000 tokens 157 us, 164 so).  128-wide heads keep
 // their 128 rows, whose loads are further ahead of their use (63 single tokens over 4000
-// keys beside a prompt of 4000 tokens 414 us, 552 by halves).
-template <int D, bool BF, int NQ>
+// keys beside a prompt of 4000 tokens 414 us, 552 by halves), and 9 registers in memory with them,
+// which converted keys do not notice (ragged prompts 853 us with and without).
+template <int D>
+constexpr int kBlocks = D > 128 ? 1 : 2;               // 16-row blocks of a wave: 64 or 128 rows, as the plan has them from kAheadUnits on
+
+template <int D, bool BF>
 __global__ __launch_bounds__(256, 2) void attn_mixed_kernel(AttnArgs a, Plan pl, Ahead h) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     TilePlace place = tile_place<false>(a, pl, static_cast<int>(pl.first + blockIdx.x));
@@ -145,10 +149,10 @@ __global__ __launch_bounds__(256, 2) void attn_mixed_kernel(AttnArgs a, Plan pl,
         a.cache.k = h.k;
         a.cache.v = h.v;
         a.cache.num_pages = h.slots * h.pages;
-        attn_tile<D, BF, false, NQ, false>(a, pl, place, seg, lds);
+        attn_tile<D, BF, false, kBlocks<D>, false>(a, pl, place, seg, lds);
         return;
     }
-    constexpr int EACH = D > 64 ? NQ : 1, PARTS = NQ / EACH;
+    constexpr int EACH = D > 64 ? kBlocks<D> : 1, PARTS = kBlocks<D> / EACH;
     const int first = place.block * PARTS;
 #pragma unroll 1
     for (int n = 0; n < PARTS; ++n) {
@@ -158,27 +162,12 @@ __global__ __launch_bounds__(256, 2) void attn_mixed_kernel(AttnArgs a, Plan pl,
     }
 }
 
-template <int D, bool BF, int NQ>
-hipError_t tiles(const AttnArgs& a, Plan p, const Ahead& h, hipStream_t st) {
-    constexpr int bytes = tile_lds(D);
-    if (bytes > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_mixed_kernel<D, BF, NQ>),
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        if (e != hipSuccess) return e;
-    }
-    return launch_all(static_cast<long long>(a.cache.heads) * p.splits * p.blocks * a.batch.num_seqs,
-                      [&](unsigned first, unsigned count) {
-                          p.first = first;
-                          hipLaunchKernelGGL((attn_mixed_kernel<D, BF, NQ>), dim3(count), dim3(256), bytes, st, a, p, h);
-                      });
-}
-
 // The conversion, then the tiles: of sequences of one length by the 16-bit cache's kernels.
 template <int D, bool BF>
 hipError_t run_ahead(AttnArgs a, Ahead h, void* ws, hipStream_t st) {
     constexpr int ROWS = 16384 / D;
     const unsigned chunks = static_cast<unsigned>(ceil_div(a.batch.key_limit, ROWS));
-    hipError_t e = launch_all(static_cast<long long>(chunks) * h.slots * a.cache.heads, [&](unsigned first, unsigned count) {
+    const hipError_t e = launch_all(static_cast<long long>(chunks) * h.slots * a.cache.heads, [&](unsigned first, unsigned count) {
         a.first = first;
         hipLaunchKernelGGL((convert_kernel<D, BF>), dim3(count), dim3(256), 0, st, a, h, chunks);
     });
@@ -191,11 +180,12 @@ hipError_t run_ahead(AttnArgs a, Ahead h, void* ws, hipStream_t st) {
         a.batch.table_width = h.pages;
         return launch_attention(a, ws, st);
     }
-    Plan p = make_plan(a.cache, a.batch, a.q_heads);
-    place_parts(a, ws, p);
-    if constexpr (D > 128) e = tiles<D, BF, 1>(a, p, h, st);
-    else e = tile_rows(a.cache, a.batch, p.rows) == 64 ? tiles<D, BF, 1>(a, p, h, st) : tiles<D, BF, 2>(a, p, h, st);
-    return e != hipSuccess || p.direct ? e : join<D>(a, p, st);
+    Plan p = make_plan(a.cache, a.batch, a.q_heads);            // kAheadUnits and more take one split: no join
+    static_assert(tile_lds(D) <= 65536, "within what a launch has without asking");
+    return launch_all(static_cast<long long>(a.cache.heads) * p.blocks * a.batch.num_seqs, [&](unsigned first, unsigned count) {
+        p.first = first;
+        hipLaunchKernelGGL((attn_mixed_kernel<D, BF>), dim3(count), dim3(256), tile_lds(D), st, a, p, h);
+    });
 }
 
 }  // namespace

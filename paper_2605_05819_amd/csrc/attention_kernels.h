@@ -1420,23 +1420,6 @@ hipError_t launch(const AttnArgs& a, Plan p, hipStream_t st) {
     });
 }
 
-// The splits' results into the call's.
-template <int D>
-hipError_t join(const AttnArgs& a, Plan p, hipStream_t st) {
-    const size_t rows = static_cast<size_t>(a.batch.tokens) * a.q_heads;
-    if (p.psplits + p.splits <= kRowSplits && rows >= 4096) {
-        constexpr size_t at = 1024 / D;
-        return launch_all(static_cast<long long>((rows + at - 1) / at), [&](unsigned first, unsigned count) {
-            p.first = first;
-            hipLaunchKernelGGL((attn_join_rows_kernel<D>), dim3(count), dim3(256), 0, st, a, p);
-        });
-    }
-    return launch_all(static_cast<long long>(rows), [&](unsigned first, unsigned count) {
-        p.first = first;
-        hipLaunchKernelGGL((attn_join_kernel<D>), dim3(count), dim3(256), 0, st, a, p);
-    });
-}
-
 // The prefix's unit has at least as many rows as a sequence's, so these
 // combinations cover every call (a tiled prefix takes 128-row tiles, a streamed
 // one of 17 to 32 rows streams the sequences' likewise).
@@ -1472,22 +1455,30 @@ hipError_t run(const AttnArgs& a, Plan p, hipStream_t st) {
             : own == T1 ? launch<D, BF, Q8, T2, T1>(a, p, st)
                         : launch<D, BF, Q8, T2, T2>(a, p, st);
     }
-    return e != hipSuccess || p.direct ? e : join<D>(a, p, st);
+    if (e != hipSuccess || p.direct) return e;
+    const size_t rows = static_cast<size_t>(a.batch.tokens) * a.q_heads;
+    if (p.psplits + p.splits <= kRowSplits && rows >= 4096) {
+        constexpr size_t at = 1024 / D;
+        return launch_all(static_cast<long long>((rows + at - 1) / at), [&](unsigned first, unsigned count) {
+            p.first = first;
+            hipLaunchKernelGGL((attn_join_rows_kernel<D>), dim3(count), dim3(256), 0, st, a, p);
+        });
+    }
+    return launch_all(static_cast<long long>(rows), [&](unsigned first, unsigned count) {
+        p.first = first;
+        hipLaunchKernelGGL((attn_join_kernel<D>), dim3(count), dim3(256), 0, st, a, p);
+    });
 }
 
-// Splits' room in the workspace.
-void place_parts(const AttnArgs& a, void* ws, Plan& p) {
-    if (p.direct) return;
-    const size_t n = static_cast<size_t>(p.psplits + p.splits) * a.batch.tokens * a.q_heads;
-    p.part = static_cast<float*>(ws);
-    p.stat = reinterpret_cast<float2*>(static_cast<char*>(ws) + up256(n * a.cache.dim * sizeof(float)));
-}
-
-// The kernels for the heads' width and type.
+// Splits' room in the workspace, and the kernels for the heads' width and type.
 template <bool Q8>
 hipError_t launch_for(const AttnArgs& a, void* ws, hipStream_t st) {
     Plan p = make_plan(a.cache, a.batch, a.q_heads);
-    place_parts(a, ws, p);
+    if (!p.direct) {
+        const size_t n = static_cast<size_t>(p.psplits + p.splits) * a.batch.tokens * a.q_heads;
+        p.part = static_cast<float*>(ws);
+        p.stat = reinterpret_cast<float2*>(static_cast<char*>(ws) + up256(n * a.cache.dim * sizeof(float)));
+    }
     const bool bf = a.cache.dtype == DT_BF16;
     if (a.cache.dim == 64) return bf ? run<64, true, Q8>(a, p, st) : run<64, false, Q8>(a, p, st);
     if (a.cache.dim == 128) return bf ? run<128, true, Q8>(a, p, st) : run<128, false, Q8>(a, p, st);
