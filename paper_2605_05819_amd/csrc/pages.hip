@@ -150,7 +150,7 @@ __device__ __forceinline__ void fork_row(const ForkArgs& a, int i) {
 // rows of one entry 5.7 us, 12 by waves).
 template <int LANES>
 __device__ __forceinline__ void give_pages(const GiveArgs& a) {
-    __shared__ int waves[kScan / 64];
+    __shared__ int waves[kScan / 64], opens[kScan / 64];
     const int tid = threadIdx.x, lane = tid % LANES, team = tid / LANES;
     constexpr int TEAMS = kScan / LANES;
     // the lanes of a row that hold true, as bits from the row's first lane
@@ -204,7 +204,13 @@ __device__ __forceinline__ void give_pages(const GiveArgs& a) {
             a.copy_to[i] = r.open ? r.page : -1;
         }
     }
-    if (__syncthreads_or(open)) {
+    const bool wave_open = __ballot(open) != 0;
+    if ((tid & 63) == 0) opens[tid >> 6] = wave_open;
+    __syncthreads();
+    int any = 0;
+#pragma unroll
+    for (int w = 0; w < kScan / 64; ++w) any |= opens[w];
+    if (any) {
         // The holders that grow leave their pages; one that nobody holds then stays
         // with the first of them (by number, through a.free's place for the page), and
         // all counts are put back.  Other waves' values are read by atomics, past the L1.
